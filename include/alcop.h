@@ -46,7 +46,13 @@
 extern "C" {
 #endif
 
-typedef enum { ALCOP_F16 = 0, ALCOP_BF16 = 1, ALCOP_F32 = 2 /* output only */ } alcop_dtype;
+typedef enum {
+  ALCOP_F16 = 0,
+  ALCOP_BF16 = 1,
+  ALCOP_F32 = 2,              /* products: output only                                       */
+  ALCOP_E4M3 = 3              /* alcop_linear's operands, results of alcop_rmsnorm and        */
+                              /* alcop_quantize_rows: 8 bits, no infinities, largest 448     */
+} alcop_dtype;
 
 typedef enum {
   ALCOP_OK = 0,
@@ -377,6 +383,102 @@ int alcop_splitk_space(const alcop_problem* prob /* host */, alcop_sched* out /*
 int alcop_splitk_auto(const alcop_problem* prob /* host */, int split,
                       alcop_sched* sched_out /* host */, int* split_out /* host */,
                       double* predicted_us /* host */);
+
+/*
+ * A linear layer with what stands between its product and the next operator in the epilogue:
+ *     Z[i][j] = alpha * scale_a[i] * scale_w[j] * sum_k A(i,k) W(k,j) + bias[j]
+ *     C[i][j] = act(Z[i][j]) + residual[i][j]
+ * all of it in fp32 on the accumulators, rounded once to the output type.  `pre` receives Z rounded to that type
+ * (what alcop_linear_backward asks for); the activation sees Z before the rounding.
+ *   A: row-major M x K.  W: transB = 0 row-major K x N, transB = 1 stored N x K (a layer's weights: out x in).
+ *   in: ALCOP_F16, ALCOP_BF16, or ALCOP_E4M3 for both operands (transB = 1), whose values stand for
+ *     e4m3 * scale_a[i] and e4m3 * scale_w[j]; scale_a, scale_w: DEVICE, M and N fp32 values, or NULL = 1.  Scales may
+ *     be given with 16-bit operands too.
+ *   out: ALCOP_F16, ALCOP_BF16 or ALCOP_F32, the type of C, residual and pre.
+ *   act: 0 identity, 1 ReLU, 2 GELU (0.5 z (1 + erf(z / sqrt 2))), 3 GELU (0.5 z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))),
+ *     4 SiLU (z / (1 + exp(-z))).
+ *   residual, pre: DEVICE, M x N, row pitches ldr, ldp >= N, or NULL.  residual may be C itself (same pitch); otherwise C
+ *     and pre overlap nothing that is read, nor each other (columns of one wider matrix do not overlap).
+ *   tail == NULL: alpha = 1 and nothing else.
+ * M is free; N is free with transB = 1, else a multiple of 8; K is a multiple of 8 (ALCOP_E4M3: 16).  A, W: 16-byte aligned,
+ * pitches multiples of 8 (16) elements; bias and scale_w 16-byte aligned.  C, residual and pre may lie at any element
+ * and have any pitch; rows made of 16-byte chunks are faster.  Sums are fp32 and their order fixed: the same
+ * call gives the same bits.  Errors as for alcop_gemm; ALCOP_ERR_UNSUPPORTED for an unknown act, overlaps, or
+ * ALCOP_E4M3 with transB = 0.  No schedule argument: the kernel is picked by measured cost.  The environment variable
+ * ALCOP_LINEAR_KERNEL (a number, read at every call) takes that one of the operand type's and layout's kernels instead,
+ * and ALCOP_ERR_SCHED is returned where there are fewer.
+ */
+typedef struct {
+  float alpha;
+  const void* bias;           /* N fp32 values or NULL */
+  int act;
+  const void* residual;
+  long ldr;
+  void* pre;
+  long ldp;
+  const void* scale_a;
+  const void* scale_w;
+} alcop_linear_tail;
+
+int alcop_linear(const void* A, const void* W, void* C, int M, int N, int K, long lda, long ldw, long ldc, int transB,
+                 alcop_dtype in, alcop_dtype out, const alcop_linear_tail* tail /* host, may be NULL */,
+                 void* hip_stream);
+
+/*
+ * Its gradients.  With dZ = dC * act'(pre), rounded to the type `in` (the products take 16-bit operands):
+ *     dA = alpha * dZ . W^T,   dW = alpha * A^T . dZ  (stored as W is),   dbias[j] = sum_i dZ[i][j] before the rounding;
+ * the residual's gradient is dC.  dA, dW, dbias may be NULL (not all); W is read for dA only, A for dW only.
+ *   dC, A, W, pre: type `in`, ALCOP_F16 or ALCOP_BF16; pre may be NULL if act = 0.  dA, dW: type `out`, which is `in` or
+ *     ALCOP_F32; dbias: N fp32 values.  M is free, N and K are multiples of 8, pointers 16-byte aligned
+ *     (dbias: 4), pitches multiples of 8.
+ *   workspace: DEVICE, 16-byte aligned, at least alcop_linear_backward_workspace_bytes(M, N, K) bytes (which
+ *     returns 0 for arguments no call accepts); needed if act != 0 or dbias is given.  Overwritten; calls that share
+ *     it, captured ones too, must be ordered on one stream.  Outputs and workspace overlap nothing else.
+ * Up to four launches.  dbias is summed in a fixed order, without atomics.
+ */
+size_t alcop_linear_backward_workspace_bytes(int M, int N, int K);
+int alcop_linear_backward(const void* dC, const void* A, const void* W, const void* pre, void* dA, void* dW,
+                          void* dbias, int M, int N, int K, long lddc, long lda, long ldw, long ldp, long ldda,
+                          long lddw, int transB, alcop_dtype in, alcop_dtype out, float alpha, int act,
+                          void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Root-mean-square norm of rows, with the residual's addition in front of it:
+ *     h = x + residual;   rstd[i] = 1 / sqrt(mean_j h[i][j]^2 + eps);   y[i][j] = h[i][j] * rstd[i] * gain[j]
+ * in fp32; total receives h, rstd (rows fp32 values) what the backward pass asks for.
+ *   x, residual, total: type `in` (ALCOP_F16, ALCOP_BF16, ALCOP_F32); gain: cols fp32 values; residual, total, gain (= 1), rstd
+ *     may be NULL.  y is computed from h before its rounding.
+ *   out = ALCOP_F16, ALCOP_BF16, ALCOP_F32: y is stored so.  out = ALCOP_E4M3: 8 bits and a scale per row,
+ *     scale[i] = max(max_j |y[i][j]| / 448, 2^-126) and e4m3(y / scale), as alcop_linear takes them as A.
+ *   A row with an infinity or a NaN gives what the formulas give: its sum is not finite, and an e4m3 row's scale is NaN
+ *   if one of its y is.  mean h^2 has to stay below the fp32 range (|h| below 1e19).
+ * rows >= 1, 1 <= cols <= 32768, any alignment and pitch >= cols (rows of 16-byte chunks are faster).  total may be x or residual,
+ * y may be x or residual if out = in (same pitch); no other output overlaps anything.  One launch.
+ */
+int alcop_rmsnorm(const void* x, const void* residual, const void* gain, void* total, void* y, void* scale,
+                  void* rstd, int rows, int cols, long ldx, long ldr, long ldt, long ldy, float eps, alcop_dtype in,
+                  alcop_dtype out, void* hip_stream);
+
+/*
+ * Its gradients: with xh = total * rstd and t = gain * dy,
+ *     dx = dtotal + rstd * (t - xh * mean_j(t * xh)),   dgain[j] = sum_i dy[i][j] * xh[i][j].
+ * dx is the gradient of x and of the residual; dtotal (may be NULL) is what arrives at total from behind.
+ *   dy, total, dtotal, dx: type `in`; gain (may be NULL = 1), rstd, dgain (may be NULL): fp32.  dx may be dy or dtotal.
+ *   workspace: DEVICE, 16-byte aligned, at least alcop_rmsnorm_backward_workspace_bytes(rows, cols) bytes, needed
+ *     with dgain, as for alcop_linear_backward.
+ * Sizes as for alcop_rmsnorm.  One launch, two with dgain, whose sums have a fixed order.
+ */
+size_t alcop_rmsnorm_backward_workspace_bytes(int rows, int cols);
+int alcop_rmsnorm_backward(const void* dy, const void* total, const void* gain, const void* rstd, const void* dtotal,
+                           void* dx, void* dgain, int rows, int cols, long lddy, long ldt, long lddt, long lddx,
+                           alcop_dtype in, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Rows to 8 bits with a scale each, as alcop_rmsnorm does it, of x as it is: a layer's weights (stored N x K: scale is
+ * alcop_linear's scale_w) or activations between two 8-bit layers.  y: ALCOP_E4M3, rows x cols.
+ */
+int alcop_quantize_rows(const void* x, void* y, void* scale, int rows, int cols, long ldx, long ldy, alcop_dtype in,
+                        void* hip_stream);
 
 /*
  * Feasibility of a schedule for a problem, without launching (the checks the paper's

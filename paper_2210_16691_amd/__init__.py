@@ -15,7 +15,7 @@ from dataclasses import dataclass
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libalcop.so")
 
-F16, BF16, F32 = 0, 1, 2
+F16, BF16, F32, E4M3 = 0, 1, 2, 3
 OP_GEMM, OP_BMM, OP_CONV2D = 0, 1, 2
 
 OK = 0
@@ -29,6 +29,8 @@ EXPORTS = [
     "alcop_corrector_features", "alcop_corrector_fit", "alcop_splitk_workspace_bytes", "alcop_gemm_splitk", "alcop_gemm_splitk_static", "alcop_conv2d_igemm_splitk", "alcop_splitk_auto", "alcop_splitk_space", "alcop_tune_splitk", "alcop_conv2d_igemm_krsc", "alcop_conv2d_igemm_fused", "alcop_conv2d_igemm_dilated", "alcop_sched_variants", "alcop_sched_ranked",
     "alcop_unaligned_workspace_bytes", "alcop_bmm_unaligned", "alcop_conv2d_unaligned_workspace_bytes",
     "alcop_conv2d_igemm_unaligned", "alcop_init",
+    "alcop_linear", "alcop_linear_backward", "alcop_linear_backward_workspace_bytes", "alcop_rmsnorm",
+    "alcop_rmsnorm_backward", "alcop_rmsnorm_backward_workspace_bytes", "alcop_quantize_rows",
 ]
 
 
@@ -60,6 +62,13 @@ def sched(bm, bn, bk, wm, wn, stages=1, reg_stages=1, fuse_inner=0, raster=1, l2
 class Epilogue(ctypes.Structure):
     """Mirror of ``alcop_epilogue``: C = act(alpha * A.B + bias[j])."""
     _fields_ = [("alpha", ctypes.c_float), ("bias", ctypes.c_void_p), ("act", ctypes.c_int)]
+
+
+class LinearTail(ctypes.Structure):
+    """Mirror of ``alcop_linear_tail``."""
+    _fields_ = [("alpha", ctypes.c_float), ("bias", ctypes.c_void_p), ("act", ctypes.c_int), ("residual", ctypes.c_void_p),
+                ("ldr", ctypes.c_long), ("pre", ctypes.c_void_p), ("ldp", ctypes.c_long), ("scale_a", ctypes.c_void_p),
+                ("scale_w", ctypes.c_void_p)]
 
 
 class Problem(ctypes.Structure):
@@ -149,6 +158,21 @@ def _declare(L: ctypes.CDLL) -> ctypes.CDLL:
     L.alcop_splitk_space.argtypes = [pp, sp, i]
     L.alcop_splitk_auto.restype = i
     L.alcop_splitk_auto.argtypes = [pp, i, sp, ip, dp]
+    tp, f = ctypes.POINTER(LinearTail), ctypes.c_float
+    L.alcop_linear.restype = i
+    L.alcop_linear.argtypes = [vp, vp, vp, i, i, i, l, l, l, i, i, i, tp, vp]
+    L.alcop_linear_backward_workspace_bytes.restype = sz
+    L.alcop_linear_backward_workspace_bytes.argtypes = [i, i, i]
+    L.alcop_linear_backward.restype = i
+    L.alcop_linear_backward.argtypes = [vp] * 7 + [i] * 3 + [l] * 6 + [i, i, i, f, i, vp, sz, vp]
+    L.alcop_rmsnorm.restype = i
+    L.alcop_rmsnorm.argtypes = [vp] * 7 + [i, i] + [l] * 4 + [f, i, i, vp]
+    L.alcop_rmsnorm_backward_workspace_bytes.restype = sz
+    L.alcop_rmsnorm_backward_workspace_bytes.argtypes = [i, i]
+    L.alcop_rmsnorm_backward.restype = i
+    L.alcop_rmsnorm_backward.argtypes = [vp] * 7 + [i, i] + [l] * 4 + [i, vp, sz, vp]
+    L.alcop_quantize_rows.restype = i
+    L.alcop_quantize_rows.argtypes = [vp, vp, vp, i, i, l, l, i, vp]
     L.alcop_init.restype = i
     L.alcop_init.argtypes = []
     L.alcop_strerror.restype = ctypes.c_char_p
@@ -171,6 +195,9 @@ def lib() -> ctypes.CDLL:
         m.init(Sched, *[ctypes.cast(f, ctypes.c_void_p).value for f in
                         (L.alcop_gemm_fused, L.alcop_bmm_fused, L.alcop_bmm_unaligned, L.alcop_conv2d_igemm_dilated,
                          L.alcop_conv2d_igemm_unaligned)])
+        m.init_layers(*[ctypes.cast(f, ctypes.c_void_p).value for f in
+                        (L.alcop_linear, L.alcop_linear_backward, L.alcop_rmsnorm, L.alcop_rmsnorm_backward,
+                         L.alcop_quantize_rows)])
         _lib, _marshal, _marshal_lib = L, m, L
     return _lib
 
@@ -373,6 +400,195 @@ def alcop_conv2d_igemm(x, w, y, stride=(1, 1), pad=(0, 0), sched=None, stream=No
                                   stride[0], stride[1], pad[0], pad[1],
                                   _dtype_code(x), _dtype_code(y), _sp(sched), _stream(stream))
     _check(rc, "alcop_conv2d_igemm")
+    return y
+
+
+# ---- linear layers, norms, 8-bit rows --------------------------------------------------------
+def _kind(t) -> int:
+    import torch
+    if t.dtype == torch.float8_e4m3fn:
+        return E4M3
+    return _dtype_code(t)
+
+
+def _rows(name, t, rows=None, cols=None, like=None):
+    """Checks a matrix of rows and returns (rows, cols, pitch).  A single row has no pitch of its own."""
+    if t.dim() != 2 or t.numel() == 0:
+        raise ValueError("%s must be a 2-D tensor with at least one element" % name)
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError("%s: the last dimension must be contiguous" % name)
+    if rows is not None and tuple(t.shape) != (rows, cols):
+        raise ValueError("%s is %s, expected %s" % (name, tuple(t.shape), (rows, cols)))
+    if like is not None and t.dtype != like.dtype:
+        raise ValueError("%s is %s, expected %s" % (name, t.dtype, like.dtype))
+    return t.shape[0], t.shape[1], t.shape[1] if t.shape[0] == 1 else t.stride(0)
+
+
+def _vector(name, t, n):
+    import torch
+    if t is not None and (t.dtype != torch.float32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous()):
+        raise ValueError("%s must be a contiguous fp32 vector of %d values" % (name, n))
+
+
+def _workspace(t):
+    if t is not None and not t.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return _ptr(t), 0 if t is None else t.numel() * t.element_size()
+
+
+def _pitch(t):
+    return 0 if t is None else (t.shape[1] if t.shape[0] == 1 else t.stride(0))
+
+
+def _call_on(t, what, fn, *args, stream=None):
+    """Calls fn(*args, stream) on t's device; without a stream on that device's current one."""
+    if t.is_cuda:
+        import torch
+        with torch.cuda.device(t.device):
+            rc = fn(*args, _stream(stream))
+    else:
+        rc = fn(*args, _stream(stream))
+    _check(rc, what)
+
+
+def alcop_linear(A, W, C, transB=False, alpha=1.0, bias=None, act=0, residual=None, pre=None, scale_a=None, scale_w=None,
+                 stream=None):
+    """C = act(Z) + residual with Z = alpha * scale_a[i] * scale_w[j] * A.W + bias[j]; `pre` receives Z.
+
+    A is [M,K], W [K,N] or, with transB, [N,K] (a layer's weights); both fp16, bf16 or, with transB, e4m3
+    (torch.float8_e4m3fn).  C, residual and pre are [M,N] of one type: fp16, bf16 or fp32; residual may be C.  bias,
+    scale_w (N) and scale_a (M) are fp32 vectors.  act: 0 none, 1 ReLU, 2 GELU (erf), 3 GELU (tanh), 4 SiLU."""
+    if _marshal_lib is _lib is not None:
+        rc = _marshal.linear(A, W, C, transB, alpha, bias, act, residual, pre, scale_a, scale_w, stream)
+        if rc is not None:
+            _check(rc, "alcop_linear")
+            return C
+    M, K, lda = _rows("A", A)
+    N, Kw, ldw = _rows("W", W, like=A)
+    if not transB:
+        N, Kw = Kw, N
+    if Kw != K:
+        raise ValueError("reduction extents differ: A has K = %d, W has K = %d" % (K, Kw))
+    _, _, ldc = _rows("C", C, M, N)
+    _dtype_code(C)
+    for name, t in (("residual", residual), ("pre", pre)):
+        if t is not None:
+            _rows(name, t, M, N, like=C)
+    _vector("bias", bias, N)
+    _vector("scale_a", scale_a, M)
+    _vector("scale_w", scale_w, N)
+    _same_place(A, W, C, bias, residual, pre, scale_a, scale_w)
+    p = lambda t: None if t is None else t.data_ptr()
+    tail = LinearTail(float(alpha), p(bias), int(act), p(residual), _pitch(residual), p(pre), _pitch(pre), p(scale_a),
+                      p(scale_w))
+    _call_on(A, "alcop_linear", lib().alcop_linear, _ptr(A), _ptr(W), _ptr(C), M, N, K, lda, ldw, ldc, int(transB), _kind(A),
+             _kind(C), ctypes.byref(tail), stream=stream)
+    return C
+
+
+def alcop_linear_backward_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(lib().alcop_linear_backward_workspace_bytes(M, N, K))
+
+
+def alcop_linear_backward(dC, A, W, dA=None, dW=None, dbias=None, pre=None, act=0, alpha=1.0, transB=False, workspace=None,
+                          stream=None):
+    """Gradients of alcop_linear: with dZ = dC * act'(pre), dA = alpha * dZ.W^T, dW = alpha * A^T.dZ (stored as W is) and
+    dbias = the column sums of dZ; what is None is left out.  dC, A, W, pre have one type, fp16 or bf16; dA and
+    dW that one or both fp32; dbias fp32.  workspace: at least alcop_linear_backward_workspace_bytes(M, N, K) bytes, for
+    an activation or dbias."""
+    if _marshal_lib is _lib is not None:
+        rc = _marshal.linear_backward(dC, A, W, dA, dW, dbias, pre, act, alpha, transB, workspace, stream)
+        if rc is not None:
+            _check(rc, "alcop_linear_backward")
+            return
+    M, N, lddc = _rows("dC", dC)
+    _, K, lda = _rows("A", A, like=dC)
+    _rows("A", A, M, K)
+    _, _, ldw = _rows("W", W, *((N, K) if transB else (K, N)), like=dC)
+    if dA is not None:
+        _rows("dA", dA, M, K, like=dW)
+    if dW is not None:
+        _rows("dW", dW, *W.shape)
+    if pre is not None:
+        _rows("pre", pre, M, N, like=dC)
+    _vector("dbias", dbias, N)
+    _same_place(dC, A, W, dA, dW, dbias, pre, workspace)
+    ws, ws_bytes = _workspace(workspace)
+    out = dA if dA is not None else dW
+    _call_on(dC, "alcop_linear_backward", lib().alcop_linear_backward, _ptr(dC), _ptr(A), _ptr(W), _ptr(pre), _ptr(dA),
+             _ptr(dW), _ptr(dbias), M, N, K, lddc, lda, ldw, _pitch(pre), _pitch(dA), _pitch(dW), int(transB), _kind(dC),
+             _kind(dC if out is None else out), float(alpha), int(act), ws, ws_bytes, stream=stream)
+
+
+def alcop_rmsnorm(x, gain, y, residual=None, total=None, scale=None, rstd=None, eps=1e-6, stream=None):
+    """y = h * rstd * gain with h = x + residual and rstd = 1 / sqrt(mean(h^2) + eps) per row; total receives h.
+
+    x, residual and total are [rows, cols] of one type (fp16, bf16, fp32); gain, rstd and scale are fp32 vectors of
+    cols, rows and rows values; residual, total, gain and rstd may be None.  y is fp16, bf16, fp32 or e4m3, which needs
+    scale: max(max |y| / 448, 2^-126) of the row, y then holding y / scale."""
+    if _marshal_lib is _lib is not None:
+        rc = _marshal.rmsnorm(x, gain, y, residual, total, scale, rstd, eps, stream)
+        if rc is not None:
+            _check(rc, "alcop_rmsnorm")
+            return y
+    rows, cols, ldx = _rows("x", x)
+    _, _, ldy = _rows("y", y, rows, cols)
+    for name, t in (("residual", residual), ("total", total)):
+        if t is not None:
+            _rows(name, t, rows, cols, like=x)
+    _vector("gain", gain, cols)
+    _vector("scale", scale, rows)
+    _vector("rstd", rstd, rows)
+    _same_place(x, y, gain, residual, total, scale, rstd)
+    _call_on(x, "alcop_rmsnorm", lib().alcop_rmsnorm, _ptr(x), _ptr(residual), _ptr(gain), _ptr(total), _ptr(y), _ptr(scale),
+             _ptr(rstd), rows, cols, ldx, _pitch(residual), _pitch(total), ldy, float(eps), _kind(x), _kind(y), stream=stream)
+    return y
+
+
+def alcop_rmsnorm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().alcop_rmsnorm_backward_workspace_bytes(rows, cols))
+
+
+def alcop_rmsnorm_backward(dy, total, gain, rstd, dx, dgain=None, dtotal=None, workspace=None, stream=None):
+    """Gradients of alcop_rmsnorm: dx (of x and of the residual), to which the gradient dtotal that arrives at total
+    is added, and dgain.  dy, total, dtotal and dx have one type; dx may be dy or dtotal.  workspace: at least
+    alcop_rmsnorm_backward_workspace_bytes(rows, cols) bytes, for dgain."""
+    if _marshal_lib is _lib is not None:
+        rc = _marshal.rmsnorm_backward(dy, total, gain, rstd, dx, dgain, dtotal, workspace, stream)
+        if rc is not None:
+            _check(rc, "alcop_rmsnorm_backward")
+            return dx
+    rows, cols, lddy = _rows("dy", dy)
+    _, _, ldt = _rows("total", total, rows, cols, like=dy)
+    _, _, lddx = _rows("dx", dx, rows, cols, like=dy)
+    if dtotal is not None:
+        _rows("dtotal", dtotal, rows, cols, like=dy)
+    _vector("gain", gain, cols)
+    _vector("dgain", dgain, cols)
+    _vector("rstd", rstd, rows)
+    _same_place(dy, total, dx, dtotal, gain, dgain, rstd, workspace)
+    ws, ws_bytes = _workspace(workspace)
+    _call_on(dy, "alcop_rmsnorm_backward", lib().alcop_rmsnorm_backward, _ptr(dy), _ptr(total), _ptr(gain), _ptr(rstd),
+             _ptr(dtotal), _ptr(dx), _ptr(dgain), rows, cols, lddy, ldt, _pitch(dtotal), lddx, _kind(dy), ws, ws_bytes,
+             stream=stream)
+    return dx
+
+
+def alcop_quantize_rows(x, y, scale, stream=None):
+    """Rows to e4m3 with a scale each: scale = max(max |x| / 448, 2^-126), y = x / scale."""
+    if _marshal_lib is _lib is not None:
+        rc = _marshal.quantize_rows(x, y, scale, stream)
+        if rc is not None:
+            _check(rc, "alcop_quantize_rows")
+            return y
+    rows, cols, ldx = _rows("x", x)
+    _, _, ldy = _rows("y", y, rows, cols)
+    if _kind(y) != E4M3:
+        raise ValueError("y must be torch.float8_e4m3fn")
+    _vector("scale", scale, rows)
+    _same_place(x, y, scale)
+    _call_on(x, "alcop_quantize_rows", lib().alcop_quantize_rows, _ptr(x), _ptr(y), _ptr(scale), rows, cols, ldx, ldy, _kind(x),
+             stream=stream)
     return y
 
 

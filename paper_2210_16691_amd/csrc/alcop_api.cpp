@@ -19,6 +19,7 @@
 #include "alcop_model.h"
 #include "alcop_registry.h"
 #include "alcop_convres.hip.h"
+#include "alcop_linear.h"
 
 namespace alcop {
 
@@ -1221,6 +1222,22 @@ XForm choose_xform(const Call& c, int C, double x_room)
 }
 
 }  // namespace
+// dW of a linear layer: the sum runs over the layer's rows, any number of them.  Both operands run along their
+// m and n there, so that rows past K lie outside the descriptors of every kernel of these layouts and read as zero; the
+// problem is checked, and its kernel picked, with K rounded up to a multiple of 8.
+int gradient_product(const void* A, const void* B, void* C, int M, int N, int K, long lda, long ldb, long ldc,
+                     alcop_dtype in, alcop_dtype out, float alpha, void* stream)
+{
+  if (K > 0x7ffffff8) return ALCOP_ERR_SIZE;
+  Call c = gemm_call(ALCOP_OP_GEMM, A, B, C, 1, M, N, (K + 7) & ~7, lda, ldb, ldc, 0, 0, 0, 1, 0, in, out);
+  c.alpha = alpha;
+  Resolved r;
+  const int rc = resolve(c, nullptr, &r);
+  if (rc) return rc;
+  c.K = K;
+  return launch_call(c, r.s, r.e, (hipStream_t)stream);
+}
+
 }  // namespace alcop
 
 using namespace alcop;
@@ -1473,6 +1490,7 @@ int alcop_init(void)
   for (const KernelEntry& e : registry())
     if (e.prepare && e.prepare() != hipSuccess) return ALCOP_ERR_LAUNCH;
   if (prepare_direct() != hipSuccess || prepare_copies() != hipSuccess) return ALCOP_ERR_LAUNCH;
+  if (prepare_layers() != hipSuccess) return ALCOP_ERR_LAUNCH;
   void* scratch = nullptr;
   size_t bytes = 0;
   if (splitk_scratch(&scratch, &bytes) != hipSuccess) return ALCOP_ERR_LAUNCH;

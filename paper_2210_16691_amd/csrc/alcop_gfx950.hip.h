@@ -10,6 +10,9 @@
 //                                 D lane l = column l%16, rows 4*(l/16)..+3
 //   v_mfma_f32_32x32x16_{f16,bf16}  X lane l = row l%32, k = 8*(l/32)..+7; Y likewise by column;
 //                                 D lane l = column l%32, rows 8*(v/4) + 4*(l/32) + v%4
+// The matrix instructions on 8-bit elements add less exactly: of the products one of them sums (16, 32 or 64 terms),
+// what lies below 2^-13 of the largest is cut off, 2^-12 to 2^-11 of the largest product per instruction on random
+// numbers.  Where sums have to be those of fp32, e4m3 is widened to bf16, exactly, in registers.
 // The direct-to-LDS loads and the waits are inline asm on purpose: the compiler treats a builtin
 // LDS-DMA as a store to LDS and would drain the vector-memory counter before the next LDS read,
 // which serialises the stages.  With asm it sees neither the loads nor their counter; the waits
@@ -109,13 +112,24 @@ struct Gfx950 {
   // nothing may be scheduled across this point
   __device__ static __forceinline__ void sched_fence() { __builtin_amdgcn_sched_barrier(0); }
 
+  // eight e4m3 as bf16
+  __device__ static __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi)
+  {
+    const auto a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+    const auto c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+    return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  }
+
   template <int DT>
   __device__ static __forceinline__ f32x16 mma(u32x4 x, u32x4 y, f32x16 acc)
   {
     if constexpr (DT == 0)
       return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x),
                                                     __builtin_bit_cast(f16x8, y), acc, 0, 0, 0);
-    else
+    else if constexpr (DT == 2) {
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(x[0], x[1]), widen(y[0], y[1]), acc, 0, 0, 0);
+      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen(x[2], x[3]), widen(y[2], y[3]), acc, 0, 0, 0);
+    } else
       return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
                                                      __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
   }
@@ -126,7 +140,10 @@ struct Gfx950 {
     if constexpr (DT == 0)
       return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x),
                                                     __builtin_bit_cast(f16x8, y), acc, 0, 0, 0);
-    else
+    else if constexpr (DT == 2) {
+      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(x[0], x[1]), widen(y[0], y[1]), acc, 0, 0, 0);
+      return __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(x[2], x[3]), widen(y[2], y[3]), acc, 0, 0, 0);
+    } else
       return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x),
                                                      __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
   }
@@ -196,6 +213,23 @@ struct Gfx950 {
   {
     return (OT)v;
   }
+
+  // ---- operations of the epilogue of linear layers and of the row kernels ---------------------------------
+  __device__ static __forceinline__ u32x2 global_load8(const void* ptr) { return *(const u32x2*)ptr; }
+  __device__ static __forceinline__ void global_store_u8(void* ptr, uint8_t v) { *(uint8_t*)ptr = v; }
+  __device__ static __forceinline__ float f16_bits(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }
+  // two floats -> two e4m3 in the low 16 bits, round to nearest even; magnitudes up to 464 give at most 448, NaN stays
+  __device__ static __forceinline__ uint32_t cvt_e4m3(float a, float b)
+  {
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false) & 0xffffu;
+  }
+  // the value that lane (lane ^ mask) of the wave passes
+  __device__ static __forceinline__ uint32_t xor_lanes(uint32_t v, int mask) { return (uint32_t)__shfl_xor((int)v, mask); }
+  __device__ static __forceinline__ void lds_write1(uint32_t addr, uint32_t v) { *(ALCOP_LDS uint32_t*)(uintptr_t)addr = v; }
+  __device__ static __forceinline__ float sqrt(float v) { return sqrtf(v); }
+  __device__ static __forceinline__ float exp2(float v) { return __builtin_amdgcn_exp2f(v); }
+  __device__ static __forceinline__ float rcp(float v) { return __builtin_amdgcn_rcpf(v); }    // within 1 ulp
+  __device__ static __forceinline__ float erf(float v) { return erff(v); }
 };
 
 }  // namespace alcop

@@ -261,7 +261,7 @@ struct Opnd {
   }
 };
 
-// One kernel = one KCfg.  DT: 0 fp16, 1 bf16 operands.  BM x BN x BK: block tile; WM x WN: wave
+// One kernel = one KCfg.  DT: 0 fp16, 1 bf16 operands (2, pairs of e4m3: alcop_linear.hip.h).  BM x BN x BK: block tile; WM x WN: wave
 // tile.  S: stages of the LDS ring (1 = unpipelined); R: register slots for fragments (2 = the
 // inner, LDS -> register pipeline); FUSE: the inner pipeline runs across k-tiles (Fig. 3(d)).
 // BL / AL: operand layouts; AM: how the A tile is produced (matrix or convolution gather);
@@ -273,6 +273,7 @@ struct KCfg {
   static constexpr int DT = DT_, BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_;
   static constexpr int S = S_, R = R_, FUSE = FUSE_, BL = BL_, AM = AM_, AL = AL_, SK = SK_;
   static constexpr int PF = PF_;
+  static constexpr bool LINEAR = false;   // the epilogue of alcop_linear.hip.h in place of the one below
   static constexpr int WAVES_M = BM / WM, WAVES_N = BN / WN, NWAVES = WAVES_M * WAVES_N;
   static constexpr int NT = NWAVES * 64;
   // AL: 0 = A stored M x K, 1 = A stored K x M.  BL: 0 = B stored K x N, 1 = B stored N x K.
@@ -655,8 +656,12 @@ __device__ __forceinline__ void store_chunk_if(const Params& p, char* dst, int n
   store_elements<OT, HW>(p, dst, (ok & !whole) ? n : p.Nv, v);
 }
 
-template <class C, class HW>
-__device__ __forceinline__ void mainloop_body(const Params& p)
+// the epilogue of linear layers (alcop_linear.hip.h)
+template <class C, class HW, class P>
+__device__ __forceinline__ void linear_tile(const P& p, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, uint32_t ebase, int lane);
+
+template <class C, class HW, class P = Params>
+__device__ __forceinline__ void mainloop_body(const P& p)
 {
   constexpr int BM = C::BM, BN = C::BN, BK = C::BK, WM = C::WM, WN = C::WN, S = C::S;
   constexpr int TM = C::TM, TN = C::TN, NKI = C::NKI, NLA = C::NLA, NLB = C::NLB;
@@ -1079,6 +1084,13 @@ __device__ __forceinline__ void mainloop_body(const Params& p)
       }
       if constexpr (S >= 2) stage_end();
     }
+  }
+  if constexpr (C::LINEAR) {
+    HW::template wait_vm<0>();
+    HW::wait_lds();
+    HW::block_barrier();   // every wave has finished reading the ring
+    linear_tile<C, HW>(p, acc, tm * BM + wm * WM, tn * BN + wn * WN, lds0 + (uint32_t)wave * C::EPI_WAVE_BYTES, lane);
+    return;
   }
   const bool fused = p.alpha != 1.0f || p.bias != nullptr || p.act != 0;
   f32x4 bv[C::BIAS_GROUPS];

@@ -82,6 +82,7 @@ struct WaveOpnd {
 template <int DT_, int BM_, int BN_, int NW_, int S_, int BL_, int AM_, int AL_ = 0>
 struct WCfg {
   static constexpr int DT = DT_, BM = BM_, BN = BN_, BK = 64, NW = NW_, S = S_, BL = BL_, AM = AM_, AL = AL_;
+  static constexpr bool LINEAR = false;   // the epilogue of alcop_linear.hip.h
   static constexpr int NT = NW * 64;
   using OA = WaveOpnd<AL ? LAY_MN : LAY_K, BM>;
   using OB = WaveOpnd<BL ? LAY_K : LAY_MN, BN>;
@@ -97,8 +98,12 @@ struct WCfg {
   static_assert(AM >= 0 && AM <= 2 && !(AM != 0 && AL == 1), "A producer");
 };
 
-template <class C, class HW>
-__device__ __forceinline__ void ksplit_body(const Params& p)
+// the epilogue of linear layers (alcop_linear.hip.h)
+template <class HW, class P>
+__device__ __forceinline__ void linear_group(const P& p, int m, int n, const f32x4& sum);
+
+template <class C, class HW, class P = Params>
+__device__ __forceinline__ void ksplit_body(const P& p)
 {
   constexpr int BM = C::BM, BN = C::BN, BK = C::BK, S = C::S, TM = C::TM, TN = C::TN;
   using OA = typename C::OA;
@@ -295,7 +300,8 @@ __device__ __forceinline__ void ksplit_body(const Params& p)
     const int row = g / GPR, col = (g % GPR) * 4;
     const int m = tm * BM + row, n = tn * BN + col;
     f32x4 b = {0.f, 0.f, 0.f, 0.f};
-    if (p.bias != nullptr) b = HW::global_load_f32x4(p.bias + (n < p.N ? n : 0));
+    if constexpr (!C::LINEAR)
+      if (p.bias != nullptr) b = HW::global_load_f32x4(p.bias + (n < p.N ? n : 0));
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < C::NW; w++) {
@@ -303,6 +309,10 @@ __device__ __forceinline__ void ksplit_body(const Params& p)
       const f32x4 f = __builtin_bit_cast(f32x4, t);
 #pragma unroll
       for (int e = 0; e < 4; e++) v[e] += f[e];
+    }
+    if constexpr (C::LINEAR) {
+      linear_group<HW>(p, m, n, v);
+      continue;
     }
     if (fused) {
 #pragma unroll

@@ -1,0 +1,401 @@
+// Host code of the linear layers and the row operators: argument checks, choice of the kernel, launches.
+// Declarations and argument contracts are in include/alcop.h.
+#include <algorithm>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+
+#include "alcop_dispatch.h"
+#include "alcop_linear.h"
+
+namespace alcop {
+namespace {
+
+const std::vector<LinearKernel>& linear_kernels()
+{
+  static const std::vector<LinearKernel> table = [] {
+    std::vector<LinearKernel> t;
+    register_linear_f16(t);
+    register_linear_bf16(t);
+    register_linear_e4m3(t);
+    return t;
+  }();
+  return table;
+}
+
+int size_of(alcop_dtype t) { return t == ALCOP_F32 ? 4 : t == ALCOP_E4M3 ? 1 : 2; }
+bool is_half(alcop_dtype t) { return t == ALCOP_F16 || t == ALCOP_BF16; }
+bool aligned(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
+
+// A matrix in memory, in bytes.
+struct Span {
+  const char* p;
+  double rows, row, pitch;
+  Span(const void* ptr, int rows_, int cols, long ld, int size)
+      : p((const char*)ptr), rows(rows_), row((double)cols * size), pitch((double)ld * size)
+  {
+  }
+};
+// Whether two matrices share bytes.  Column ranges of one buffer, rows equally far apart, do not.
+bool meet(const Span& a, const Span& b)
+{
+  if (!a.p || !b.p) return false;
+  const double ea = (a.rows - 1) * a.pitch + a.row, eb = (b.rows - 1) * b.pitch + b.row;
+  if (!(a.p < b.p + (size_t)eb && b.p < a.p + (size_t)ea)) return false;
+  if (a.pitch != b.pitch || a.rows < 2 || b.rows < 2) return true;
+  const long pitch = (long)a.pitch;
+  const long d = (long)((((b.p - a.p) % pitch) + pitch) % pitch);      // b's columns start d bytes behind a's
+  return !(d >= (long)a.row && d + (long)b.row <= pitch);
+}
+bool same(const Span& a, const Span& b) { return a.p == b.p && (a.rows < 2 || a.pitch == b.pitch) && a.row == b.row; }
+
+// The kernel of the lowest measured cost (alcop_dispatch.h); an e4m3 problem counts as one of half its K on 16 bits,
+// which moves as many bytes and takes as many matrix instructions.
+const LinearKernel* pick(int dt, int bl, const alcop_problem& p)
+{
+  const LinearKernel* best = nullptr;
+  double best_us = 0;
+  const char* env = std::getenv("ALCOP_LINEAR_KERNEL");       // a tuning and test knob: its number among those of the layout
+  int nr = 0;
+  for (const LinearKernel& k : linear_kernels()) {
+    if (k.dt != dt || k.bl != bl) continue;
+    if (env && *env) {
+      if (nr++ == std::atoi(env)) return &k;
+      continue;
+    }
+    for (const MeasuredCost& m : kMeasured) {
+      if (std::memcmp(&m.s, &k.s, sizeof(k.s)) != 0 || !measured_applies(p, m)) continue;
+      const double us = measured_us(p, m);
+      if (!best || us < best_us) {
+        best = &k;
+        best_us = us;
+      }
+    }
+  }
+  return best;
+}
+
+size_t r256(double bytes) { return ((size_t)bytes + 255) & ~(size_t)255; }
+
+// Blocks of rows whose sums of the bias's gradient are added by a second kernel, and their rows: enough blocks to fill
+// the card (2048 with 512 columns each), at most 256 sums to a column.
+int act_grad_rows(int M, int N)
+{
+  const int strips = (N + ACT_COLS - 1) / ACT_COLS;
+  const int want = std::max(1, std::min(256, 2048 / strips));
+  return std::max(4, (M + want - 1) / want);
+}
+
+// Groups of threads that walk the rows of a norm's gradient.
+int norm_groups(int rows, int cols)
+{
+  const int per = rows_per_block(cols);
+  const int blocks = (rows + per - 1) / per;
+  return std::min(blocks, 1024) * per;
+}
+
+}  // namespace
+
+hipError_t prepare_layers()
+{
+  for (const LinearKernel& k : linear_kernels()) {
+    const hipError_t rc = k.prepare();
+    if (rc != hipSuccess) return rc;
+  }
+  return prepare_rows();
+}
+
+}  // namespace alcop
+
+using namespace alcop;
+
+extern "C" {
+
+int alcop_linear(const void* A, const void* W, void* C, int M, int N, int K, long lda, long ldw, long ldc, int transB,
+                 alcop_dtype in, alcop_dtype out, const alcop_linear_tail* tail, void* hip_stream)
+{
+  alcop_linear_tail t;
+  std::memset(&t, 0, sizeof(t));
+  t.alpha = 1.0f;
+  if (tail) t = *tail;
+  transB = transB ? 1 : 0;
+  if (!A || !W || !C) return ALCOP_ERR_NULL;
+  if (!is_half(in) && in != ALCOP_E4M3) return ALCOP_ERR_DTYPE;
+  if (!is_half(out) && out != ALCOP_F32) return ALCOP_ERR_DTYPE;
+  if (t.act < 0 || t.act > 4 || (in == ALCOP_E4M3 && !transB)) return ALCOP_ERR_UNSUPPORTED;
+  const int esz = size_of(in), osz = size_of(out), unit = 16 / esz;
+  if (M <= 0 || N <= 0 || K <= 0 || K % unit || (!transB && N % unit)) return ALCOP_ERR_SHAPE;
+  if (lda < K || ldw < (transB ? K : N) || ldc < N || (t.residual && t.ldr < N) || (t.pre && t.ldp < N)) return ALCOP_ERR_SHAPE;
+  if (!aligned(A, 16) || !aligned(W, 16) || lda % unit || ldw % unit) return ALCOP_ERR_ALIGN;
+  if (!aligned(C, osz) || !aligned(t.residual, osz) || !aligned(t.pre, osz)) return ALCOP_ERR_ALIGN;
+  if (!aligned(t.bias, 16) || !aligned(t.scale_w, 16) || !aligned(t.scale_a, 4)) return ALCOP_ERR_ALIGN;
+  const long far = 1L << 30;
+  if (lda >= far || ldw >= far || ldc >= far || t.ldr >= far || t.ldp >= far) return ALCOP_ERR_SIZE;
+
+  alcop_problem p;
+  std::memset(&p, 0, sizeof(p));
+  p.op = ALCOP_OP_GEMM;
+  p.batch = 1;
+  p.M = M;
+  p.N = N;
+  p.K = in == ALCOP_E4M3 ? K / 2 : K;
+  p.transB = transB;
+  p.in = in == ALCOP_F16 ? ALCOP_F16 : ALCOP_BF16;
+  p.out = out;
+  const LinearKernel* k = pick(in == ALCOP_E4M3 ? 2 : in == ALCOP_BF16 ? 1 : 0, transB, p);
+  if (!k) return ALCOP_ERR_SCHED;
+  // 32-bit byte offsets from a tile's origin, rows past the end of a partial k-tile included
+  const double rows = std::min(k->s.bm, M), cols = std::min(k->s.bn, N);
+  const double kceil = (double)((p.K + k->s.bk - 1) / k->s.bk) * k->s.bk;
+  if (esz * (rows * (double)lda) >= 2147483648.0 || (transB ? esz * (cols * (double)ldw) : 2.0 * kceil * ldw) >= 2147483648.0)
+    return ALCOP_ERR_SIZE;
+  const long ntm = ((long)M + k->s.bm - 1) / k->s.bm, ntn = ((long)N + k->s.bn - 1) / k->s.bn;
+  if (ntm * ntn > 0x7fffffffL) return ALCOP_ERR_SHAPE;
+
+  const Span c(C, M, N, ldc, osz), r(t.residual, M, N, t.ldr, osz), z(t.pre, M, N, t.ldp, osz);
+  const Span read[] = {Span(A, M, K, lda, esz), Span(W, transB ? N : K, transB ? K : N, ldw, esz), Span(t.bias, 1, N, N, 4),
+                       Span(t.scale_a, 1, M, M, 4), Span(t.scale_w, 1, N, N, 4)};
+  for (const Span& s : read)
+    if (meet(c, s) || meet(z, s)) return ALCOP_ERR_UNSUPPORTED;
+  if (meet(c, z) || meet(r, z) || (meet(c, r) && !same(c, r))) return ALCOP_ERR_UNSUPPORTED;
+
+  LinearArgs a;
+  a.A = A;
+  a.W = W;
+  a.C = C;
+  a.residual = t.residual;
+  a.pre = t.pre;
+  a.bias = (const float*)t.bias;
+  a.sa = (const float*)t.scale_a;
+  a.sw = (const float*)t.scale_w;
+  a.M = M;
+  a.N = N;
+  a.K = p.K;
+  a.lda = (int)(in == ALCOP_E4M3 ? lda / 2 : lda);
+  a.ldw = (int)(in == ALCOP_E4M3 ? ldw / 2 : ldw);
+  a.ldc = (int)ldc;
+  a.ldr = t.residual ? (int)t.ldr : 0;
+  a.ldp = t.pre ? (int)t.ldp : 0;
+  a.alpha = t.alpha;
+  const int chunk = 16 / osz;
+  const bool chunks = N % 8 == 0 && aligned(C, 16) && aligned(t.residual, 16) && aligned(t.pre, 16) && ldc % chunk == 0 &&
+                      a.ldr % chunk == 0 && a.ldp % chunk == 0;
+  a.flags = (int)out | t.act << 2 | (chunks ? 32 : 0);
+  if (std::getenv("ALCOP_LOG"))
+    std::fprintf(stderr, "alcop: linear M %d N %d K %d in %d -> tile %dx%dx%d waves %dx%d S%d R%d F%d variant %d grid %ld\n", M,
+                 N, K, (int)in, k->s.bm, k->s.bn, k->s.bk, k->s.wm, k->s.wn, k->s.stages, k->s.reg_stages, k->s.fuse_inner,
+                 k->s.variant, ntm * ntn);
+  return k->launch(a, dim3((unsigned)(ntm * ntn)), (hipStream_t)hip_stream) == hipSuccess ? ALCOP_OK : ALCOP_ERR_LAUNCH;
+}
+
+size_t alcop_linear_backward_workspace_bytes(int M, int N, int K)
+{
+  if (M <= 0 || N <= 0 || K <= 0 || N % 8 || K % 8) return 0;
+  const int rows = act_grad_rows(M, N);
+  return r256(2.0 * M * N) + r256(4.0 * N * ((M + (double)rows - 1) / rows));
+}
+
+int alcop_linear_backward(const void* dC, const void* A, const void* W, const void* pre, void* dA, void* dW, void* dbias,
+                          int M, int N, int K, long lddc, long lda, long ldw, long ldp, long ldda, long lddw, int transB,
+                          alcop_dtype in, alcop_dtype out, float alpha, int act, void* workspace, size_t workspace_bytes,
+                          void* hip_stream)
+{
+  transB = transB ? 1 : 0;
+  if (!dC || (!dA && !dW && !dbias) || (dA && !W) || (dW && !A)) return ALCOP_ERR_NULL;
+  if (!is_half(in) || (out != in && out != ALCOP_F32)) return ALCOP_ERR_DTYPE;
+  if (act < 0 || act > 4) return ALCOP_ERR_UNSUPPORTED;
+  if (act && !pre) return ALCOP_ERR_NULL;
+  if ((act || dbias) && !workspace) return ALCOP_ERR_NULL;
+  if (M <= 0 || N <= 0 || K <= 0 || N % 8 || K % 8) return ALCOP_ERR_SHAPE;
+  const int w_rows = transB ? N : K, w_cols = transB ? K : N;
+  if (lddc < N || (dW && lda < K) || (dA && ldw < w_cols) || (act && ldp < N) || (dA && ldda < K) || (dW && lddw < w_cols))
+    return ALCOP_ERR_SHAPE;
+  if (!aligned(dC, 16) || !aligned(workspace, 16) || !aligned(dbias, 4) || lddc % 8) return ALCOP_ERR_ALIGN;
+  if (act && (!aligned(pre, 16) || ldp % 8)) return ALCOP_ERR_ALIGN;
+  if (dA && (!aligned(dA, 16) || !aligned(W, 16) || ldda % 8 || ldw % 8)) return ALCOP_ERR_ALIGN;
+  if (dW && (!aligned(dW, 16) || !aligned(A, 16) || lddw % 8 || lda % 8)) return ALCOP_ERR_ALIGN;
+  const long far = 1L << 30;
+  if (lddc >= far || (act && ldp >= far) || (dA && (ldda >= far || ldw >= far)) || (dW && (lddw >= far || lda >= far)))
+    return ALCOP_ERR_SIZE;
+  if ((act || dbias) && workspace_bytes < alcop_linear_backward_workspace_bytes(M, N, K)) return ALCOP_ERR_SIZE;
+
+  // outputs overlap nothing that is read, nor each other
+  const int osz = size_of(out);
+  const Span outs[] = {Span(dA, M, K, ldda, osz), Span(dW, w_rows, w_cols, lddw, osz), Span(dbias, 1, N, N, 4),
+                       Span(act || dbias ? workspace : nullptr, 1, 1, 1, 1)};
+  const Span ins[] = {Span(dC, M, N, lddc, 2), Span(dW ? A : nullptr, M, K, lda, 2), Span(dA ? W : nullptr, w_rows, w_cols, ldw, 2),
+                      Span(act ? pre : nullptr, M, N, ldp, 2)};
+  for (int i = 0; i < 4; i++) {
+    Span o = outs[i];
+    if (i == 3) o.row = o.pitch = (double)workspace_bytes;
+    for (const Span& s : ins)
+      if (meet(o, s)) return ALCOP_ERR_UNSUPPORTED;
+    for (int j = 0; j < i; j++)
+      if (meet(o, outs[j])) return ALCOP_ERR_UNSUPPORTED;
+  }
+
+  hipStream_t st = (hipStream_t)hip_stream;
+  const void* dZ = dC;
+  long lddz = lddc;
+  if (act || dbias) {
+    ActGradArgs g;
+    std::memset(&g, 0, sizeof(g));
+    g.rows_per_block = act_grad_rows(M, N);
+    const int blocks = (M + g.rows_per_block - 1) / g.rows_per_block;
+    g.dc = dC;
+    g.pre = act ? pre : nullptr;
+    g.M = M;
+    g.N = N;
+    g.lddc = lddc;
+    g.ldp = ldp;
+    g.act = act;
+    g.dt = in == ALCOP_BF16;
+    if (act && (dA || dW)) {
+      dZ = g.dz = workspace;
+      lddz = g.ldz = N;
+    }
+    float* sums = (float*)((char*)workspace + r256(2.0 * M * N));
+    if (dbias) g.partial = blocks == 1 ? (float*)dbias : sums;
+    if (launch_act_grad(g, st) != hipSuccess) return ALCOP_ERR_LAUNCH;
+    if (dbias && blocks > 1) {
+      const ColumnSumArgs s{sums, (float*)dbias, blocks, N};
+      if (launch_column_sums(s, st) != hipSuccess) return ALCOP_ERR_LAUNCH;
+    }
+  }
+  if (dA) {
+    const alcop_epilogue e{alpha, nullptr, 0};
+    const int rc = alcop_gemm_fused(dZ, W, dA, M, K, N, lddz, ldw, ldda, 0, transB ? 0 : 1, in, out, &e, nullptr, st);
+    if (rc) return rc;
+  }
+  if (dW) {
+    const int rc = transB ? gradient_product(dZ, A, dW, N, K, M, lddz, lda, lddw, in, out, alpha, st)
+                          : gradient_product(A, dZ, dW, K, N, M, lda, lddz, lddw, in, out, alpha, st);
+    if (rc) return rc;
+  }
+  return ALCOP_OK;
+}
+
+static int norm_rows(const void* x, const void* residual, const void* gain, void* total, void* y, void* scale, void* rstd,
+                     int rows, int cols, long ldx, long ldr, long ldt, long ldy, float eps, bool norm, alcop_dtype in,
+                     alcop_dtype out, void* hip_stream)
+{
+  if (!x || !y || (out == ALCOP_E4M3 && !scale)) return ALCOP_ERR_NULL;
+  if (!is_half(in) && in != ALCOP_F32) return ALCOP_ERR_DTYPE;
+  if (!is_half(out) && out != ALCOP_F32 && out != ALCOP_E4M3) return ALCOP_ERR_DTYPE;
+  if (rows <= 0 || cols <= 0) return ALCOP_ERR_SHAPE;
+  if (ldx < cols || ldy < cols || (residual && ldr < cols) || (total && ldt < cols)) return ALCOP_ERR_SHAPE;
+  if (cols > ROWS_MAX_COLS) return ALCOP_ERR_SIZE;
+  const int isz = size_of(in), osz = size_of(out);
+  if (!aligned(x, isz) || !aligned(residual, isz) || !aligned(total, isz) || !aligned(y, osz) || !aligned(gain, 4) ||
+      !aligned(scale, 4) || !aligned(rstd, 4))
+    return ALCOP_ERR_ALIGN;
+  if (out != ALCOP_E4M3) scale = nullptr;
+  // a row is read whole before anything of y is stored, element by element before the sum is
+  const Span sx(x, rows, cols, ldx, isz), sr(residual, rows, cols, ldr, isz), st(total, rows, cols, ldt, isz),
+      sy(y, rows, cols, ldy, osz), sg(gain, 1, cols, cols, 4), ss(scale, 1, rows, rows, 4), sd(rstd, 1, rows, rows, 4);
+  if ((meet(sy, sx) && !(same(sy, sx) && in == out)) || (meet(sy, sr) && !(same(sy, sr) && in == out)) || meet(sy, st))
+    return ALCOP_ERR_UNSUPPORTED;
+  if ((meet(st, sx) && !same(st, sx)) || (meet(st, sr) && !same(st, sr))) return ALCOP_ERR_UNSUPPORTED;
+  for (const Span& o : {sy, st, ss, sd})
+    if (meet(o, sg)) return ALCOP_ERR_UNSUPPORTED;
+  for (const Span& s : {sx, sr, st, sy})
+    if (meet(s, ss) || meet(s, sd)) return ALCOP_ERR_UNSUPPORTED;
+  if (meet(ss, sd)) return ALCOP_ERR_UNSUPPORTED;
+
+  NormArgs a;
+  a.x = x;
+  a.residual = residual;
+  a.gain = (const float*)gain;
+  a.total = total;
+  a.y = y;
+  a.scale = (float*)scale;
+  a.rstd = (float*)rstd;
+  a.ldx = ldx;
+  a.ldr = residual ? ldr : 0;
+  a.ldt = total ? ldt : 0;
+  a.ldy = ldy;
+  a.rows = rows;
+  a.cols = cols;
+  a.eps = eps;
+  a.flags = (int)out | (norm ? 4 : 0);
+  const int ci = 16 / isz, co = out == ALCOP_E4M3 ? 8 : 16 / osz;
+  const bool vec = cols % 8 == 0 && aligned(x, 16) && aligned(residual, 16) && aligned(total, 16) &&
+                   aligned(y, out == ALCOP_E4M3 ? 8 : 16) && aligned(gain, 16) && a.ldx % ci == 0 && a.ldr % ci == 0 &&
+                   a.ldt % ci == 0 && a.ldy % co == 0;
+  return launch_norm_rows(a, (int)in, vec, (hipStream_t)hip_stream) == hipSuccess ? ALCOP_OK : ALCOP_ERR_LAUNCH;
+}
+
+int alcop_rmsnorm(const void* x, const void* residual, const void* gain, void* total, void* y, void* scale, void* rstd,
+                  int rows, int cols, long ldx, long ldr, long ldt, long ldy, float eps, alcop_dtype in, alcop_dtype out,
+                  void* hip_stream)
+{
+  return norm_rows(x, residual, gain, total, y, scale, rstd, rows, cols, ldx, ldr, ldt, ldy, eps, true, in, out, hip_stream);
+}
+
+int alcop_quantize_rows(const void* x, void* y, void* scale, int rows, int cols, long ldx, long ldy, alcop_dtype in,
+                        void* hip_stream)
+{
+  return norm_rows(x, nullptr, nullptr, nullptr, y, scale, nullptr, rows, cols, ldx, 0, 0, ldy, 0.0f, false, in, ALCOP_E4M3,
+                   hip_stream);
+}
+
+size_t alcop_rmsnorm_backward_workspace_bytes(int rows, int cols)
+{
+  if (rows <= 0 || cols <= 0 || cols > ROWS_MAX_COLS) return 0;
+  return r256(4.0 * norm_groups(rows, cols) * cols);
+}
+
+int alcop_rmsnorm_backward(const void* dy, const void* total, const void* gain, const void* rstd, const void* dtotal,
+                           void* dx, void* dgain, int rows, int cols, long lddy, long ldt, long lddt, long lddx,
+                           alcop_dtype in, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+  if (!dy || !total || !rstd || !dx || (dgain && !workspace)) return ALCOP_ERR_NULL;
+  if (!is_half(in) && in != ALCOP_F32) return ALCOP_ERR_DTYPE;
+  if (rows <= 0 || cols <= 0) return ALCOP_ERR_SHAPE;
+  if (lddy < cols || ldt < cols || lddx < cols || (dtotal && lddt < cols)) return ALCOP_ERR_SHAPE;
+  if (cols > ROWS_MAX_COLS) return ALCOP_ERR_SIZE;
+  const int isz = size_of(in);
+  if (!aligned(dy, isz) || !aligned(total, isz) || !aligned(dtotal, isz) || !aligned(dx, isz) || !aligned(gain, 4) ||
+      !aligned(rstd, 4) || !aligned(dgain, 4) || !aligned(workspace, 16))
+    return ALCOP_ERR_ALIGN;
+  const size_t need = alcop_rmsnorm_backward_workspace_bytes(rows, cols);
+  if (dgain && workspace_bytes < need) return ALCOP_ERR_SIZE;
+  // dx may be dy or dtotal, whose elements its own threads have read by then
+  const Span sdy(dy, rows, cols, lddy, isz), sh(total, rows, cols, ldt, isz), sdt(dtotal, rows, cols, lddt, isz),
+      sdx(dx, rows, cols, lddx, isz), sg(gain, 1, cols, cols, 4), sr(rstd, 1, rows, rows, 4), sdg(dgain, 1, cols, cols, 4);
+  if ((meet(sdx, sdy) && !(same(sdx, sdy))) || (meet(sdx, sdt) && !same(sdx, sdt)) || meet(sdx, sh) || meet(sdx, sg) ||
+      meet(sdx, sr) || meet(sdx, sdg))
+    return ALCOP_ERR_UNSUPPORTED;
+  Span sw(dgain ? workspace : nullptr, 1, 1, 1, 1);
+  sw.row = sw.pitch = (double)need;
+  for (const Span& s : {sdy, sh, sdt, sg, sr})
+    if (meet(s, sdg) || meet(s, sw)) return ALCOP_ERR_UNSUPPORTED;
+  if (meet(sw, sdx) || meet(sw, sdg)) return ALCOP_ERR_UNSUPPORTED;
+
+  NormGradArgs a;
+  a.dy = dy;
+  a.total = total;
+  a.dtotal = dtotal;
+  a.gain = (const float*)gain;
+  a.rstd = (const float*)rstd;
+  a.dx = dx;
+  a.partial = dgain ? (float*)workspace : nullptr;
+  a.lddy = lddy;
+  a.ldt = ldt;
+  a.lddt = dtotal ? lddt : 0;
+  a.lddx = lddx;
+  a.rows = rows;
+  a.cols = cols;
+  const int ci = 16 / isz, groups = norm_groups(rows, cols);
+  const bool vec = cols % 8 == 0 && aligned(dy, 16) && aligned(total, 16) && aligned(dtotal, 16) && aligned(dx, 16) &&
+                   aligned(gain, 16) && a.lddy % ci == 0 && a.ldt % ci == 0 && a.lddt % ci == 0 && a.lddx % ci == 0;
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (launch_norm_grad(a, groups, (int)in, vec, st) != hipSuccess) return ALCOP_ERR_LAUNCH;
+  if (dgain) {
+    const ColumnSumArgs s{(const float*)workspace, (float*)dgain, groups, cols};
+    if (launch_column_sums(s, st) != hipSuccess) return ALCOP_ERR_LAUNCH;
+  }
+  return ALCOP_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,74 @@
+// Tables and launchers of the linear layers and the row operators, between their host code (alcop_linear.cpp) and
+// the shards that hold the kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <vector>
+
+#include "../../include/alcop.h"
+#include "alcop_rows.hip.h"
+
+namespace alcop {
+
+struct LinearKernel {
+  int dt, bl;                  // as in LCfg
+  alcop_sched s;               // tile and pipelining, by which alcop_dispatch.h knows the kernel's cost
+  int threads, lds_bytes;
+  hipError_t (*launch)(const LinearArgs&, dim3, hipStream_t);
+  hipError_t (*prepare)();
+};
+void register_linear_f16(std::vector<LinearKernel>&);
+void register_linear_bf16(std::vector<LinearKernel>&);
+void register_linear_e4m3(std::vector<LinearKernel>&);
+
+hipError_t launch_norm_rows(const NormArgs& a, int dt, bool vec, hipStream_t st);
+hipError_t launch_norm_grad(const NormGradArgs& a, int groups, int dt, bool vec, hipStream_t st);
+hipError_t launch_column_sums(const ColumnSumArgs& a, hipStream_t st);
+hipError_t launch_act_grad(const ActGradArgs& a, hipStream_t st);
+hipError_t prepare_rows();
+
+// Threads that share a row, and their chunks of eight elements: a wave while that takes at most four chunks a lane,
+// then a block of 256 or 1024.
+constexpr int ROWS_MAX_COLS = 32768;
+template <int DT, bool VEC, template <class> class LAUNCH, class... A>
+hipError_t dispatch_rows(int cols, const A&... a)
+{
+  if (cols <= 512) return LAUNCH<RowCfg<DT, 64, 1, VEC>>::go(a...);
+  if (cols <= 1024) return LAUNCH<RowCfg<DT, 64, 2, VEC>>::go(a...);
+  if (cols <= 2048) return LAUNCH<RowCfg<DT, 256, 1, VEC>>::go(a...);
+  if (cols <= 4096) return LAUNCH<RowCfg<DT, 256, 2, VEC>>::go(a...);
+  if (cols <= 8192) return LAUNCH<RowCfg<DT, 256, 4, VEC>>::go(a...);
+  if (cols <= 16384) return LAUNCH<RowCfg<DT, 1024, 2, VEC>>::go(a...);
+  return LAUNCH<RowCfg<DT, 1024, 4, VEC>>::go(a...);
+}
+inline int rows_per_block(int cols) { return cols <= 1024 ? 4 : 1; }
+template <template <class> class LAUNCH, class... A>
+hipError_t dispatch_rows_of(int dt, bool vec, int cols, const A&... a)
+{
+  if (dt == 0) return vec ? dispatch_rows<0, true, LAUNCH>(cols, a...) : dispatch_rows<0, false, LAUNCH>(cols, a...);
+  if (dt == 1) return vec ? dispatch_rows<1, true, LAUNCH>(cols, a...) : dispatch_rows<1, false, LAUNCH>(cols, a...);
+  return vec ? dispatch_rows<2, true, LAUNCH>(cols, a...) : dispatch_rows<2, false, LAUNCH>(cols, a...);
+}
+
+// What the first calls of these operators would do besides launching.
+hipError_t prepare_layers();
+
+// dW[M,N] = alpha * A^T . B with A stored K x M and B stored K x N, as alcop_gemm computes it, for any K
+// (alcop_api.cpp): rows past K lie outside both descriptors.
+int gradient_product(const void* A, const void* B, void* C, int M, int N, int K, long lda, long ldb, long ldc,
+                     alcop_dtype in, alcop_dtype out, float alpha, void* stream);
+
+}  // namespace alcop
+
+// The kernels of one operand type and layout.
+#define ALCOP_LINEAR_KERNELS(T, DT, BL)                    \
+  add_linear_ksplit<DT, 16, 16, 8, BL>(T);                 \
+  add_linear_ksplit<DT, 16, 32, 8, BL>(T);                 \
+  add_linear_ksplit<DT, 32, 32, 8, BL>(T);                 \
+  add_linear_ksplit<DT, 32, 64, 4, BL>(T);                 \
+  add_linear<DT, 64, 64, 64, 32, 32, 3, 2, 1, BL>(T);      \
+  add_linear<DT, 128, 128, 64, 64, 64, 2, 1, 0, BL>(T);    \
+  add_linear<DT, 128, 128, 64, 64, 64, 4, 2, 1, BL>(T);    \
+  add_linear<DT, 256, 128, 64, 128, 64, 3, 2, 1, BL>(T);   \
+  add_linear<DT, 256, 192, 32, 128, 96, 3, 2, 1, BL>(T);   \
+  add_linear<DT, 256, 256, 32, 128, 64, 3, 2, 1, BL>(T);

@@ -1,0 +1,426 @@
+// Operators on rows around the products of a transformer block: root-mean-square norm with the residual's addition
+// and its gradients, rows to 8 bits with a scale each, the gradient of an activation with the bias's.
+//
+//   norm      h = x + residual;  rstd = 1 / sqrt(mean(h^2) + eps);  y = h rstd gain
+//   8 bits    scale = max(max |y| / 448, 2^-126);  q = e4m3(y / scale)            (448: the largest e4m3 number)
+//   gradient  with xh = h rstd, t = gain dy:  dx = dtotal + rstd (t - xh mean(t xh)),  dgain = sum over rows of dy xh
+//
+// All of them are bound by memory: a row is loaded once, held in registers in fp32 while its sum and its maximum are
+// found, and stored once.  Sums are fp32 in a fixed order; nothing is atomic, so results do not change between runs.
+//
+// A row belongs to TPR threads (a wave, or a whole block), each holding NV chunks of eight elements.  Rows made of
+// 16-byte chunks (VEC) are moved sixteen bytes a load; others element by element, thread next to thread.
+#pragma once
+#include "alcop_linear.hip.h"
+
+namespace alcop {
+
+constexpr int ROWS_LDS_BYTES = 256;      // a float per wave and reduction, two reductions, twice
+
+struct NormArgs {
+  const void *x, *residual;
+  const float* gain;
+  void *total, *y;
+  float *scale, *rstd;
+  long ldx, ldr, ldt, ldy;
+  int rows, cols;
+  float eps;
+  int flags;                   // type of y (3: e4m3) | the rows are normalised << 2
+};
+
+struct NormGradArgs {
+  const void *dy, *total, *dtotal;
+  const float *gain, *rstd;
+  void* dx;
+  float* partial;              // dgain's sums of the rows of each group of threads, or null
+  long lddy, ldt, lddt, lddx;
+  int rows, cols;
+};
+
+struct ActGradArgs {
+  const void *dc, *pre;
+  void* dz;                    // null: only the sums
+  float* partial;              // dbias's sums of the rows of each block, or null
+  long lddc, ldp, ldz;
+  int M, N, rows_per_block, act, dt;
+};
+
+struct ColumnSumArgs {
+  const float* partial;
+  float* out;
+  int count, cols;
+};
+
+// ---- sums and maxima over the threads of a row -------------------------------------------------------------
+template <class HW>
+__device__ __forceinline__ float wave_sum(float v)
+{
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) v += __builtin_bit_cast(float, HW::xor_lanes(__builtin_bit_cast(uint32_t, v), m));
+  return v;
+}
+// of magnitudes, as bit patterns: those of NaN are above all others, so that one NaN makes the result NaN
+template <class HW>
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
+{
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) {
+    const uint32_t o = HW::xor_lanes(v, m);
+    v = o > v ? o : v;
+  }
+  return v;
+}
+// over a row's TPR threads; `at`: LDS of this reduction, 4 bytes a wave, not used by the one before
+template <int TPR, class HW>
+__device__ __forceinline__ float row_sum(float v, uint32_t at)
+{
+  v = wave_sum<HW>(v);
+  if constexpr (TPR > 64) {
+    HW::lds_write1(at + 4 * HW::wave_id(), __builtin_bit_cast(uint32_t, v));
+    HW::wait_lds();
+    HW::block_barrier();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < TPR / 64; w++) v += __builtin_bit_cast(float, HW::lds_read4(at + 4 * w));
+  }
+  return v;
+}
+template <int TPR, class HW>
+__device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t at)
+{
+  v = wave_max<HW>(v);
+  if constexpr (TPR > 64) {
+    HW::lds_write1(at + 4 * HW::wave_id(), v);
+    HW::wait_lds();
+    HW::block_barrier();
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < TPR / 64; w++) {
+      const uint32_t o = HW::lds_read4(at + 4 * w);
+      v = o > v ? o : v;
+    }
+  }
+  return v;
+}
+
+// ---- a thread's part of a row ----------------------------------------------------------------------------------
+// VEC: chunk i is columns (i TPR + me) 8 ..+7; else its element e is column (8 i + e) TPR + me.
+template <int DT_, int TPR_, int NV_, bool VEC_>
+struct RowCfg {
+  static constexpr int DT = DT_, TPR = TPR_, NV = NV_, NT = TPR_ < 256 ? 256 : TPR_;
+  static constexpr bool VEC = VEC_;
+  static constexpr int ROWS = NT / TPR;            // rows of a block
+};
+
+template <class C, class HW>
+__device__ __forceinline__ int column(int me, int i, int e)
+{
+  return C::VEC ? (i * C::TPR + me) * 8 + e : (8 * i + e) * C::TPR + me;
+}
+
+// The chunks of a row as they lie in memory; columns past the end are 0.
+template <class C>
+struct Raw {
+  RawRow<8> c[C::NV];
+};
+template <class C, class HW, int DT = C::DT>
+__device__ __forceinline__ Raw<C> load_raw(const void* row, int me, int cols)
+{
+  Raw<C> r;
+#pragma unroll
+  for (int i = 0; i < C::NV; i++) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) r.c[i].w[e] = 0;
+    if constexpr (C::VEC) {
+      const int n = column<C, HW>(me, i, 0);
+      if (n < cols) r.c[i] = load_chunk<8, HW>(row, n, DT);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const int n = column<C, HW>(me, i, e);
+        if (n < cols) {
+          if constexpr (DT == 2)
+            r.c[i].w[e] = HW::global_load_u32((const char*)row + (long)n * 4);
+          else
+            r.c[i].w[e / 2] |= (uint32_t)HW::global_load_u16((const char*)row + (long)n * 2) << (e & 1 ? 16 : 0);
+        }
+      }
+    }
+  }
+  return r;
+}
+template <class C, class HW, int DT = C::DT>
+__device__ __forceinline__ float value(const Raw<C>& r, int i, int e)
+{
+  return element<8, HW>(r.c[i], e, DT);
+}
+
+// v[NV][8] to a row of type dt (0, 1, 2; 3: e4m3)
+template <class C, class HW>
+__device__ __forceinline__ void store_values(void* row, int me, int cols, int dt, const float (&v)[C::NV][8])
+{
+#pragma unroll
+  for (int i = 0; i < C::NV; i++) {
+    if constexpr (C::VEC) {
+      const int n = column<C, HW>(me, i, 0);
+      if (n >= cols) continue;
+      if (dt == 3) {
+        const uint32_t lo = HW::cvt_e4m3(v[i][0], v[i][1]) | HW::cvt_e4m3(v[i][2], v[i][3]) << 16;
+        const uint32_t hi = HW::cvt_e4m3(v[i][4], v[i][5]) | HW::cvt_e4m3(v[i][6], v[i][7]) << 16;
+        HW::template global_store<u32x2>((char*)row + n, u32x2{lo, hi});
+      } else {
+        store_row<8, HW, false>(row, n, dt, v[i]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const int n = column<C, HW>(me, i, e);
+        if (n >= cols) continue;
+        if (dt == 3)
+          HW::global_store_u8((char*)row + n, (uint8_t)HW::cvt_e4m3(v[i][e], v[i][e]));
+        else
+          store_element<HW>(row, n, dt, v[i][e]);
+      }
+    }
+  }
+}
+
+template <class C, class HW>
+__device__ __forceinline__ void load_gain(const float* gain, int me, int cols, float (&g)[C::NV][8])
+{
+#pragma unroll
+  for (int i = 0; i < C::NV; i++) {
+    const int n = column<C, HW>(me, i, 0);
+#pragma unroll
+    for (int e = 0; e < 8; e++) g[i][e] = 1.0f;
+    if (gain == nullptr) continue;
+    if constexpr (C::VEC) {
+      if (n >= cols) continue;
+#pragma unroll
+      for (int q = 0; q < 2; q++) {
+        const f32x4 t = HW::global_load_f32x4(gain + n + 4 * q);
+#pragma unroll
+        for (int e = 0; e < 4; e++) g[i][4 * q + e] = t[e];
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const int m = column<C, HW>(me, i, e);
+        if (m < cols) g[i][e] = __builtin_bit_cast(float, HW::global_load_u32(gain + m));
+      }
+    }
+  }
+}
+
+template <int DT>
+__device__ __forceinline__ const char* row_at(const void* base, long row, long ld)
+{
+  return (const char*)base + row * ld * (DT == 2 ? 4 : 2);
+}
+
+// ---- norm, 8 bits ------------------------------------------------------------------------------------------------
+template <class C, class HW>
+__global__ void __launch_bounds__(C::NT) alcop_norm_rows(const NormArgs p)
+{
+  constexpr int NV = C::NV, DT = C::DT;
+  const uint32_t lds = HW::lds_base();
+  const int tid = HW::wave_id() * 64 + HW::lane_id();
+  const int me = tid % C::TPR;
+  const long row = (long)HW::block_x() * C::ROWS + tid / C::TPR;
+  if (row >= p.rows) return;                       // a whole wave, where a wave has a row; else never
+  const bool norm = (p.flags & 4) != 0;
+  const int out = p.flags & 3;
+
+  const Raw<C> x = load_raw<C, HW>(row_at<DT>(p.x, row, p.ldx), me, p.cols);
+  float h[NV][8];
+  if (p.residual != nullptr) {
+    const Raw<C> r = load_raw<C, HW>(row_at<DT>(p.residual, row, p.ldr), me, p.cols);
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) h[i][e] = value<C, HW>(x, i, e) + value<C, HW>(r, i, e);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) h[i][e] = value<C, HW>(x, i, e);
+  }
+  if (p.total != nullptr)
+    store_values<C, HW>((void*)row_at<DT>(p.total, row, p.ldt), me, p.cols, DT, h);
+  if (norm) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) s += h[i][e] * h[i][e];
+    s = row_sum<C::TPR, HW>(s, lds);
+    const float rstd = 1.0f / HW::sqrt(s / (float)p.cols + p.eps);
+    if (p.rstd != nullptr && me == 0) HW::global_store_u32(p.rstd + row, __builtin_bit_cast(uint32_t, rstd));
+    float g[NV][8];
+    load_gain<C, HW>(p.gain, me, p.cols, g);
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) h[i][e] = h[i][e] * rstd * g[i][e];
+  }
+  if (out == 3) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const uint32_t b = __builtin_bit_cast(uint32_t, h[i][e]) & 0x7fffffffu;
+        // a thread past the row's end holds zeros, which a gain of its own must not turn into NaN
+        if (column<C, HW>(me, i, e) < p.cols) top = b > top ? b : top;
+      }
+    top = row_max<C::TPR, HW>(top, lds + 64);
+    const float peak = __builtin_bit_cast(float, top) / 448.0f;
+    const float scale = peak < 1.17549435e-38f ? 1.17549435e-38f : peak;     // NaN stays
+    if (me == 0) HW::global_store_u32(p.scale + row, __builtin_bit_cast(uint32_t, scale));
+    const float inv = 1.0f / scale;
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) h[i][e] *= inv;
+  }
+  store_values<C, HW>((char*)p.y + row * p.ldy * (out == 3 ? 1 : out == 2 ? 4 : 2), me, p.cols, out, h);
+}
+
+// ---- gradients of the norm ------------------------------------------------------------------------------------------
+// A group of TPR threads takes rows g, g + groups, ... and keeps the sums of dgain for its columns in registers;
+// alcop_column_sums adds the groups'.
+template <class C, class HW>
+__global__ void __launch_bounds__(C::NT) alcop_norm_grad(const NormGradArgs p, int groups)
+{
+  constexpr int NV = C::NV, DT = C::DT;
+  // rows of more elements than the registers have room for are read again behind the sum
+  constexpr bool HOLD = NV * C::TPR <= 2048;
+  const uint32_t lds = HW::lds_base();
+  const int tid = HW::wave_id() * 64 + HW::lane_id();
+  const int me = tid % C::TPR;
+  const int group = (int)HW::block_x() * C::ROWS + tid / C::TPR;
+  float dg[NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; i++)
+#pragma unroll
+    for (int e = 0; e < 8; e++) dg[i][e] = 0.f;
+  int turn = 0;
+  for (long row = group; row < p.rows; row += groups, turn ^= 1) {
+    const char *dy_row = row_at<DT>(p.dy, row, p.lddy), *h_row = row_at<DT>(p.total, row, p.ldt);
+    Raw<C> dy = load_raw<C, HW>(dy_row, me, p.cols);
+    Raw<C> h = load_raw<C, HW>(h_row, me, p.cols);
+    const float rstd = __builtin_bit_cast(float, HW::global_load_u32(p.rstd + row));
+    float g[NV][8];
+    load_gain<C, HW>(p.gain, me, p.cols, g);
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const float d = value<C, HW>(dy, i, e), xh = value<C, HW>(h, i, e) * rstd;
+        s += d * g[i][e] * xh;
+        dg[i][e] += d * xh;
+      }
+    const float mean = row_sum<C::TPR, HW>(s, lds + 64 * turn) / (float)p.cols;
+    if constexpr (!HOLD) {
+      dy = load_raw<C, HW>(dy_row, me, p.cols);
+      h = load_raw<C, HW>(h_row, me, p.cols);
+      load_gain<C, HW>(p.gain, me, p.cols, g);
+    }
+    float dx[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++)
+        dx[i][e] = rstd * (value<C, HW>(dy, i, e) * g[i][e] - value<C, HW>(h, i, e) * rstd * mean);
+    if (p.dtotal != nullptr) {
+      const Raw<C> dt = load_raw<C, HW>(row_at<DT>(p.dtotal, row, p.lddt), me, p.cols);
+#pragma unroll
+      for (int i = 0; i < NV; i++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) dx[i][e] += value<C, HW>(dt, i, e);
+    }
+    store_values<C, HW>((void*)row_at<DT>(p.dx, row, p.lddx), me, p.cols, DT, dx);
+  }
+  if (p.partial != nullptr && group < groups)
+    store_values<C, HW>(p.partial + (long)group * p.cols, me, p.cols, 2, dg);
+}
+
+// ---- column sums ------------------------------------------------------------------------------------------------------
+// out[j] = sum over i of partial[i][j], in a fixed order: 32 columns a block, 32 runs of rows, then the runs.
+constexpr int SUM_THREADS = 1024, SUM_COLS = 32;
+template <class HW>
+__global__ void __launch_bounds__(SUM_THREADS) alcop_column_sums(const ColumnSumArgs p)
+{
+  const uint32_t lds = HW::lds_base();
+  const int tid = HW::wave_id() * 64 + HW::lane_id();
+  const int c = tid % SUM_COLS, run = tid / SUM_COLS;
+  const int j = (int)HW::block_x() * SUM_COLS + c;
+  float s = 0.f;
+  if (j < p.cols) {
+#pragma unroll 4
+    for (int i = run; i < p.count; i += SUM_THREADS / SUM_COLS)
+      s += __builtin_bit_cast(float, HW::global_load_u32(p.partial + (long)i * p.cols + j));
+  }
+  HW::lds_write1(lds + 4 * (run * SUM_COLS + c), __builtin_bit_cast(uint32_t, s));
+  HW::wait_lds();
+  HW::block_barrier();
+  if (tid >= 64) return;
+  float t = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < SUM_THREADS / SUM_COLS; i++) t += __builtin_bit_cast(float, HW::lds_read4(lds + 4 * (i * SUM_COLS + c)));
+  if (tid < SUM_COLS && j < p.cols) HW::global_store_u32(p.out + j, __builtin_bit_cast(uint32_t, t));
+}
+
+// ---- gradient of an activation, sums for the bias ----------------------------------------------------------------------
+// dZ = dC act'(Z), rounded to the operands' type: it is an operand of the two products that follow, which take
+// 16 bits.  A block has 512 columns and a run of rows, its four waves every fourth row of it; 16-byte chunks.
+constexpr int ACT_COLS = 512;
+template <class HW>
+__global__ void __launch_bounds__(256) alcop_act_grad(const ActGradArgs p)
+{
+  const uint32_t lds = HW::lds_base();
+  const int lane = HW::lane_id(), wave = HW::wave_id();
+  const int n = (int)HW::block_x() * ACT_COLS + lane * 8;
+  const long r0 = (long)HW::block_y() * p.rows_per_block;
+  const long r1 = r0 + p.rows_per_block < p.M ? r0 + p.rows_per_block : p.M;
+  float sum[8];
+#pragma unroll
+  for (int e = 0; e < 8; e++) sum[e] = 0.f;
+  if (n < p.N) {
+    for (long m = r0 + wave; m < r1; m += 4) {
+      const RawRow<8> dc = load_chunk<8, HW>(p.dc, m * p.lddc + n, p.dt);
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[e] = element<8, HW>(dc, e, p.dt);
+      if (p.act != ACT_NONE) {
+        const RawRow<8> z = load_chunk<8, HW>(p.pre, m * p.ldp + n, p.dt);
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] *= slope<HW>(element<8, HW>(z, e, p.dt), p.act);
+      }
+      if (p.dz != nullptr) store_row<8, HW, true>(p.dz, m * p.ldz + n, p.dt, v);
+#pragma unroll
+      for (int e = 0; e < 8; e++) sum[e] += v[e];
+    }
+  }
+  if (p.partial == nullptr) return;
+  const uint32_t mine = lds + (uint32_t)(wave * ACT_COLS + lane * 8) * 4;
+  HW::lds_write(mine, f32x4{sum[0], sum[1], sum[2], sum[3]});
+  HW::lds_write(mine + 16, f32x4{sum[4], sum[5], sum[6], sum[7]});
+  HW::wait_lds();
+  HW::block_barrier();
+  const int at = (wave * 64 + lane) * 2, j = (int)HW::block_x() * ACT_COLS + at;
+  float t[2] = {0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < 4; w++) {
+    const u32x2 s = HW::lds_read8(lds + (uint32_t)(w * ACT_COLS + at) * 4);
+    const uint32_t a = s[0], b = s[1];
+    t[0] += __builtin_bit_cast(float, a);
+    t[1] += __builtin_bit_cast(float, b);
+  }
+  if (j < p.N)                                    // N is a multiple of 8
+    HW::template global_store<u32x2>(p.partial + (long)HW::block_y() * p.N + j,
+                                     u32x2{__builtin_bit_cast(uint32_t, t[0]), __builtin_bit_cast(uint32_t, t[1])});
+}
+
+}  // namespace alcop

@@ -25,6 +25,11 @@ struct Api {
   decltype(&alcop_bmm_unaligned) bmm_any = nullptr;
   decltype(&alcop_conv2d_igemm_dilated) conv = nullptr;
   decltype(&alcop_conv2d_igemm_unaligned) conv_any = nullptr;
+  decltype(&alcop_linear) linear = nullptr;
+  decltype(&alcop_linear_backward) linear_backward = nullptr;
+  decltype(&alcop_rmsnorm) rmsnorm = nullptr;
+  decltype(&alcop_rmsnorm_backward) rmsnorm_backward = nullptr;
+  decltype(&alcop_quantize_rows) quantize_rows = nullptr;
 } api;
 
 PyObject* sched_type = nullptr;   // the binding's ctypes mirror of alcop_sched
@@ -305,6 +310,187 @@ PyObject* conv_any(PyObject*, PyObject* const* a, Py_ssize_t n)
   });
 }
 
+// ---- linear layers, norms, 8-bit rows ----
+// A matrix of rows on the device of the call, or (None) none.
+struct Rows {
+  const at::Tensor* t = nullptr;
+  int rows = 0, cols = 0;
+  long ld = 0;
+  alcop_dtype type = ALCOP_F32;
+  Rows() = default;
+  explicit Rows(PyObject* o) : Rows(tensor(o)) {}
+  explicit Rows(const at::Tensor& m) : t(&m)
+  {
+    need(m.dim() == 2 && m.is_cuda());
+    const int64_t r = m.size(0), c = m.size(1);
+    need(r >= 1 && c >= 1 && r <= INT32_MAX && c <= INT32_MAX && (c == 1 || m.stride(1) == 1));
+    rows = (int)r;
+    cols = (int)c;
+    ld = r == 1 ? (long)c : (long)m.stride(0);     // a single row has no pitch of its own
+    type = m.scalar_type() == at::kFloat8_e4m3fn ? ALCOP_E4M3 : dtype(m);
+  }
+  // of this shape (and type), beside `like`
+  Rows(PyObject* o, int r, int c, const Rows& like, bool same_type)
+  {
+    if (o == Py_None) return;
+    *this = Rows(o);
+    need(rows == r && cols == c && t->device() == like.t->device() && (!same_type || type == like.type));
+  }
+  const void* in() const { return t ? t->const_data_ptr() : nullptr; }
+  void* out() const { return t ? t->data_ptr() : nullptr; }
+};
+const at::Tensor* floats(PyObject* o, int n, const Rows& like)
+{
+  if (o == Py_None) return nullptr;
+  const at::Tensor& v = tensor(o);
+  need(v.dim() == 1 && v.size(0) == n && v.is_contiguous() && v.scalar_type() == at::kFloat && v.device() == like.t->device());
+  return &v;
+}
+const void* in(const at::Tensor* t) { return t ? t->const_data_ptr() : nullptr; }
+void* out(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+float number(PyObject* o)
+{
+  const double a = PyFloat_AsDouble(o);
+  need(!(a == -1.0 && PyErr_Occurred()));
+  return (float)a;
+}
+struct Scratch {
+  void* p = nullptr;
+  size_t bytes = 0;
+  Scratch(PyObject* o, const Rows& like)
+  {
+    if (o == Py_None) return;
+    const at::Tensor& w = tensor(o);
+    need(w.is_contiguous() && w.device() == like.t->device());
+    p = w.data_ptr();
+    bytes = w.nbytes();
+  }
+};
+// The stream of a call on m's device, which has to be the current one.
+void* stream_on(const Rows& m, PyObject* o)
+{
+  need(m.t->device().index() == c10::hip::current_device());
+  return stream_of(o);
+}
+
+// linear(A, W, C, transB, alpha, bias, act, residual, pre, scale_a, scale_w, stream)
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+  return guarded([&] {
+    need(api.linear && n == 12);
+    const Rows A(a[0]), W(a[1]);
+    const int tb = truth(a[3]), N = tb ? W.rows : W.cols;
+    need((tb ? W.cols : W.rows) == A.cols && W.type == A.type && W.t->device() == A.t->device());
+    need(a[2] != Py_None);
+    const Rows C(a[2], A.rows, N, A, false), res(a[7], A.rows, N, C, true), pre(a[8], A.rows, N, C, true);
+    const at::Tensor *bias = floats(a[5], N, A), *sa = floats(a[9], A.rows, A), *sw = floats(a[10], N, A);
+    const alcop_linear_tail t{number(a[4]), in(bias), integer(a[6]), res.in(), res.ld, pre.out(), pre.ld, in(sa), in(sw)};
+    void* st = stream_on(A, a[11]);
+    const void *pa = A.in(), *pw = W.in();
+    void* pc = C.out();
+    return unlocked([&] {
+      return api.linear(pa, pw, pc, A.rows, N, A.cols, A.ld, W.ld, C.ld, tb, A.type, C.type, &t, st);
+    });
+  });
+}
+
+// linear_backward(dC, A, W, dA, dW, dbias, pre, act, alpha, transB, workspace, stream)
+PyObject* linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+  return guarded([&] {
+    need(api.linear_backward && n == 12);
+    const Rows dC(a[0]), A(a[1]);
+    const int tb = truth(a[9]), M = dC.rows, N = dC.cols, K = A.cols;
+    need(a[2] != Py_None && A.rows == M && A.type == dC.type && A.t->device() == dC.t->device());
+    const Rows W(a[2], tb ? N : K, tb ? K : N, dC, true), dA(a[3], M, K, dC, false), dW(a[4], W.rows, W.cols, dC, false);
+    const Rows pre(a[6], M, N, dC, true);
+    need(!dA.t || !dW.t || dA.type == dW.type);
+    const at::Tensor* db = floats(a[5], N, dC);
+    const int act = integer(a[7]);
+    const float alpha = number(a[8]);
+    const Scratch ws(a[10], dC);
+    void* st = stream_on(dC, a[11]);
+    const void *pc = dC.in(), *pa = A.in(), *pw = W.in(), *pp = pre.in();
+    void *oa = dA.out(), *ow = dW.out(), *ob = out(db);
+    const alcop_dtype type = dA.t ? dA.type : dW.t ? dW.type : dC.type;
+    return unlocked([&] {
+      return api.linear_backward(pc, pa, pw, pp, oa, ow, ob, M, N, K, dC.ld, A.ld, W.ld, pre.ld, dA.ld, dW.ld, tb, dC.type,
+                                 type, alpha, act, ws.p, ws.bytes, st);
+    });
+  });
+}
+
+// rmsnorm(x, gain, y, residual, total, scale, rstd, eps, stream)
+PyObject* rmsnorm(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+  return guarded([&] {
+    need(api.rmsnorm && n == 9 && a[2] != Py_None);
+    const Rows x(a[0]), y(a[2], x.rows, x.cols, x, false), r(a[3], x.rows, x.cols, x, true), h(a[4], x.rows, x.cols, x, true);
+    const at::Tensor *g = floats(a[1], x.cols, x), *s = floats(a[5], x.rows, x), *d = floats(a[6], x.rows, x);
+    const float eps = number(a[7]);
+    void* st = stream_on(x, a[8]);
+    const void *px = x.in(), *pr = r.in(), *pg = in(g);
+    void *ph = h.out(), *py = y.out(), *ps = out(s), *pd = out(d);
+    return unlocked([&] {
+      return api.rmsnorm(px, pr, pg, ph, py, ps, pd, x.rows, x.cols, x.ld, r.ld, h.ld, y.ld, eps, x.type, y.type, st);
+    });
+  });
+}
+
+// rmsnorm_backward(dy, total, gain, rstd, dx, dgain, dtotal, workspace, stream)
+PyObject* rmsnorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+  return guarded([&] {
+    need(api.rmsnorm_backward && n == 9 && a[1] != Py_None && a[4] != Py_None);
+    const Rows dy(a[0]);
+    const int R = dy.rows, N = dy.cols;
+    const Rows h(a[1], R, N, dy, true), dx(a[4], R, N, dy, true), dt(a[6], R, N, dy, true);
+    const at::Tensor *g = floats(a[2], N, dy), *d = floats(a[3], R, dy), *dg = floats(a[5], N, dy);
+    const Scratch ws(a[7], dy);
+    void* st = stream_on(dy, a[8]);
+    const void *py = dy.in(), *ph = h.in(), *pg = in(g), *pd = in(d), *pt = dt.in();
+    void *ox = dx.out(), *og = out(dg);
+    return unlocked([&] {
+      return api.rmsnorm_backward(py, ph, pg, pd, pt, ox, og, R, N, dy.ld, h.ld, dt.ld, dx.ld, dy.type, ws.p, ws.bytes, st);
+    });
+  });
+}
+
+// quantize_rows(x, y, scale, stream)
+PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+  return guarded([&] {
+    need(api.quantize_rows && n == 4 && a[1] != Py_None);
+    const Rows x(a[0]), y(a[1], x.rows, x.cols, x, false);
+    need(y.type == ALCOP_E4M3);
+    const at::Tensor* s = floats(a[2], x.rows, x);
+    void* st = stream_on(x, a[3]);
+    const void* px = x.in();
+    void *py = y.out(), *ps = out(s);
+    return unlocked([&] { return api.quantize_rows(px, py, ps, x.rows, x.cols, x.ld, y.ld, x.type, st); });
+  });
+}
+
+// init_layers(linear, linear_backward, rmsnorm, rmsnorm_backward, quantize_rows): addresses in the library
+PyObject* init_layers(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+  if (n != 5) {
+    PyErr_SetString(PyExc_TypeError, "init_layers takes five addresses");
+    return nullptr;
+  }
+  void* f[5];
+  for (int i = 0; i < 5; i++) {
+    f[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+  }
+  api.linear = (decltype(api.linear))f[0];
+  api.linear_backward = (decltype(api.linear_backward))f[1];
+  api.rmsnorm = (decltype(api.rmsnorm))f[2];
+  api.rmsnorm_backward = (decltype(api.rmsnorm_backward))f[3];
+  api.quantize_rows = (decltype(api.quantize_rows))f[4];
+  Py_RETURN_NONE;
+}
+
 // init(Sched, gemm_fused, bmm_fused, bmm_unaligned, conv_dilated, conv_unaligned): the class of schedules
 // and addresses in the library
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n)
@@ -334,6 +520,12 @@ PyMethodDef methods[] = {
     {"mm", (PyCFunction)(void*)mm, METH_FASTCALL, "matrix product, plain or batched"},
     {"mm_any", (PyCFunction)(void*)mm_any, METH_FASTCALL, "matrix product of unaligned operands"},
     {"conv", (PyCFunction)(void*)conv, METH_FASTCALL, "convolution"},
+    {"init_layers", (PyCFunction)(void*)init_layers, METH_FASTCALL, "set the entry points of layers and norms"},
+    {"linear", (PyCFunction)(void*)linear, METH_FASTCALL, "linear layer"},
+    {"linear_backward", (PyCFunction)(void*)linear_backward, METH_FASTCALL, "gradients of a linear layer"},
+    {"rmsnorm", (PyCFunction)(void*)rmsnorm, METH_FASTCALL, "root-mean-square norm of rows"},
+    {"rmsnorm_backward", (PyCFunction)(void*)rmsnorm_backward, METH_FASTCALL, "gradients of the norm"},
+    {"quantize_rows", (PyCFunction)(void*)quantize_rows, METH_FASTCALL, "rows to 8 bits"},
     {"conv_any", (PyCFunction)(void*)conv_any, METH_FASTCALL, "convolution of unaligned operands"},
     {nullptr, nullptr, 0, nullptr}};
 

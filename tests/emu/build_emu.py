@@ -20,7 +20,7 @@ FLAGS = [os.environ.get("EMU_OPT", "-O1"), "-std=c++17", "-fPIC", "-D__HIP_PLATF
 
 def _newest_dep() -> float:
     deps = glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(HERE, "*.h")) + \
-        glob.glob(os.path.join(ROOT, "include", "*.h")) + [os.path.join(HERE, "emu_lib.cpp")]
+        glob.glob(os.path.join(ROOT, "include", "*.h")) + [os.path.join(HERE, "emu_lib.cpp"), os.path.join(HERE, "emu_linear.cpp")]
     return max(os.path.getmtime(d) for d in deps)
 
 
@@ -36,8 +36,10 @@ def build() -> str:
     emu = os.path.join(HERE, "emu_lib.cpp")
     jobs = [(emu, os.path.join(OUT, "emu_part%d.o" % p), ["-DEMU_PART=%d" % p]) for p in range(8)]
     jobs.append((emu, os.path.join(OUT, "emu_main.o"), ["-DEMU_PART=-1"]))
-    for name in ("alcop_api.cpp", "alcop_model.cpp"):
+    for name in ("alcop_api.cpp", "alcop_model.cpp", "alcop_linear.cpp"):
         jobs.append((os.path.join(CSRC, name), os.path.join(OUT, name + ".o"), []))
+    lin = os.path.join(HERE, "emu_linear.cpp")
+    jobs += [(lin, os.path.join(OUT, "emu_linear%d.o" % p), ["-DEMU_PART=%d" % p]) for p in range(4)]
     with cf.ThreadPoolExecutor(max_workers=8) as ex:
         objs = list(ex.map(_compile, jobs))
     if not os.path.exists(LIB) or any(os.path.getmtime(o) > os.path.getmtime(LIB) for o in objs):

@@ -52,6 +52,7 @@
 #include "alcop_stream.hip.h"
 #include "alcop_ksplit.hip.h"
 #include "alcop_convres.hip.h"
+#include "alcop_rows.hip.h"
 
 namespace emu {
 
@@ -276,6 +277,31 @@ inline uint16_t float_to_bf16(float f)
   return (uint16_t)(u >> 16);
 }
 
+// e4m3: sign, 4 bits of exponent (bias 7), 3 of mantissa; no infinities, all ones is NaN
+inline float e4m3_to_float(uint8_t b)
+{
+  const int e = (b >> 3) & 15, m = b & 7;
+  if ((b & 0x7f) == 0x7f) return __builtin_nanf("");
+  const float v = e ? (float)(8 + m) * __builtin_exp2f((float)(e - 10)) : (float)m * __builtin_exp2f(-9.0f);
+  return (b & 0x80) ? -v : v;
+}
+// round to nearest even; magnitudes that round beyond 448 give NaN
+inline uint8_t float_to_e4m3(float f)
+{
+  uint32_t u;
+  memcpy(&u, &f, 4);
+  const uint8_t s = (uint8_t)(u >> 24 & 0x80);
+  const float a = f < 0 ? -f : f;
+  if (!(a <= 464.0f)) return s | 0x7f;
+  // the distance of neighbours at a: 2^(e - 3), 2^-9 below the normal numbers
+  int e = a > 0 ? (int)(u >> 23 & 255) - 127 : -6;
+  if (e < -6) e = -6;
+  const float q = __builtin_rintf(a * __builtin_exp2f((float)(3 - e)));      // 0 .. 16
+  const int n = (int)q;
+  const int bits = e == -6 ? n : ((e + 6) << 3) + n;                         // a carry moves into the exponent
+  return s | (uint8_t)(bits > 0x7e ? 0x7e : bits);
+}
+
 // ---- the policy class -------------------------------------------------------------------------
 struct Rsrc {
   const char* base;
@@ -406,6 +432,17 @@ struct Emu {
   static void wait_matrix(A&) {}
   static void sched_fence() {}
 
+  // sixteen products of e4m3
+  static float e4m3_dot(u32x4 x, u32x4 y)
+  {
+    uint8_t a[16], b[16];
+    memcpy(a, &x, 16);
+    memcpy(b, &y, 16);
+    float s = 0;
+    for (int k = 0; k < 16; k++) s += e4m3_to_float(a[k]) * e4m3_to_float(b[k]);
+    return s;
+  }
+
   template <int DT>
   static f32x16 mma(u32x4 x, u32x4 y, f32x16 acc)
   {
@@ -419,6 +456,15 @@ struct Emu {
     W.Y[par][l] = y;
     wave_sync();
     const int j = l & 31;
+    if constexpr (DT == 2) {
+      for (int v = 0; v < 16; v++) {
+        const int i = 8 * (v / 4) + 4 * (l >> 5) + (v & 3);
+        float t = acc[v];
+        for (int h = 0; h < 2; h++) t += e4m3_dot(W.X[par][i + 32 * h], W.Y[par][j + 32 * h]);
+        acc[v] = t;
+      }
+      return acc;
+    }
     for (int v = 0; v < 16; v++) {
       const int i = 8 * (v / 4) + 4 * (l >> 5) + (v & 3);
       float s = acc[v];
@@ -449,6 +495,15 @@ struct Emu {
     W.Y[par][l] = y;
     wave_sync();
     const int j = l & 15;
+    if constexpr (DT == 2) {
+      for (int v = 0; v < 4; v++) {
+        const int i = 4 * (l >> 4) + v;
+        float t = acc[v];
+        for (int h = 0; h < 4; h++) t += e4m3_dot(W.X[par][i + 16 * h], W.Y[par][j + 16 * h]);
+        acc[v] = t;
+      }
+      return acc;
+    }
     for (int v = 0; v < 4; v++) {
       const int i = 4 * (l >> 4) + v;
       float s = acc[v];
@@ -599,6 +654,37 @@ struct Emu {
     else
       fail("element store outside the output: block %u,%u thread %d", blk()->bx, blk()->by, blk()->cur);
   }
+  static u32x2 global_load8(const void* ptr)
+  {
+    u32x2 v = {0, 0};
+    if ((uintptr_t)ptr % 8) fail("8-byte global load from an unaligned address (thread %d)", blk()->cur);
+    if (in_buffer(ptr, 8, false))
+      memcpy(&v, ptr, 8);
+    else
+      fail("global load outside every operand (thread %d)", blk()->cur);
+    return v;
+  }
+  static void global_store_u8(void* ptr, uint8_t v) { global_store_elem<uint8_t>(ptr, v); }
+  static float f16_bits(uint16_t b) { return f16_to_float(b); }
+  static uint32_t cvt_e4m3(float a, float b) { return (uint32_t)float_to_e4m3(a) | (uint32_t)float_to_e4m3(b) << 8; }
+  // the exchange takes two slots in turn, as a lane may be one exchange ahead of another
+  static uint32_t xor_lanes(uint32_t v, int mask)
+  {
+    Block& b = *blk();
+    const int l = b.cur & 63;
+    Lane& L = b.lanes[b.cur];
+    Wave& W = b.waves[b.cur >> 6];
+    const int par = L.tr_par;
+    L.tr_par ^= 1;
+    W.T[par][l] = v;
+    wave_sync();
+    return W.T[par][l ^ mask];
+  }
+  static void lds_write1(uint32_t addr, uint32_t v) { lds_write(addr, v); }
+  static float sqrt(float v) { return __builtin_sqrtf(v); }
+  static float exp2(float v) { return __builtin_exp2f(v); }
+  static float rcp(float v) { return 1.0f / v; }
+  static float erf(float v) { return __builtin_erff(v); }
   static uint16_t global_load_u16(const void* ptr) { return global_load_elem<uint16_t>(ptr); }
   static uint32_t global_load_u32(const void* ptr) { return global_load_elem<uint32_t>(ptr); }
   static void global_store_u16(void* ptr, uint16_t v) { global_store_elem<uint16_t>(ptr, v); }

@@ -1,0 +1,114 @@
+// The linear layers and the row operators on the functional model: their host code (alcop_linear.cpp) linked with
+// tables whose launchers run the kernel templates on emu_hw.h.
+#include <hip/hip_runtime.h>
+
+#include "emu_hw.h"
+#include "alcop_linear.h"
+
+namespace alcop {
+
+template <class C>
+static void tile_entry(const void* p)
+{
+  alcop_linear_tile<C, emu::Emu>(*(const LinearArgs*)p);
+}
+template <class C>
+static void ksplit_entry(const void* p)
+{
+  alcop_linear_ksplit<C, emu::Emu>(*(const LinearArgs*)p);
+}
+template <class C, void (*ENTRY)(const void*)>
+static hipError_t launch_linear(const LinearArgs& a, dim3 grid, hipStream_t)
+{
+  emu::run_grid(ENTRY, &a, C::NT, C::LDS_BYTES, grid.x, 1, 1);
+  return hipSuccess;
+}
+static hipError_t prepare_none() { return hipSuccess; }
+
+template <int DT, int BM, int BN, int BK, int WM, int WN, int S, int R, int F, int BL>
+void add_linear(std::vector<LinearKernel>& t)
+{
+  using C = LCfg<DT, BM, BN, BK, WM, WN, S, R, F, BL>;
+  t.push_back(LinearKernel{DT, BL, alcop_sched{BM, BN, BK, WM, WN, S, R, F, 1, 0, 0}, C::NT, C::LDS_BYTES,
+                           &launch_linear<C, &tile_entry<C>>, &prepare_none});
+}
+template <int DT, int BM, int BN, int NW, int BL>
+void add_linear_ksplit(std::vector<LinearKernel>& t)
+{
+  using C = LWCfg<DT, BM, BN, NW, 2, BL>;
+  t.push_back(LinearKernel{DT, BL, alcop_sched{BM, BN, 64, BM, BN, 2, 1, 0, 1, 0, 3}, C::NT, C::LDS_BYTES,
+                           &launch_linear<C, &ksplit_entry<C>>, &prepare_none});
+}
+
+#if EMU_PART == 0
+void register_linear_f16(std::vector<LinearKernel>& t)
+{
+  ALCOP_LINEAR_KERNELS(t, 0, 0)
+  ALCOP_LINEAR_KERNELS(t, 0, 1)
+}
+#elif EMU_PART == 1
+void register_linear_bf16(std::vector<LinearKernel>& t)
+{
+  ALCOP_LINEAR_KERNELS(t, 1, 0)
+  ALCOP_LINEAR_KERNELS(t, 1, 1)
+}
+#elif EMU_PART == 2
+void register_linear_e4m3(std::vector<LinearKernel>& t)
+{
+  ALCOP_LINEAR_KERNELS(t, 2, 1)
+}
+#elif EMU_PART == 3
+template <class C>
+struct Norm {
+  static void entry(const void* p) { alcop_norm_rows<C, emu::Emu>(*(const NormArgs*)p); }
+  static hipError_t go(const NormArgs& a, hipStream_t)
+  {
+    emu::run_grid(&entry, &a, C::NT, ROWS_LDS_BYTES, (unsigned)((a.rows + C::ROWS - 1) / C::ROWS), 1, 1);
+    return hipSuccess;
+  }
+};
+template <class C>
+struct NormGrad {
+  struct Both {
+    NormGradArgs a;
+    int groups;
+  };
+  static void entry(const void* p) { alcop_norm_grad<C, emu::Emu>(((const Both*)p)->a, ((const Both*)p)->groups); }
+  static hipError_t go(const NormGradArgs& a, int groups, hipStream_t)
+  {
+    const Both b{a, groups};
+    emu::run_grid(&entry, &b, C::NT, ROWS_LDS_BYTES, (unsigned)(groups / C::ROWS), 1, 1);
+    return hipSuccess;
+  }
+};
+hipError_t launch_norm_rows(const NormArgs& a, int dt, bool vec, hipStream_t st)
+{
+  return dispatch_rows_of<Norm>(dt, vec, a.cols, a, st);
+}
+hipError_t launch_norm_grad(const NormGradArgs& a, int groups, int dt, bool vec, hipStream_t st)
+{
+  return dispatch_rows_of<NormGrad>(dt, vec, a.cols, a, groups, st);
+}
+static void sums_entry(const void* p) { alcop_column_sums<emu::Emu>(*(const ColumnSumArgs*)p); }
+hipError_t launch_column_sums(const ColumnSumArgs& a, hipStream_t)
+{
+  emu::run_grid(&sums_entry, &a, SUM_THREADS, SUM_THREADS * 4, (unsigned)((a.cols + SUM_COLS - 1) / SUM_COLS), 1, 1);
+  return hipSuccess;
+}
+static void act_entry(const void* p) { alcop_act_grad<emu::Emu>(*(const ActGradArgs*)p); }
+hipError_t launch_act_grad(const ActGradArgs& a, hipStream_t)
+{
+  emu::run_grid(&act_entry, &a, 256, 4 * ACT_COLS * 4, (unsigned)((a.N + ACT_COLS - 1) / ACT_COLS),
+                (unsigned)((a.M + a.rows_per_block - 1) / a.rows_per_block), 1);
+  return hipSuccess;
+}
+hipError_t prepare_rows() { return hipSuccess; }
+#endif
+
+}  // namespace alcop
+
+#if EMU_PART == 3
+// the model's conversions of 8-bit numbers, so that a test can pin them
+extern "C" uint8_t emu_f32_to_e4m3(float v) { return emu::float_to_e4m3(v); }
+extern "C" float emu_e4m3_to_f32(uint8_t b) { return emu::e4m3_to_float(b); }
+#endif
