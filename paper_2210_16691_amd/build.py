@@ -19,6 +19,7 @@ CSRC = os.path.join(HERE, "csrc")
 ROOT = os.path.dirname(HERE)
 OBJDIR = os.path.join(ROOT, "_build", "alcop")
 LIB = os.path.join(HERE, "libalcop.so")
+F8_LIB = os.path.join(HERE, "libalcop_f8.so")         # kernels of the 8-bit matrix instruction, linked by libalcop.so
 DIAG_LIB = os.path.join(HERE, "libalcop_diag.so")     # measurement aid: csrc/diag_*.hip
 
 MARSHAL_SRC = os.path.join(CSRC, "py_binding.cpp")    # argument marshalling of the Python binding
@@ -34,12 +35,16 @@ FLAGS = [
 
 
 def sources():
-    hip = [f for f in glob.glob(os.path.join(CSRC, "*.hip")) if not os.path.basename(f).startswith("diag_")]
+    hip = [f for f in glob.glob(os.path.join(CSRC, "*.hip")) if not os.path.basename(f).startswith(("diag_", "f8_"))]
     return sorted(hip + [f for f in glob.glob(os.path.join(CSRC, "*.cpp")) if f != MARSHAL_SRC])
 
 
 def diag_sources():
     return sorted(glob.glob(os.path.join(CSRC, "diag_*.hip")))
+
+
+def f8_sources():
+    return sorted(glob.glob(os.path.join(CSRC, "f8_*.hip")))
 
 
 def _deps_mtime(obj: str) -> float:
@@ -91,16 +96,17 @@ def build_marshal(force: bool = False) -> str:
 
 def build(jobs: int = 8, force: bool = False) -> str:
     os.makedirs(OBJDIR, exist_ok=True)
-    srcs = sources()
-    dsrcs = diag_sources()
+    groups = [(F8_LIB, f8_sources(), []),
+              (LIB, sources(), ["-L" + HERE, "-lalcop_f8", "-Wl,-rpath,$ORIGIN"]),
+              (DIAG_LIB, diag_sources(), [])]
     with cf.ThreadPoolExecutor(max_workers=max(1, min(jobs, 16))) as ex:
         marshal = ex.submit(build_marshal, force)
-        allobjs = list(ex.map(lambda s: _compile(s, force), srcs + dsrcs))
+        pending = [[ex.submit(_compile, f, force) for f in srcs] for _, srcs, _ in groups]
+        objs = [[p.result() for p in ps] for ps in pending]
         marshal.result()
-    objs, dobjs = allobjs[:len(srcs)], allobjs[len(srcs):]
-    for lib, obs in ((LIB, objs), (DIAG_LIB, dobjs)):
+    for (lib, _, libs), obs in zip(groups, objs):
         if obs and (force or not os.path.exists(lib) or any(os.path.getmtime(o) > os.path.getmtime(lib) for o in obs)):
-            subprocess.check_call([HIPCC, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", lib] + obs)
+            subprocess.check_call([HIPCC, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", lib] + obs + libs)
     return LIB
 
 

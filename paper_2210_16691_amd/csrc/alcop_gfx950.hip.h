@@ -134,6 +134,15 @@ struct Gfx950 {
                                                      __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
   }
 
+  // v_mfma_f32_32x32x64_f8f6f4 on e4m3: X lane l = row l%32, 32 of the k in its 32 bytes; Y likewise by column; D as above
+  typedef int i32x8 __attribute__((ext_vector_type(8)));
+  __device__ static __forceinline__ f32x16 mma64(u32x4 x0, u32x4 x1, u32x4 y0, u32x4 y1, f32x16 acc)
+  {
+    const i32x8 x = {(int)x0[0], (int)x0[1], (int)x0[2], (int)x0[3], (int)x1[0], (int)x1[1], (int)x1[2], (int)x1[3]};
+    const i32x8 y = {(int)y0[0], (int)y0[1], (int)y0[2], (int)y0[3], (int)y1[0], (int)y1[1], (int)y1[2], (int)y1[3]};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, acc, 0, 0, 0, 0, 0, 0);      // no scales
+  }
+
   template <int DT>
   __device__ static __forceinline__ f32x4 mma16(u32x4 x, u32x4 y, f32x4 acc)
   {
@@ -215,7 +224,12 @@ struct Gfx950 {
   }
 
   // ---- operations of the epilogue of linear layers and of the row kernels ---------------------------------
-  __device__ static __forceinline__ u32x2 global_load8(const void* ptr) { return *(const u32x2*)ptr; }
+  typedef u32x2 u32x2_any __attribute__((aligned(2)));
+  __device__ static __forceinline__ u32x2 global_load8_any(const void* ptr) { return *(const u32x2_any*)ptr; }
+  __device__ static __forceinline__ void global_store8_any(void* ptr, u32x2 v)
+  {
+    __builtin_nontemporal_store(v, (u32x2_any*)ptr);
+  }
   __device__ static __forceinline__ void global_store_u8(void* ptr, uint8_t v) { *(uint8_t*)ptr = v; }
   __device__ static __forceinline__ float f16_bits(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }
   // two floats -> two e4m3 in the low 16 bits, round to nearest even; magnitudes up to 464 give at most 448, NaN stays

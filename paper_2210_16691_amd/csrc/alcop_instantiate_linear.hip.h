@@ -32,20 +32,20 @@ hipError_t launch_linear(const LinearArgs& a, dim3 grid, hipStream_t st)
   return hipGetLastError();
 }
 
-template <int DT, int BM, int BN, int BK, int WM, int WN, int S, int R, int F, int BL>
+template <int CL, int DT, int BM, int BN, int BK, int WM, int WN, int S, int R, int F, int BL>
 void add_linear(std::vector<LinearKernel>& t)
 {
-  using C = LCfg<DT, BM, BN, BK, WM, WN, S, R, F, BL>;
+  using C = LCfg<CL, DT, BM, BN, BK, WM, WN, S, R, F, BL>;
   constexpr auto K = &alcop_linear_tile<C, Gfx950>;
-  t.push_back(LinearKernel{DT, BL, alcop_sched{BM, BN, BK, WM, WN, S, R, F, 1, 0, 0}, C::NT, C::LDS_BYTES,
+  t.push_back(LinearKernel{CL, DT, BL, alcop_sched{BM, BN, BK, WM, WN, S, R, F, 1, 0, 0}, C::NT, C::LDS_BYTES,
                            &launch_linear<C, K>, &prepare_linear<C, K>});
 }
-template <int DT, int BM, int BN, int NW, int BL>
+template <int CL, int DT, int BM, int BN, int NW, int BL>
 void add_linear_ksplit(std::vector<LinearKernel>& t)
 {
-  using C = LWCfg<DT, BM, BN, NW, 2, BL>;
+  using C = LWCfg<CL, DT, BM, BN, NW, 2, BL>;
   constexpr auto K = &alcop_linear_ksplit<C, Gfx950>;
-  t.push_back(LinearKernel{DT, BL, alcop_sched{BM, BN, 64, BM, BN, 2, 1, 0, 1, 0, 3}, C::NT, C::LDS_BYTES,
+  t.push_back(LinearKernel{CL, DT, BL, alcop_sched{BM, BN, 64, BM, BN, 2, 1, 0, 1, 0, 3}, C::NT, C::LDS_BYTES,
                            &launch_linear<C, K>, &prepare_linear<C, K>});
 }
 

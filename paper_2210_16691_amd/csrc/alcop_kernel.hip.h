@@ -261,7 +261,7 @@ struct Opnd {
   }
 };
 
-// One kernel = one KCfg.  DT: 0 fp16, 1 bf16 operands (2, pairs of e4m3: alcop_linear.hip.h).  BM x BN x BK: block tile; WM x WN: wave
+// One kernel = one KCfg.  DT: 0 fp16, 1 bf16 operands (2, 3: pairs of e4m3, alcop_linear.hip.h).  BM x BN x BK: block tile; WM x WN: wave
 // tile.  S: stages of the LDS ring (1 = unpipelined); R: register slots for fragments (2 = the
 // inner, LDS -> register pipeline); FUSE: the inner pipeline runs across k-tiles (Fig. 3(d)).
 // BL / AL: operand layouts; AM: how the A tile is produced (matrix or convolution gather);
@@ -273,13 +273,15 @@ struct KCfg {
   static constexpr int DT = DT_, BM = BM_, BN = BN_, BK = BK_, WM = WM_, WN = WN_;
   static constexpr int S = S_, R = R_, FUSE = FUSE_, BL = BL_, AM = AM_, AL = AL_, SK = SK_;
   static constexpr int PF = PF_;
-  static constexpr bool LINEAR = false;   // the epilogue of alcop_linear.hip.h in place of the one below
+  static constexpr bool LINEAR = false;   // the epilogue of alcop_linear.hip.h in place of the one below, and
+  struct Ahead {};                         // what it loads ahead of the main loop
   static constexpr int WAVES_M = BM / WM, WAVES_N = BN / WN, NWAVES = WAVES_M * WAVES_N;
   static constexpr int NT = NWAVES * 64;
   // AL: 0 = A stored M x K, 1 = A stored K x M.  BL: 0 = B stored K x N, 1 = B stored N x K.
   using OA = Opnd<AL ? LAY_MN : LAY_K, BM, WM, BK, NT>;
   using OB = Opnd<BL ? LAY_K : LAY_MN, BN, WN, BK, NT>;
-  static constexpr int TM = WM / 32, TN = WN / 32, NKI = BK / 16;
+  static constexpr int KF = DT == 3 ? 2 : 1;    // 16-byte chunks a lane holds of an operand's fragment
+  static constexpr int TM = WM / 32, TN = WN / 32, NKI = BK / (16 * KF);
   static constexpr bool FLAT_STORES = !AL && TM == 4 && TN == 4;   // see store_chunk_if
   // kernels that can leave C in the caches (store_chunk): layers; not where no register is free
   static constexpr bool KEEPS = AM == 0 && !AL && !SK && !FLAT_STORES;
@@ -306,6 +308,7 @@ struct KCfg {
   static constexpr int WAIT = (S >= 2 ? (S - 2) * L : 0);    // loads allowed in flight at a wait
   static_assert(BM % WM == 0 && BN % WN == 0 && WM % 32 == 0 && WN % 32 == 0, "wave tile");
   static_assert(BK == 32 || BK == 64 || BK == 128, "bk");
+  static_assert(KF == 1 || (R == 2 && BK >= 64), "fragments of two chunks: register pipeline of two slots, two steps");
   static_assert(S >= 1 && S <= 4 && R >= 1 && R <= 4, "stages");
   static_assert(!FUSE || (R >= 2 && S >= 2), "fusion needs a register double buffer and S>=2");
   // R >= 3: R - 1 fragments are in flight ahead of the one the matrix cores consume.  They may
@@ -658,7 +661,8 @@ __device__ __forceinline__ void store_chunk_if(const Params& p, char* dst, int n
 
 // the epilogue of linear layers (alcop_linear.hip.h)
 template <class C, class HW, class P>
-__device__ __forceinline__ void linear_tile(const P& p, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, uint32_t ebase, int lane);
+__device__ __forceinline__ void linear_tile(const P& p, typename C::Ahead& ahead, f32x16 (&acc)[C::TN][C::TM], int m0, int n0,
+                                            uint32_t ebase, int lane);
 
 template <class C, class HW, class P = Params>
 __device__ __forceinline__ void mainloop_body(const P& p)
@@ -676,6 +680,8 @@ __device__ __forceinline__ void mainloop_body(const P& p)
 
   int tm, tn;
   tile_of_block(p, HW::block_x(), tm, tn);
+  typename C::Ahead ahead;
+  if constexpr (C::LINEAR) ahead.template load<HW>(p, tm * BM + wm * WM, tn * BN + wn * WN, lane);
   // the k range of this block: all of K, or one slice of it (split-K; slices are whole k-tiles)
   int k0 = 0, Kb = p.K;
   if constexpr (C::SK) {
@@ -899,15 +905,25 @@ __device__ __forceinline__ void mainloop_body(const P& p)
 #pragma unroll
     for (int i = 0; i < OB::NRD; i++) curB[i] = sbase + rdB[i];
   };
-  // LDS read instruction r of fragment ki: the A reads come first, then the B reads.
-  constexpr int NRI = OA::NRI + OB::NRI;
-  auto read_one = [&](int ki, int r, u32x4(&fa)[TM], u32x4(&fb)[TN]) {
-    if (r < OA::NRI)
-      read_instr<OA, HW>(curA, ki, r, fa);
-    else
-      read_instr<OB, HW>(curB, ki, r - OA::NRI, fb);
+  // LDS read instruction r of fragment ki: the A reads come first, then the B reads.  Fragments of two chunks: element
+  // TM (TN) + i of the array is the second chunk of sub-tile i.
+  constexpr int KF = C::KF;
+  constexpr int NRI = (OA::NRI + OB::NRI) * KF;
+  auto read_one = [&](int ki, int r, u32x4(&fa)[TM * KF], u32x4(&fb)[TN * KF]) {
+    if constexpr (KF == 1) {
+      if (r < OA::NRI)
+        read_instr<OA, HW>(curA, ki, r, fa);
+      else
+        read_instr<OB, HW>(curB, ki, r - OA::NRI, fb);
+    } else {
+      static_assert(KF == 1 || (OA::LAY == LAY_K && OB::LAY == LAY_K), "fragments of two chunks");
+      if (r < TM * KF)
+        fa[r] = HW::lds_read16(curA[ki * KF + r / TM] + r % TM * (32 * BK * 2));
+      else
+        fb[r - TM * KF] = HW::lds_read16(curB[ki * KF + (r - TM * KF) / TN] + (r - TM * KF) % TN * (32 * BK * 2));
+    }
   };
-  auto load_frags = [&](int ki, u32x4(&fa)[TM], u32x4(&fb)[TN]) {
+  auto load_frags = [&](int ki, u32x4(&fa)[TM * KF], u32x4(&fb)[TN * KF]) {
 #pragma unroll
     for (int r = 0; r < NRI; r++) read_one(ki, r, fa, fb);
   };
@@ -927,14 +943,17 @@ __device__ __forceinline__ void mainloop_body(const P& p)
   // leaves room for the block-wide synchronisation that `sync` performs after instruction
   // first-1.  The compiler must keep exactly this order (sched_barrier).
   constexpr int NMM = TM * TN;
-  auto step = [&](u32x4(&ua)[TM], u32x4(&ub)[TN], bool nread, int nki, u32x4(&na)[TM],
-                  u32x4(&nb)[TN], int d0, int d1, int first, auto&& sync) {
+  auto step = [&](u32x4(&ua)[TM * KF], u32x4(&ub)[TN * KF], bool nread, int nki, u32x4(&na)[TM * KF],
+                  u32x4(&nb)[TN * KF], int d0, int d1, int first, auto&& sync) {
     const int gaps = NMM - first > 0 ? NMM - first : 1;
     const int rpg = (NRI + gaps - 1) / gaps > 2 ? (NRI + gaps - 1) / gaps : 2;   // reads per gap
 #pragma unroll
     for (int m = 0; m < NMM; m++) {
       const int i = m / TM, j = m % TM;
-      acc[i][j] = HW::template mma<C::DT>(ub[i], ua[j], acc[i][j]);
+      if constexpr (KF == 1)
+        acc[i][j] = HW::template mma<C::DT>(ub[i], ua[j], acc[i][j]);
+      else
+        acc[i][j] = HW::mma64(ub[i], ub[TN + i], ua[j], ua[TM + j], acc[i][j]);
       if (m + 1 == first || (first >= NMM && m == NMM - 1)) sync();
       if (nread && (m >= first || m == NMM - 1)) {
         const int g = m >= first ? m - first : 0;
@@ -948,7 +967,7 @@ __device__ __forceinline__ void mainloop_body(const P& p)
   };
   auto no_sync = [] {};
 
-  u32x4 fa[C::R][TM], fb[C::R][TN];
+  u32x4 fa[C::R][TM * KF], fb[C::R][TN * KF];
 
   // ---- the pipelined main loop -----------------------------------------------------------
   if constexpr (C::FUSE && C::R >= 3) {
@@ -1086,10 +1105,11 @@ __device__ __forceinline__ void mainloop_body(const P& p)
     }
   }
   if constexpr (C::LINEAR) {
+    ahead.template load_late<HW>(p, tm * BM + wm * WM, tn * BN + wn * WN, lane);
     HW::template wait_vm<0>();
     HW::wait_lds();
     HW::block_barrier();   // every wave has finished reading the ring
-    linear_tile<C, HW>(p, acc, tm * BM + wm * WM, tn * BN + wn * WN, lds0 + (uint32_t)wave * C::EPI_WAVE_BYTES, lane);
+    linear_tile<C, HW>(p, ahead, acc, tm * BM + wm * WM, tn * BN + wn * WN, lds0 + (uint32_t)wave * C::EPI_WAVE_BYTES, lane);
     return;
   }
   const bool fused = p.alpha != 1.0f || p.bias != nullptr || p.act != 0;

@@ -82,7 +82,8 @@ struct WaveOpnd {
 template <int DT_, int BM_, int BN_, int NW_, int S_, int BL_, int AM_, int AL_ = 0>
 struct WCfg {
   static constexpr int DT = DT_, BM = BM_, BN = BN_, BK = 64, NW = NW_, S = S_, BL = BL_, AM = AM_, AL = AL_;
-  static constexpr bool LINEAR = false;   // the epilogue of alcop_linear.hip.h
+  static constexpr bool LINEAR = false;   // the epilogue of alcop_linear.hip.h, and
+  struct Ahead {};                         // what it loads ahead of the main loop
   static constexpr int NT = NW * 64;
   using OA = WaveOpnd<AL ? LAY_MN : LAY_K, BM>;
   using OB = WaveOpnd<BL ? LAY_K : LAY_MN, BN>;
@@ -99,8 +100,8 @@ struct WCfg {
 };
 
 // the epilogue of linear layers (alcop_linear.hip.h)
-template <class HW, class P>
-__device__ __forceinline__ void linear_group(const P& p, int m, int n, const f32x4& sum);
+template <class C, class HW, class P>
+__device__ __forceinline__ void linear_group(const P& p, const typename C::Ahead& ahead, int turn, int m, int n, const f32x4& sum);
 
 template <class C, class HW, class P = Params>
 __device__ __forceinline__ void ksplit_body(const P& p)
@@ -114,6 +115,8 @@ __device__ __forceinline__ void ksplit_body(const P& p)
   const int batch = HW::block_y();
   int tm, tn;
   tile_of_block(p, HW::block_x(), tm, tn);
+  typename C::Ahead ahead;
+  if constexpr (C::LINEAR) ahead.template load<HW>(p, tm * BM, tn * BN, wave * 64 + lane);
 
   // this wave's k-tiles: [kt0, kt1)
   const int nko = (p.K + BK - 1) / BK;
@@ -311,7 +314,7 @@ __device__ __forceinline__ void ksplit_body(const P& p)
       for (int e = 0; e < 4; e++) v[e] += f[e];
     }
     if constexpr (C::LINEAR) {
-      linear_group<HW>(p, m, n, v);
+      linear_group<C, HW>(p, ahead, g0 / C::NT, m, n, v);
       continue;
     }
     if (fused) {

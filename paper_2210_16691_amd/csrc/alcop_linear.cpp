@@ -5,8 +5,8 @@
 #include <cstdlib>
 #include <cstring>
 
-#include "alcop_dispatch.h"
 #include "alcop_linear.h"
+#include "alcop_linear_cost.h"
 
 namespace alcop {
 namespace {
@@ -18,6 +18,10 @@ const std::vector<LinearKernel>& linear_kernels()
     register_linear_f16(t);
     register_linear_bf16(t);
     register_linear_e4m3(t);
+    register_linear_f8(t);
+    for (LinearKernel& k : t)
+      for (const LinearCost& m : kLinearCost)
+        if (m.dt == (k.dt == 0 ? 1 : k.dt) && m.bl == k.bl && std::memcmp(&m.s, &k.s, sizeof(k.s)) == 0) k.cost = &m;
     return t;
   }();
   return table;
@@ -49,27 +53,25 @@ bool meet(const Span& a, const Span& b)
 }
 bool same(const Span& a, const Span& b) { return a.p == b.p && (a.rows < 2 || a.pitch == b.pitch) && a.row == b.row; }
 
-// The kernel of the lowest measured cost (alcop_dispatch.h); an e4m3 problem counts as one of half its K on 16 bits,
-// which moves as many bytes and takes as many matrix instructions.
-const LinearKernel* pick(int dt, int bl, const alcop_problem& p)
+// The kernel of the lowest measured cost.  fine: e4m3 operands may be multiplied as they are (a sum of the 8-bit matrix
+// instruction is not one of fp32, which a result in fp32 is worth; 8192 x 8192 x 4096: 306 us so, 436 widened).
+const LinearKernel* pick(int cls, int dt, int bl, bool fine, int M, int N, int K, double bytes)
 {
   const LinearKernel* best = nullptr;
   double best_us = 0;
   const char* env = std::getenv("ALCOP_LINEAR_KERNEL");       // a tuning and test knob: its number among those of the layout
   int nr = 0;
   for (const LinearKernel& k : linear_kernels()) {
-    if (k.dt != dt || k.bl != bl) continue;
+    if (k.cls != cls || k.bl != bl || !(k.dt == dt || (dt == 2 && k.dt == 3 && !fine))) continue;
     if (env && *env) {
       if (nr++ == std::atoi(env)) return &k;
       continue;
     }
-    for (const MeasuredCost& m : kMeasured) {
-      if (std::memcmp(&m.s, &k.s, sizeof(k.s)) != 0 || !measured_applies(p, m)) continue;
-      const double us = measured_us(p, m);
-      if (!best || us < best_us) {
-        best = &k;
-        best_us = us;
-      }
+    if (!k.cost || !linear_applies(*k.cost, M, N)) continue;
+    const double us = linear_us(*k.cost, M, N, K, bytes);
+    if (!best || us < best_us) {
+      best = &k;
+      best_us = us;
     }
   }
   return best;
@@ -132,23 +134,18 @@ int alcop_linear(const void* A, const void* W, void* C, int M, int N, int K, lon
   const long far = 1L << 30;
   if (lda >= far || ldw >= far || ldc >= far || t.ldr >= far || t.ldp >= far) return ALCOP_ERR_SIZE;
 
-  alcop_problem p;
-  std::memset(&p, 0, sizeof(p));
-  p.op = ALCOP_OP_GEMM;
-  p.batch = 1;
-  p.M = M;
-  p.N = N;
-  p.K = in == ALCOP_E4M3 ? K / 2 : K;
-  p.transB = transB;
-  p.in = in == ALCOP_F16 ? ALCOP_F16 : ALCOP_BF16;
-  p.out = out;
-  const LinearKernel* k = pick(in == ALCOP_E4M3 ? 2 : in == ALCOP_BF16 ? 1 : 0, transB, p);
+  const int K16 = in == ALCOP_E4M3 ? K / 2 : K;              // in units of 16 bits
+  const double c_bytes = (double)osz * M * N;
+  const double bytes = 2.0 * K16 * ((double)M + N) + c_bytes * (1 + (t.residual ? 1 : 0) + (t.pre ? 1 : 0));
+  const LinearKernel* k = pick(class_of(t.act), in == ALCOP_E4M3 ? 2 : in == ALCOP_BF16 ? 1 : 0, transB, out == ALCOP_F32, M, N, K16,
+                               bytes);
   if (!k) return ALCOP_ERR_SCHED;
   // 32-bit byte offsets from a tile's origin, rows past the end of a partial k-tile included
   const double rows = std::min(k->s.bm, M), cols = std::min(k->s.bn, N);
-  const double kceil = (double)((p.K + k->s.bk - 1) / k->s.bk) * k->s.bk;
+  const double kceil = (double)((K16 + k->s.bk - 1) / k->s.bk) * k->s.bk;
   if (esz * (rows * (double)lda) >= 2147483648.0 || (transB ? esz * (cols * (double)ldw) : 2.0 * kceil * ldw) >= 2147483648.0)
     return ALCOP_ERR_SIZE;
+  if (osz * rows * (double)std::max(ldc, std::max(t.residual ? t.ldr : 0, t.pre ? t.ldp : 0)) >= 2147483648.0) return ALCOP_ERR_SIZE;
   const long ntm = ((long)M + k->s.bm - 1) / k->s.bm, ntn = ((long)N + k->s.bn - 1) / k->s.bn;
   if (ntm * ntn > 0x7fffffffL) return ALCOP_ERR_SHAPE;
 
@@ -159,6 +156,10 @@ int alcop_linear(const void* A, const void* W, void* C, int M, int N, int K, lon
     if (meet(c, s) || meet(z, s)) return ALCOP_ERR_UNSUPPORTED;
   if (meet(c, z) || meet(r, z) || (meet(c, r) && !same(c, r))) return ALCOP_ERR_UNSUPPORTED;
 
+  // C stays in the memory-side cache, for the operator that reads it next, unless it is too large for that: two layers in a
+  // row (hidden results of 4 to 34 MB) are 4 to 10 % faster kept, from 67 MB on 1 to 2.5 % slower; what nothing reads
+  // costs 1 to 6 % more to keep
+  const bool keep = c_bytes <= 48e6;
   LinearArgs a;
   a.A = A;
   a.W = W;
@@ -170,17 +171,14 @@ int alcop_linear(const void* A, const void* W, void* C, int M, int N, int K, lon
   a.sw = (const float*)t.scale_w;
   a.M = M;
   a.N = N;
-  a.K = p.K;
+  a.K = K16;
   a.lda = (int)(in == ALCOP_E4M3 ? lda / 2 : lda);
   a.ldw = (int)(in == ALCOP_E4M3 ? ldw / 2 : ldw);
   a.ldc = (int)ldc;
   a.ldr = t.residual ? (int)t.ldr : 0;
   a.ldp = t.pre ? (int)t.ldp : 0;
   a.alpha = t.alpha;
-  const int chunk = 16 / osz;
-  const bool chunks = N % 8 == 0 && aligned(C, 16) && aligned(t.residual, 16) && aligned(t.pre, 16) && ldc % chunk == 0 &&
-                      a.ldr % chunk == 0 && a.ldp % chunk == 0;
-  a.flags = (int)out | t.act << 2 | (chunks ? 32 : 0);
+  a.flags = (int)out | t.act << 2 | (keep ? 32 : 0);
   if (std::getenv("ALCOP_LOG"))
     std::fprintf(stderr, "alcop: linear M %d N %d K %d in %d -> tile %dx%dx%d waves %dx%d S%d R%d F%d variant %d grid %ld\n", M,
                  N, K, (int)in, k->s.bm, k->s.bn, k->s.bk, k->s.wm, k->s.wn, k->s.stages, k->s.reg_stages, k->s.fuse_inner,
@@ -249,14 +247,13 @@ int alcop_linear_backward(const void* dC, const void* A, const void* W, const vo
     g.lddc = lddc;
     g.ldp = ldp;
     g.act = act;
-    g.dt = in == ALCOP_BF16;
     if (act && (dA || dW)) {
       dZ = g.dz = workspace;
       lddz = g.ldz = N;
     }
     float* sums = (float*)((char*)workspace + r256(2.0 * M * N));
     if (dbias) g.partial = blocks == 1 ? (float*)dbias : sums;
-    if (launch_act_grad(g, st) != hipSuccess) return ALCOP_ERR_LAUNCH;
+    if (launch_act_grad(g, in == ALCOP_BF16, st) != hipSuccess) return ALCOP_ERR_LAUNCH;
     if (dbias && blocks > 1) {
       const ColumnSumArgs s{sums, (float*)dbias, blocks, N};
       if (launch_column_sums(s, st) != hipSuccess) return ALCOP_ERR_LAUNCH;

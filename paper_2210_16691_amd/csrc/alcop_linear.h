@@ -10,21 +10,24 @@
 
 namespace alcop {
 
+struct LinearCost;
 struct LinearKernel {
-  int dt, bl;                  // as in LCfg
-  alcop_sched s;               // tile and pipelining, by which alcop_dispatch.h knows the kernel's cost
+  int cls, dt, bl;             // as in LCfg
+  alcop_sched s;               // tile and pipelining
   int threads, lds_bytes;
   hipError_t (*launch)(const LinearArgs&, dim3, hipStream_t);
   hipError_t (*prepare)();
+  const LinearCost* cost = nullptr;     // alcop_linear_cost.h
 };
 void register_linear_f16(std::vector<LinearKernel>&);
 void register_linear_bf16(std::vector<LinearKernel>&);
 void register_linear_e4m3(std::vector<LinearKernel>&);
+void register_linear_f8(std::vector<LinearKernel>&);      // in libalcop_f8.so
 
 hipError_t launch_norm_rows(const NormArgs& a, int dt, bool vec, hipStream_t st);
 hipError_t launch_norm_grad(const NormGradArgs& a, int groups, int dt, bool vec, hipStream_t st);
 hipError_t launch_column_sums(const ColumnSumArgs& a, hipStream_t st);
-hipError_t launch_act_grad(const ActGradArgs& a, hipStream_t st);
+hipError_t launch_act_grad(const ActGradArgs& a, int dt, hipStream_t st);
 hipError_t prepare_rows();
 
 // Threads that share a row, and their chunks of eight elements: a wave while that takes at most four chunks a lane,
@@ -60,15 +63,27 @@ int gradient_product(const void* A, const void* B, void* C, int M, int N, int K,
 
 }  // namespace alcop
 
-// The kernels of one operand type and layout.
-#define ALCOP_LINEAR_KERNELS(T, DT, BL)                    \
-  add_linear_ksplit<DT, 16, 16, 8, BL>(T);                 \
-  add_linear_ksplit<DT, 16, 32, 8, BL>(T);                 \
-  add_linear_ksplit<DT, 32, 32, 8, BL>(T);                 \
-  add_linear_ksplit<DT, 32, 64, 4, BL>(T);                 \
-  add_linear<DT, 64, 64, 64, 32, 32, 3, 2, 1, BL>(T);      \
-  add_linear<DT, 128, 128, 64, 64, 64, 2, 1, 0, BL>(T);    \
-  add_linear<DT, 128, 128, 64, 64, 64, 4, 2, 1, BL>(T);    \
-  add_linear<DT, 256, 128, 64, 128, 64, 3, 2, 1, BL>(T);   \
-  add_linear<DT, 256, 192, 32, 128, 96, 3, 2, 1, BL>(T);   \
-  add_linear<DT, 256, 256, 32, 128, 64, 3, 2, 1, BL>(T);
+// The kernels of one operand type and layout, each per class of activation.
+#define ALCOP_LINEAR_CLASS(T, CL, DT, BL)                      \
+  add_linear_ksplit<CL, DT, 16, 16, 8, BL>(T);                 \
+  add_linear_ksplit<CL, DT, 16, 32, 8, BL>(T);                 \
+  add_linear_ksplit<CL, DT, 32, 32, 8, BL>(T);                 \
+  add_linear_ksplit<CL, DT, 32, 64, 4, BL>(T);                 \
+  add_linear<CL, DT, 64, 64, 64, 32, 32, 3, 2, 1, BL>(T);      \
+  add_linear<CL, DT, 128, 64, 64, 64, 32, 3, 2, 1, BL>(T);     \
+  add_linear<CL, DT, 128, 128, 64, 64, 64, 2, 2, 1, BL>(T);    \
+  add_linear<CL, DT, 128, 128, 64, 64, 64, 4, 2, 1, BL>(T);    \
+  add_linear<CL, DT, 256, 128, 64, 128, 64, 3, 2, 1, BL>(T);   \
+  add_linear<CL, DT, 256, 256, 32, 128, 64, 3, 2, 1, BL>(T);
+#define ALCOP_LINEAR_KERNELS(T, DT, BL)     \
+  ALCOP_LINEAR_CLASS(T, CLASS_PLAIN, DT, BL)   \
+  ALCOP_LINEAR_CLASS(T, CLASS_SIGMOID, DT, BL) \
+  ALCOP_LINEAR_CLASS(T, CLASS_ERF, DT, BL)
+// The kernels that multiply e4m3 as they are.
+#define ALCOP_LINEAR_F8(T, CL)                              \
+  add_linear<CL, 3, 64, 64, 64, 32, 32, 3, 2, 1, 1>(T);     \
+  add_linear<CL, 3, 128, 64, 64, 64, 32, 3, 2, 1, 1>(T);    \
+  add_linear<CL, 3, 128, 128, 64, 64, 64, 2, 2, 1, 1>(T);   \
+  add_linear<CL, 3, 128, 128, 64, 64, 64, 4, 2, 1, 1>(T);   \
+  add_linear<CL, 3, 256, 128, 64, 128, 64, 3, 2, 1, 1>(T);  \
+  add_linear<CL, 3, 256, 256, 64, 128, 64, 2, 2, 1, 1>(T);

@@ -9,16 +9,22 @@
 // The loops are those of alcop_kernel.hip.h and alcop_ksplit.hip.h.  An e4m3 operand is to them one of 16-bit
 // elements, two e4m3 each: K and the pitches count pairs, and a fragment's 16 bytes are sixteen k in place of eight, for
 // two matrix instructions.  Which k a lane holds differs from the 16-bit layouts, but equally for both operands, and a
-// sum over k does not ask for their order.  They are widened to bf16 in registers (alcop_gfx950.hip.h says why).
+// sum over k does not ask for their order.  They are widened to bf16 in registers, or (large products whose result is
+// rounded to 16 bits) multiplied as they are, at twice the rate: alcop_gfx950.hip.h says what that costs a sum.
 //
 // Epilogue of a tile (linear_tile): as in alcop_kernel.hip.h a wave parks 32 rows of its accumulators in LDS, here
 // in fp32, and reads them back along the rows, eight columns a lane, so that residual, pre and C move in 16-byte
-// accesses that cover whole lines.  A lane's columns are the same in every row: bias and column scales are
-// fetched once per tile.
+// accesses (at any element) that cover whole lines.  A lane's columns are the same in every row: bias and column scales
+// are fetched once per tile.
 #pragma once
 #include "alcop_ksplit.hip.h"
 
 namespace alcop {
+
+template <int V>
+struct TypeOf {
+  static constexpr int value = V;
+};
 
 enum { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_GELU_TANH = 3, ACT_SILU = 4 };
 
@@ -31,7 +37,7 @@ struct LinearArgs {
   const float *bias, *sa, *sw;
   int M, N, K, lda, ldw, ldc, ldr, ldp;
   float alpha;
-  int flags;                   // output type | activation << 2 | rows of C, residual and pre made of 16-byte chunks << 5
+  int flags;                   // output type | activation << 2 | C is kept in the caches << 5
 };
 
 struct LinearParams : Params {
@@ -39,7 +45,6 @@ struct LinearParams : Params {
   void* pre;
   const float *sa, *sw;
   int ldr, ldp;
-  bool chunks;
 };
 
 template <class C>
@@ -59,7 +64,7 @@ __device__ __forceinline__ LinearParams expand_linear(const LinearArgs& a)
   p.alpha = a.alpha;
   p.out_dtype = a.flags & 3;
   p.act = (a.flags >> 2) & 7;
-  p.chunks = (a.flags & 32) != 0;
+  p.keep = (short)(a.flags >> 5 & 1);
   p.raster = 1;
   p.ntm = (p.M + C::BM - 1) / C::BM;
   p.ntn = (p.N + C::BN - 1) / C::BN;
@@ -91,16 +96,38 @@ struct Sigmoid {
   }
 };
 
-template <class HW, int W>
+// Kernels exist per class of activation: their epilogues are unrolled, and with all five in each the code of one tile
+// would be several times the instruction cache.
+enum { CLASS_PLAIN = 0, CLASS_SIGMOID = 1, CLASS_ERF = 2 };
+inline int class_of(int act) { return act == ACT_GELU ? CLASS_ERF : act >= ACT_GELU_TANH ? CLASS_SIGMOID : CLASS_PLAIN; }
+
+// erfc(|z| / sqrt 2) within 1.5e-7: Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26.  Its form,
+// a polynomial of t = 1 / (1 + p x) times exp(-x^2), keeps its relative accuracy where erfc is small, which 1 + erf does
+// not; the library's erff, with a branch of its own on either side of 1, cost 50 us of 311 in a layer of 8192 x 8192.
+template <class HW>
+__device__ __forceinline__ float erfc_of(float z, float& gauss)
+{
+  const float x = __builtin_fabsf(z) * 0.70710678119f;
+  const float t = HW::rcp(1.0f + 0.3275911f * x);
+  gauss = HW::exp2(-1.44269504089f * (x * x));
+  return gauss * (t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f)))));
+}
+
+template <int CLASS, class HW, int W>
 __device__ __forceinline__ void activate(float (&v)[W], int act)
 {
-  if (act == ACT_RELU) {
+  if constexpr (CLASS == CLASS_PLAIN) {
+    const float floor = act == ACT_RELU ? 0.f : -__builtin_inff();
 #pragma unroll
-    for (int e = 0; e < W; e++) v[e] = v[e] < 0.f ? 0.f : v[e];
-  } else if (act == ACT_GELU) {
+    for (int e = 0; e < W; e++) v[e] = v[e] < floor ? 0.f : v[e];
+  } else if constexpr (CLASS == CLASS_ERF) {
 #pragma unroll
-    for (int e = 0; e < W; e++) v[e] = 0.5f * v[e] * (1.0f + HW::erf(v[e] * 0.70710678119f));
-  } else if (act >= ACT_GELU_TANH) {
+    for (int e = 0; e < W; e++) {
+      float gauss;
+      const float q = erfc_of<HW>(v[e], gauss), half = q == 0.f ? 0.f : 0.5f * v[e] * q;      // v may be infinite
+      v[e] = v[e] < 0.f ? half : v[e] - half;
+    }
+  } else {
     const Sigmoid s = Sigmoid::of(act);
 #pragma unroll
     for (int e = 0; e < W; e++) v[e] *= s.at<HW>(v[e]);
@@ -113,8 +140,9 @@ __device__ __forceinline__ float slope(float z, int act)
 {
   if (act == ACT_RELU) return z > 0.f ? 1.f : 0.f;
   if (act == ACT_GELU) {
-    const float e = HW::exp2(-0.72134752044f * (z * z));          // exp(-z^2 / 2)
-    return 0.5f * (1.0f + HW::erf(z * 0.70710678119f)) + (e == 0.f ? 0.f : z * e * 0.39894228040f);
+    float gauss;                                                  // exp(-z^2 / 2)
+    const float half = 0.5f * erfc_of<HW>(z, gauss);
+    return (z < 0.f ? half : 1.0f - half) + (gauss == 0.f ? 0.f : z * gauss * 0.39894228040f);
   }
   if (act >= ACT_GELU_TANH) {
     const Sigmoid g = Sigmoid::of(act);
@@ -124,96 +152,113 @@ __device__ __forceinline__ float slope(float z, int act)
   return 1.f;
 }
 
-// ---- elements of the three output types ------------------------------------------------------------------
-template <class HW>
-__device__ __forceinline__ float half_to_float(uint32_t bits, int dt)
+// ---- elements of the three output types (DT: 0 fp16, 1 bf16, 2 fp32) -----------------------------------------
+template <int DT, class HW>
+__device__ __forceinline__ float half_to_float(uint32_t bits)
 {
-  return dt == 0 ? HW::f16_bits((uint16_t)bits) : __builtin_bit_cast(float, bits << 16);
+  return DT == 0 ? HW::f16_bits((uint16_t)bits) : __builtin_bit_cast(float, bits << 16);
 }
-template <class HW>
-__device__ __forceinline__ uint32_t float_to_half(float v, int dt)
+template <int DT, class HW>
+__device__ __forceinline__ uint32_t float_to_half(float v)
 {
-  return dt == 0 ? (uint32_t)__builtin_bit_cast(uint16_t, HW::template cvt<_Float16>(v))
+  return DT == 0 ? (uint32_t)__builtin_bit_cast(uint16_t, HW::template cvt<_Float16>(v))
                  : (uint32_t)__builtin_bit_cast(uint16_t, HW::template cvt<__bf16>(v));
 }
-
-// W consecutive elements of a row as they lie in memory: 16-bit ones in the first W / 2 words.
-template <int W>
-struct RawRow {
-  uint32_t w[W];
-};
-template <int W, class HW>
-__device__ __forceinline__ RawRow<W> load_chunk(const void* base, long at, int dt)
+template <int DT>
+__device__ __forceinline__ const char* element_at(const void* base, long at)
 {
-  RawRow<W> r;
-  const char* ptr = (const char*)base + at * (dt == 2 ? 4 : 2);
-  if (dt == 2) {
+  return (const char*)base + at * (DT == 2 ? 4 : 2);
+}
+
+// W consecutive elements of a row as they lie in memory, at any element.
+template <int W, int DT>
+struct RawRow {
+  uint32_t w[DT == 2 ? W : W / 2];
+};
+template <int W, int DT, class HW>
+__device__ __forceinline__ RawRow<W, DT> load_chunk(const char* ptr)
+{
+  constexpr int WORDS = DT == 2 ? W : W / 2;
+  RawRow<W, DT> r;
+  if constexpr (WORDS % 4 == 0) {
 #pragma unroll
-    for (int i = 0; i < W / 4; i++) {
+    for (int i = 0; i < WORDS / 4; i++) {
       const u32x4 t = HW::global_load16_any(ptr + 16 * i);
 #pragma unroll
       for (int e = 0; e < 4; e++) r.w[4 * i + e] = t[e];
     }
-  } else if constexpr (W == 8) {
-    const u32x4 t = HW::global_load16_any(ptr);
-#pragma unroll
-    for (int e = 0; e < 4; e++) r.w[e] = t[e];
   } else {
-    const u32x2 t = HW::global_load8(ptr);
+    const u32x2 t = HW::global_load8_any(ptr);
     r.w[0] = t[0];
     r.w[1] = t[1];
   }
   return r;
 }
-template <int W, class HW>
-__device__ __forceinline__ float element(const RawRow<W>& r, int e, int dt)
+template <int W, int DT, class HW>
+__device__ __forceinline__ float element(const RawRow<W, DT>& r, int e)
 {
-  if (dt == 2) return __builtin_bit_cast(float, r.w[e]);
-  const uint32_t h = (e & 1) ? r.w[e / 2] >> 16 : r.w[e / 2] & 0xffffu;
-  return half_to_float<HW>(h, dt);
+  if constexpr (DT == 2)
+    return __builtin_bit_cast(float, r.w[e]);
+  else
+    return half_to_float<DT, HW>((e & 1) ? r.w[e / 2] >> 16 : r.w[e / 2] & 0xffffu);
 }
 // KEEP: the line stays in the memory-side cache, as the next operator reads it (store_chunk in alcop_kernel.hip.h)
-template <int W, class HW, bool KEEP>
-__device__ __forceinline__ void store_row(void* base, long at, int dt, const float (&v)[W])
+template <int W, int DT, class HW, bool KEEP>
+__device__ __forceinline__ void store_row(const char* at, const float (&v)[W])
 {
-  char* ptr = (char*)base + at * (dt == 2 ? 4 : 2);
-  auto put16 = [&](char* dst, u32x4 t) {
+  char* ptr = const_cast<char*>(at);
+  auto put16 = [&](char* dst, u32x4 t) __attribute__((always_inline)) {
     if constexpr (KEEP)
       HW::global_store16_through(dst, t);
     else
-      HW::global_store16(dst, t);
+      HW::global_store16_any(dst, t);
   };
-  if (dt == 2) {
+  if constexpr (DT == 2) {
 #pragma unroll
     for (int i = 0; i < W / 4; i++)
       put16(ptr + 16 * i, __builtin_bit_cast(u32x4, f32x4{v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]}));
-    return;
-  }
-  uint32_t w[W / 2];
+  } else {
+    uint32_t w[W / 2];
 #pragma unroll
-  for (int e = 0; e < W / 2; e++) w[e] = float_to_half<HW>(v[2 * e], dt) | float_to_half<HW>(v[2 * e + 1], dt) << 16;
-  if constexpr (W == 8)
-    put16(ptr, u32x4{w[0], w[1], w[2], w[3]});
-  else
-    HW::template global_store<u32x2>(ptr, u32x2{w[0], w[1]});
+    for (int e = 0; e < W / 2; e++) w[e] = float_to_half<DT, HW>(v[2 * e]) | float_to_half<DT, HW>(v[2 * e + 1]) << 16;
+    if constexpr (W == 8)
+      put16(ptr, u32x4{w[0], w[1], w[2], w[3]});
+    else
+      HW::global_store8_any(ptr, u32x2{w[0], w[1]});
+  }
 }
-template <class HW>
-__device__ __forceinline__ float load_element(const void* base, long at, int dt)
+template <int DT, class HW>
+__device__ __forceinline__ float load_element(const void* base, long at)
 {
-  if (dt == 2) return __builtin_bit_cast(float, HW::global_load_u32((const char*)base + at * 4));
-  return half_to_float<HW>(HW::global_load_u16((const char*)base + at * 2), dt);
+  const char* ptr = element_at<DT>(base, at);
+  if constexpr (DT == 2)
+    return __builtin_bit_cast(float, HW::global_load_u32(ptr));
+  else
+    return half_to_float<DT, HW>(HW::global_load_u16(ptr));
 }
-template <class HW>
-__device__ __forceinline__ void store_element(void* base, long at, int dt, float v)
+template <int DT, class HW>
+__device__ __forceinline__ void store_element(void* base, long at, float v)
+{
+  char* ptr = const_cast<char*>(element_at<DT>(base, at));
+  if constexpr (DT == 2)
+    HW::global_store_u32(ptr, __builtin_bit_cast(uint32_t, v));
+  else
+    HW::global_store_u16(ptr, (uint16_t)float_to_half<DT, HW>(v));
+}
+// f(integral constant of the type)
+template <class F>
+__device__ __forceinline__ void by_type(int dt, F&& f)
 {
   if (dt == 2)
-    HW::global_store_u32((char*)base + at * 4, __builtin_bit_cast(uint32_t, v));
+    f(TypeOf<2>{});
+  else if (dt == 0)
+    f(TypeOf<0>{});
   else
-    HW::global_store_u16((char*)base + at * 2, (uint16_t)float_to_half<HW>(v, dt));
+    f(TypeOf<1>{});
 }
 
 // ---- the epilogue ------------------------------------------------------------------------------------------
-// What W consecutive columns from n < N on have in common over all rows.  W > 1: all of them exist.
+// What W consecutive columns from n on, all of which exist, have in common over all rows.
 template <int W>
 struct LinearColumns {
   float scale[W], bias[W];
@@ -245,68 +290,144 @@ __device__ __forceinline__ LinearColumns<W> linear_columns(const LinearParams& p
   for (int e = 0; e < W; e++) c.scale[e] *= p.alpha;
   return c;
 }
-
-// Row m's W columns from n on, of which v holds the sums.  W > 1: C, pre and the residual's chunk `res` are aligned.
-template <int W, class HW>
-__device__ __forceinline__ void linear_row(const LinearParams& p, const LinearColumns<W>& c, int m, int n, float (&v)[W],
-                                           float sa, const RawRow<W>& res)
-{
-#pragma unroll
-  for (int e = 0; e < W; e++) v[e] = v[e] * (c.scale[e] * sa) + c.bias[e];
-  const long at = (long)m * p.ldc + n, at_p = (long)m * p.ldp + n;
-  if (p.pre != nullptr) {
-    if constexpr (W == 1)
-      store_element<HW>(p.pre, at_p, p.out_dtype, v[0]);
-    else
-      store_row<W, HW, false>(p.pre, at_p, p.out_dtype, v);
-  }
-  activate<HW>(v, p.act);
-  if (p.residual != nullptr) {
-    if constexpr (W == 1) {
-      v[0] += load_element<HW>(p.residual, (long)m * p.ldr + n, p.out_dtype);
-    } else {
-#pragma unroll
-      for (int e = 0; e < W; e++) v[e] += element<W, HW>(res, e, p.out_dtype);
-    }
-  }
-  if constexpr (W == 1)
-    store_element<HW>(p.C, at, p.out_dtype, v[0]);
-  else
-    store_row<W, HW, true>(p.C, at, p.out_dtype, v);
-}
 template <class HW>
 __device__ __forceinline__ float row_scale(const LinearParams& p, int m)
 {
   return p.sa != nullptr ? __builtin_bit_cast(float, HW::global_load_u32(p.sa + m)) : 1.0f;
 }
 
-// A wave's tile, rows m0.., columns n0..; `ebase`: the wave's band in LDS.
-template <class C, class HW, class P>
-__device__ __forceinline__ void linear_tile(const P& p, f32x16 (&acc)[C::TN][C::TM], int m0, int n0, uint32_t ebase, int lane)
+// W columns of a row, of which v holds the sums and `res` the residual's; at_c, at_p: their place in C and pre.
+template <int W, int DT, int CLASS, class HW>
+__device__ __forceinline__ void linear_row(const LinearParams& p, const LinearColumns<W>& c, const char* at_c, const char* at_p,
+                                           float (&v)[W], float sa, const RawRow<W, DT>& res)
 {
-  constexpr int TN = C::TN, TM = C::TM;
-  constexpr int RS = C::WN * 4 + 16;               // LDS row stride of the band
-  constexpr int LPR = C::WN / 8;                   // lanes per row when reading back
-  constexpr int RPI = 64 / LPR;                    // rows per read; 96 columns: five, and four lanes idle
-  constexpr int NIT = (32 + RPI - 1) / RPI;
-  const int r0 = lane / LPR, n = n0 + lane % LPR * 8;
-  const bool lane_ok = r0 < RPI && n < p.N;
+#pragma unroll
+  for (int e = 0; e < W; e++) v[e] = v[e] * (c.scale[e] * sa) + c.bias[e];
+  if (p.pre != nullptr) store_row<W, DT, HW, false>(at_p, v);
+  activate<CLASS, HW>(v, p.act);
+  if (p.residual != nullptr) {
+#pragma unroll
+    for (int e = 0; e < W; e++) v[e] += element<W, DT, HW>(res, e);
+  }
+  if (p.keep)
+    store_row<W, DT, HW, true>(at_c, v);
+  else
+    store_row<W, DT, HW, false>(at_c, v);
+}
+// A single element, the last of a row that are no whole chunk.
+template <int DT, int CLASS, class HW>
+__device__ __forceinline__ void linear_element(const LinearParams& p, int m, int n, float sum)
+{
+  const LinearColumns<1> c = linear_columns<1, HW>(p, n);
+  float v[1] = {sum * (c.scale[0] * row_scale<HW>(p, m)) + c.bias[0]};
+  if (p.pre != nullptr) store_element<DT, HW>(p.pre, (long)m * p.ldp + n, v[0]);
+  activate<CLASS, HW>(v, p.act);
+  if (p.residual != nullptr) v[0] += load_element<DT, HW>(p.residual, (long)m * p.ldr + n);
+  store_element<DT, HW>(p.C, (long)m * p.ldc + n, v[0]);
+}
+
+// A lane's place in a matrix of results, read or written band by band: the address of row `row` (the same for all lanes)
+// and column n0, and the bytes from there to the lane's row and column, less than 2^31.
+struct LanePlace {
+  const char* tile;
+  long pitch;
+  uint32_t lane;
+  __device__ __forceinline__ const char* at(int row) const { return tile + (long)row * pitch + lane; }
+};
+template <int DT>
+__device__ __forceinline__ LanePlace lane_place(const void* base, int ld, int m0, int n0, int row, int col)
+{
+  constexpr int SIZE = DT == 2 ? 4 : 2;
+  return LanePlace{element_at<DT>(base, (long)m0 * ld + n0), (long)ld * SIZE, (uint32_t)row * (uint32_t)ld * SIZE + (uint32_t)col * SIZE};
+}
+
+// What a wave's lanes need for the epilogue of their tile: columns' bias and scale, rows' scales, the residual
+// (16-bit types).  Tiles of up to eight reads fetch all of it ahead of the main loop, so that its latency is not the
+// epilogue's; larger ones, which have no registers for that, fetch the columns' values and a band behind the loop and
+// every other band while the one before it is worked on.  Each band fetched where it is used, the residual cost 2 us a
+// band: a layer of 8192 x 8192 x 4096 on e4m3 302 us, without a residual 259.
+template <class C>
+struct LinearAhead {
+  static constexpr int LPR = C::WN / 8;            // lanes per row when reading a band back
+  static constexpr int RPI = 64 / LPR;             // rows per read
+  static constexpr int NIT = 32 / RPI;
+  static constexpr int TM = C::TM;
+  static constexpr bool EARLY = TM * NIT <= 8;
+  static constexpr int BANDS = EARLY ? TM : 2;
+  static_assert(64 % LPR == 0 && 32 % RPI == 0, "a wave reads whole rows");
   LinearColumns<8> cols;
-  if (p.chunks) cols = linear_columns<8, HW>(p, lane_ok ? n : 0);
-  // this lane's row in read t of band j; its part of the residual there
-  auto row_of = [&](int j, int t) __attribute__((always_inline)) { return m0 + j * 32 + t * RPI + r0; };
-  auto there = [&](int j, int t) __attribute__((always_inline)) {
-    return lane_ok & (t * RPI + r0 < 32) & (row_of(j, t) < p.M);
-  };
-  auto fetch = [&](int j, int t) __attribute__((always_inline)) {
-    RawRow<8> r = {};
-    if (p.residual != nullptr && there(j, t)) r = load_chunk<8, HW>(p.residual, (long)row_of(j, t) * p.ldr + n, p.out_dtype);
-    return r;
-  };
+  float sa[BANDS][NIT];
+  RawRow<8, 0> res[BANDS][NIT];
+
+  static __device__ __forceinline__ int row_of(int m0, int lane, int j, int t) { return m0 + j * 32 + t * RPI + lane / LPR; }
+  // whether read t of band j is part of C for this lane, as a whole chunk
+  static __device__ __forceinline__ bool there(const LinearParams& p, int m0, int n0, int lane, int j, int t)
+  {
+    return (n0 + lane % LPR * 8 + 8 <= p.N) & (row_of(m0, lane, j, t) < p.M);
+  }
+  template <class HW>
+  __device__ __forceinline__ void load_columns(const LinearParams& p, int n0, int lane)
+  {
+    const int n = n0 + lane % LPR * 8;
+    cols = {};
+    if (p.N >= 8) cols = linear_columns<8, HW>(p, n + 8 <= p.N ? n : 0);
+  }
+  template <class HW>
+  __device__ __forceinline__ void load_band(const LinearParams& p, int m0, int n0, int lane, int j)
+  {
+#pragma unroll
+    for (int t = 0; t < NIT; t++) {
+      sa[j % BANDS][t] = 1.0f;
+      res[j % BANDS][t] = {};
+    }
+    if (p.sa != nullptr) {
+#pragma unroll
+      for (int t = 0; t < NIT; t++) {
+        const int m = row_of(m0, lane, j, t);
+        sa[j % BANDS][t] = row_scale<HW>(p, m < p.M ? m : 0);
+      }
+    }
+    if (p.residual != nullptr && p.out_dtype != 2) {
+      const LanePlace r = lane_place<0>(p.residual, p.ldr, m0, n0, lane / LPR, lane % LPR * 8);
+#pragma unroll
+      for (int t = 0; t < NIT; t++)
+        if (there(p, m0, n0, lane, j, t)) res[j % BANDS][t] = load_chunk<8, 0, HW>(r.at(j * 32 + t * RPI));
+    }
+  }
+  template <class HW>
+  __device__ __forceinline__ void load(const LinearParams& p, int m0, int n0, int lane)
+  {
+    if constexpr (EARLY) {
+      load_columns<HW>(p, n0, lane);
+#pragma unroll
+      for (int j = 0; j < BANDS; j++) load_band<HW>(p, m0, n0, lane, j);
+    }
+  }
+  template <class HW>
+  __device__ __forceinline__ void load_late(const LinearParams& p, int m0, int n0, int lane)
+  {
+    if constexpr (!EARLY) {
+      load_columns<HW>(p, n0, lane);
+      load_band<HW>(p, m0, n0, lane, 0);
+    }
+  }
+};
+
+// A wave's tile, rows m0.., columns n0..; `ebase`: the wave's band in LDS.
+template <class C, int DT, class HW>
+__device__ __forceinline__ void linear_bands(const LinearParams& p, LinearAhead<C>& ahead, f32x16 (&acc)[C::TN][C::TM], int m0,
+                                             int n0, uint32_t ebase, int lane)
+{
+  using L = LinearAhead<C>;
+  constexpr int TN = C::TN, TM = C::TM, NIT = L::NIT;
+  constexpr int RS = C::WN * 4 + 16;               // LDS row stride of the band
+  constexpr int PART = L::EARLY ? NIT : 2;         // reads in registers at a time
+  const int r0 = lane / L::LPR, c8 = lane % L::LPR * 8;
+  const LanePlace c_at = lane_place<DT>(p.C, p.ldc, m0, n0, r0, c8), p_at = lane_place<DT>(p.pre, p.ldp, m0, n0, r0, c8);
+  const LanePlace r_at = lane_place<DT>(p.residual, p.ldr, m0, n0, r0, c8);
 #pragma unroll
   for (int j = 0; j < TM; j++) {
-    RawRow<8> res = {};
-    if (p.chunks) res = fetch(j, 0);
+    if (!L::EARLY && j + 1 < TM) ahead.template load_band<HW>(p, m0, n0, lane, j + 1);
     const uint32_t row = ebase + (lane & 31) * RS + 16 * (lane >> 5);
 #pragma unroll
     for (int i = 0; i < TN; i++)
@@ -314,61 +435,116 @@ __device__ __forceinline__ void linear_tile(const P& p, f32x16 (&acc)[C::TN][C::
       for (int vq = 0; vq < 4; vq++)
         HW::lds_write(row + (i * 32 + 8 * vq) * 4, f32x4{acc[i][j][4 * vq], acc[i][j][4 * vq + 1], acc[i][j][4 * vq + 2],
                                                         acc[i][j][4 * vq + 3]});
-    if (p.chunks) {
-#pragma unroll 1
-      for (int t = 0; t < NIT; t++) {
-        const RawRow<8> next = fetch(j, t + 1);
-        const int r = t * RPI + r0;
-        const uint32_t at = ebase + (r < 32 ? r : 0) * RS + lane % LPR * 32;     // every lane takes part in the read
-        const f32x4 lo = __builtin_bit_cast(f32x4, HW::lds_read16(at)), hi = __builtin_bit_cast(f32x4, HW::lds_read16(at + 16));
-        float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        if (there(j, t)) {
-          const int m = row_of(j, t);
-          linear_row<8, HW>(p, cols, m, n, v, row_scale<HW>(p, m), res);
+#pragma unroll
+    for (int t0 = 0; t0 < NIT; t0 += PART) {
+      RawRow<8, DT> res[PART];
+      float v[PART][8];
+#pragma unroll
+      for (int q = 0; q < PART; q++) {
+        const int t = t0 + q;
+        if constexpr (DT == 2) {
+          res[q] = {};
+          if (p.residual != nullptr && L::there(p, m0, n0, lane, j, t)) res[q] = load_chunk<8, DT, HW>(r_at.at(j * 32 + t * L::RPI));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; e++) res[q].w[e] = ahead.res[j % L::BANDS][t].w[e];
         }
-        res = next;
+        const uint32_t at = ebase + (t * L::RPI + r0) * RS + c8 * 4;
+        const f32x4 lo = __builtin_bit_cast(f32x4, HW::lds_read16(at)), hi = __builtin_bit_cast(f32x4, HW::lds_read16(at + 16));
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+          v[q][e] = lo[e];
+          v[q][4 + e] = hi[e];
+        }
       }
-    } else {
-      // rows that are not made of chunks: element by element, lane next to lane
+#pragma unroll
+      for (int q = 0; q < PART; q++) {
+        const int t = t0 + q;
+        if (L::there(p, m0, n0, lane, j, t))
+          linear_row<8, DT, C::CLASS, HW>(p, ahead.cols, c_at.at(j * 32 + t * L::RPI), p_at.at(j * 32 + t * L::RPI), v[q],
+                                          ahead.sa[j % L::BANDS][t], res[q]);
+      }
+    }
+    // columns behind the last whole chunk: at most seven, element by element
+    const int tail = p.N - (p.N & ~7), c0 = (p.N & ~7) - n0;
+    if ((tail > 0) & (c0 >= 0) & (c0 < C::WN)) {
 #pragma unroll 1
-      for (int t = lane; t < 32 * C::WN; t += 64) {
-        const int r = t / C::WN, c = t % C::WN;
-        float v[1] = {__builtin_bit_cast(float, HW::lds_read4(ebase + r * RS + c * 4))};
-        const int m = m0 + j * 32 + r;
-        if ((m < p.M) & (n0 + c < p.N))
-          linear_row<1, HW>(p, linear_columns<1, HW>(p, n0 + c), m, n0 + c, v, row_scale<HW>(p, m), RawRow<1>{});
+      for (int k = lane; k < 32 * 8; k += 64) {
+        const int r = k >> 3, c = k & 7, m = m0 + j * 32 + r;
+        const uint32_t bits = HW::lds_read4(ebase + r * RS + (c0 + c) * 4);
+        if ((c < tail) & (m < p.M)) linear_element<DT, C::CLASS, HW>(p, m, n0 + c0 + c, __builtin_bit_cast(float, bits));
       }
     }
   }
 }
-
-// Four columns of a row, from the kernels whose waves split K.
-template <class HW, class P>
-__device__ __forceinline__ void linear_group(const P& p, int m, int n, const f32x4& sum)
+template <class C, class HW, class P>
+__device__ __forceinline__ void linear_tile(const P& p, typename C::Ahead& ahead, f32x16 (&acc)[C::TN][C::TM], int m0, int n0,
+                                            uint32_t ebase, int lane)
 {
-  if (p.chunks) {
-    if ((m >= p.M) | (n >= p.N)) return;
-    const LinearColumns<4> cols = linear_columns<4, HW>(p, n);
-    RawRow<4> res = {};
-    if (p.residual != nullptr) res = load_chunk<4, HW>(p.residual, (long)m * p.ldr + n, p.out_dtype);
-    float v[4] = {sum[0], sum[1], sum[2], sum[3]};
-    linear_row<4, HW>(p, cols, m, n, v, row_scale<HW>(p, m), res);
-  } else {
+  by_type(p.out_dtype, [&](auto t) __attribute__((always_inline)) {
+    linear_bands<C, decltype(t)::value, HW>(p, ahead, acc, m0, n0, ebase, lane);
+  });
+}
+
+// The same for the kernels whose waves split K, where a thread ends up with groups of four columns of a row (group
+// `turn` NT + thread of the tile).
+template <class C>
+struct LinearGroups {
+  static constexpr int GPR = C::BN / 4, GROUPS = C::BM * GPR, TURNS = (GROUPS + C::NT - 1) / C::NT;
+  LinearColumns<4> cols[TURNS];
+  float sa[TURNS];
+  RawRow<4, 0> res[TURNS];
+  template <class HW>
+  __device__ __forceinline__ void load(const LinearParams& p, int m0, int n0, int thread)
+  {
 #pragma unroll
-    for (int e = 0; e < 4; e++) {
-      float v[1] = {sum[e]};
-      if ((m < p.M) & (n + e < p.N))
-        linear_row<1, HW>(p, linear_columns<1, HW>(p, n + e), m, n + e, v, row_scale<HW>(p, m), RawRow<1>{});
+    for (int i = 0; i < TURNS; i++) {
+      const int g = i * C::NT + thread, m = m0 + g / GPR, n = n0 + g % GPR * 4;
+      cols[i] = {};
+      sa[i] = 1.0f;
+      res[i] = {};
+      if ((g < GROUPS) & (m < p.M) & (n + 4 <= p.N)) {
+        cols[i] = linear_columns<4, HW>(p, n);
+        sa[i] = row_scale<HW>(p, m);
+        if (p.residual != nullptr && p.out_dtype != 2) res[i] = load_chunk<4, 0, HW>(element_at<0>(p.residual, (long)m * p.ldr + n));
+      }
     }
   }
+};
+
+template <class C, class HW, class P>
+__device__ __forceinline__ void linear_group(const P& p, const typename C::Ahead& ahead, int turn, int m, int n, const f32x4& sum)
+{
+  if ((m >= p.M) | (n >= p.N)) return;
+  by_type(p.out_dtype, [&](auto t) __attribute__((always_inline)) {
+    constexpr int DT = decltype(t)::value;
+    if (n + 4 <= p.N) {
+      RawRow<4, DT> res = {};
+      if constexpr (DT == 2) {
+        if (p.residual != nullptr) res = load_chunk<4, DT, HW>(element_at<DT>(p.residual, (long)m * p.ldr + n));
+      } else {
+        res.w[0] = ahead.res[turn].w[0];
+        res.w[1] = ahead.res[turn].w[1];
+      }
+      float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+      linear_row<4, DT, C::CLASS, HW>(p, ahead.cols[turn], element_at<DT>(p.C, (long)m * p.ldc + n),
+                                      element_at<DT>(p.pre, (long)m * p.ldp + n), v, ahead.sa[turn], res);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; e++)
+        if (n + e < p.N) linear_element<DT, C::CLASS, HW>(p, m, n + e, sum[e]);
+    }
+  });
 }
 
 // ---- the kernels -------------------------------------------------------------------------------------------
-// DT: 0 fp16, 1 bf16, 2 pairs of e4m3; BL: 0 W stored K x N, 1 N x K.
-template <int DT, int BM, int BN, int BK, int WM, int WN, int S, int R, int FUSE, int BL>
+// DT: 0 fp16, 1 bf16, 2 pairs of e4m3 widened to bf16, 3 pairs of e4m3 as they are; BL: 0 W stored K x N, 1 N x K.
+template <int CLASS_, int DT, int BM, int BN, int BK, int WM, int WN, int S, int R, int FUSE, int BL>
 struct LCfg : KCfg<DT, BM, BN, BK, WM, WN, S, R, FUSE, BL, 0> {
   static constexpr bool LINEAR = true;
-  static_assert(DT != 2 || BL == 1, "the transposing read moves 16-bit elements");
+  using Ahead = LinearAhead<LCfg>;
+  static constexpr int CLASS = CLASS_;
+  static_assert(DT < 2 || BL == 1, "the transposing read moves 16-bit elements");
 };
 template <class C, class HW>
 __global__ void __launch_bounds__(C::NT) alcop_linear_tile(const LinearArgs a)
@@ -376,9 +552,11 @@ __global__ void __launch_bounds__(C::NT) alcop_linear_tile(const LinearArgs a)
   mainloop_body<C, HW>(expand_linear<C>(a));
 }
 
-template <int DT, int BM, int BN, int NW, int S, int BL>
+template <int CLASS_, int DT, int BM, int BN, int NW, int S, int BL>
 struct LWCfg : WCfg<DT, BM, BN, NW, S, BL, 0> {
   static constexpr bool LINEAR = true;
+  using Ahead = LinearGroups<LWCfg>;
+  static constexpr int CLASS = CLASS_;
   static_assert(DT != 2 || BL == 1, "the transposing read moves 16-bit elements");
 };
 template <class C, class HW>

@@ -42,7 +42,7 @@ struct ActGradArgs {
   void* dz;                    // null: only the sums
   float* partial;              // dbias's sums of the rows of each block, or null
   long lddc, ldp, ldz;
-  int M, N, rows_per_block, act, dt;
+  int M, N, rows_per_block, act;
 };
 
 struct ColumnSumArgs {
@@ -121,19 +121,19 @@ __device__ __forceinline__ int column(int me, int i, int e)
 // The chunks of a row as they lie in memory; columns past the end are 0.
 template <class C>
 struct Raw {
-  RawRow<8> c[C::NV];
+  RawRow<8, C::DT> c[C::NV];
 };
-template <class C, class HW, int DT = C::DT>
+template <class C, class HW>
 __device__ __forceinline__ Raw<C> load_raw(const void* row, int me, int cols)
 {
+  constexpr int DT = C::DT;
   Raw<C> r;
 #pragma unroll
   for (int i = 0; i < C::NV; i++) {
-#pragma unroll
-    for (int e = 0; e < 8; e++) r.c[i].w[e] = 0;
+    r.c[i] = {};
     if constexpr (C::VEC) {
       const int n = column<C, HW>(me, i, 0);
-      if (n < cols) r.c[i] = load_chunk<8, HW>(row, n, DT);
+      if (n < cols) r.c[i] = load_chunk<8, DT, HW>(element_at<DT>(row, n));
     } else {
 #pragma unroll
       for (int e = 0; e < 8; e++) {
@@ -149,37 +149,37 @@ __device__ __forceinline__ Raw<C> load_raw(const void* row, int me, int cols)
   }
   return r;
 }
-template <class C, class HW, int DT = C::DT>
+template <class C, class HW>
 __device__ __forceinline__ float value(const Raw<C>& r, int i, int e)
 {
-  return element<8, HW>(r.c[i], e, DT);
+  return element<8, C::DT, HW>(r.c[i], e);
 }
 
-// v[NV][8] to a row of type dt (0, 1, 2; 3: e4m3)
-template <class C, class HW>
-__device__ __forceinline__ void store_values(void* row, int me, int cols, int dt, const float (&v)[C::NV][8])
+// v[NV][8] to a row of type DT (0, 1, 2; 3: e4m3)
+template <class C, int DT, class HW>
+__device__ __forceinline__ void store_values(void* row, int me, int cols, const float (&v)[C::NV][8])
 {
 #pragma unroll
   for (int i = 0; i < C::NV; i++) {
     if constexpr (C::VEC) {
       const int n = column<C, HW>(me, i, 0);
       if (n >= cols) continue;
-      if (dt == 3) {
+      if constexpr (DT == 3) {
         const uint32_t lo = HW::cvt_e4m3(v[i][0], v[i][1]) | HW::cvt_e4m3(v[i][2], v[i][3]) << 16;
         const uint32_t hi = HW::cvt_e4m3(v[i][4], v[i][5]) | HW::cvt_e4m3(v[i][6], v[i][7]) << 16;
         HW::template global_store<u32x2>((char*)row + n, u32x2{lo, hi});
       } else {
-        store_row<8, HW, false>(row, n, dt, v[i]);
+        store_row<8, DT, HW, false>(element_at<DT>(row, n), v[i]);
       }
     } else {
 #pragma unroll
       for (int e = 0; e < 8; e++) {
         const int n = column<C, HW>(me, i, e);
         if (n >= cols) continue;
-        if (dt == 3)
+        if constexpr (DT == 3)
           HW::global_store_u8((char*)row + n, (uint8_t)HW::cvt_e4m3(v[i][e], v[i][e]));
         else
-          store_element<HW>(row, n, dt, v[i][e]);
+          store_element<DT, HW>(row, n, v[i][e]);
       }
     }
   }
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_rows(const NormArgs p)
       for (int e = 0; e < 8; e++) h[i][e] = value<C, HW>(x, i, e);
   }
   if (p.total != nullptr)
-    store_values<C, HW>((void*)row_at<DT>(p.total, row, p.ldt), me, p.cols, DT, h);
+    store_values<C, DT, HW>((void*)row_at<DT>(p.total, row, p.ldt), me, p.cols, h);
   if (norm) {
     float s = 0.f;
 #pragma unroll
@@ -283,7 +283,11 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_rows(const NormArgs p)
 #pragma unroll
       for (int e = 0; e < 8; e++) h[i][e] *= inv;
   }
-  store_values<C, HW>((char*)p.y + row * p.ldy * (out == 3 ? 1 : out == 2 ? 4 : 2), me, p.cols, out, h);
+  char* y = (char*)p.y + row * p.ldy * (out == 3 ? 1 : out == 2 ? 4 : 2);
+  if (out == 3)
+    store_values<C, 3, HW>(y, me, p.cols, h);
+  else
+    by_type(out, [&](auto t) __attribute__((always_inline)) { store_values<C, decltype(t)::value, HW>(y, me, p.cols, h); });
 }
 
 // ---- gradients of the norm ------------------------------------------------------------------------------------------
@@ -340,10 +344,10 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_grad(const NormGradArgs p, i
 #pragma unroll
         for (int e = 0; e < 8; e++) dx[i][e] += value<C, HW>(dt, i, e);
     }
-    store_values<C, HW>((void*)row_at<DT>(p.dx, row, p.lddx), me, p.cols, DT, dx);
+    store_values<C, DT, HW>((void*)row_at<DT>(p.dx, row, p.lddx), me, p.cols, dx);
   }
   if (p.partial != nullptr && group < groups)
-    store_values<C, HW>(p.partial + (long)group * p.cols, me, p.cols, 2, dg);
+    store_values<C, 2, HW>(p.partial + (long)group * p.cols, me, p.cols, dg);
 }
 
 // ---- column sums ------------------------------------------------------------------------------------------------------
@@ -376,7 +380,7 @@ __global__ void __launch_bounds__(SUM_THREADS) alcop_column_sums(const ColumnSum
 // dZ = dC act'(Z), rounded to the operands' type: it is an operand of the two products that follow, which take
 // 16 bits.  A block has 512 columns and a run of rows, its four waves every fourth row of it; 16-byte chunks.
 constexpr int ACT_COLS = 512;
-template <class HW>
+template <int DT, class HW>
 __global__ void __launch_bounds__(256) alcop_act_grad(const ActGradArgs p)
 {
   const uint32_t lds = HW::lds_base();
@@ -389,16 +393,16 @@ __global__ void __launch_bounds__(256) alcop_act_grad(const ActGradArgs p)
   for (int e = 0; e < 8; e++) sum[e] = 0.f;
   if (n < p.N) {
     for (long m = r0 + wave; m < r1; m += 4) {
-      const RawRow<8> dc = load_chunk<8, HW>(p.dc, m * p.lddc + n, p.dt);
+      const RawRow<8, DT> dc = load_chunk<8, DT, HW>(element_at<DT>(p.dc, m * p.lddc + n));
       float v[8];
 #pragma unroll
-      for (int e = 0; e < 8; e++) v[e] = element<8, HW>(dc, e, p.dt);
+      for (int e = 0; e < 8; e++) v[e] = element<8, DT, HW>(dc, e);
       if (p.act != ACT_NONE) {
-        const RawRow<8> z = load_chunk<8, HW>(p.pre, m * p.ldp + n, p.dt);
+        const RawRow<8, DT> z = load_chunk<8, DT, HW>(element_at<DT>(p.pre, m * p.ldp + n));
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[e] *= slope<HW>(element<8, HW>(z, e, p.dt), p.act);
+        for (int e = 0; e < 8; e++) v[e] *= slope<HW>(element<8, DT, HW>(z, e), p.act);
       }
-      if (p.dz != nullptr) store_row<8, HW, true>(p.dz, m * p.ldz + n, p.dt, v);
+      if (p.dz != nullptr) store_row<8, DT, HW, true>(element_at<DT>(p.dz, m * p.ldz + n), v);
 #pragma unroll
       for (int e = 0; e < 8; e++) sum[e] += v[e];
     }

@@ -46,10 +46,13 @@ hipError_t launch_column_sums(const ColumnSumArgs& a, hipStream_t st)
   return hipGetLastError();
 }
 
-hipError_t launch_act_grad(const ActGradArgs& a, hipStream_t st)
+hipError_t launch_act_grad(const ActGradArgs& a, int dt, hipStream_t st)
 {
   const dim3 grid((unsigned)((a.N + ACT_COLS - 1) / ACT_COLS), (unsigned)((a.M + a.rows_per_block - 1) / a.rows_per_block));
-  alcop_act_grad<Gfx950><<<grid, dim3(256), 4 * ACT_COLS * 4, st>>>(a);
+  if (dt)
+    alcop_act_grad<1, Gfx950><<<grid, dim3(256), 4 * ACT_COLS * 4, st>>>(a);
+  else
+    alcop_act_grad<0, Gfx950><<<grid, dim3(256), 4 * ACT_COLS * 4, st>>>(a);
   return hipGetLastError();
 }
 
@@ -57,7 +60,8 @@ hipError_t prepare_rows()
 {
   hipFuncAttributes at;
   hipError_t rc = hipFuncGetAttributes(&at, (const void*)alcop_column_sums<Gfx950>);
-  if (rc == hipSuccess) rc = hipFuncGetAttributes(&at, (const void*)alcop_act_grad<Gfx950>);
+  if (rc == hipSuccess) rc = hipFuncGetAttributes(&at, (const void*)alcop_act_grad<0, Gfx950>);
+  if (rc == hipSuccess) rc = hipFuncGetAttributes(&at, (const void*)alcop_act_grad<1, Gfx950>);
   for (int dt = 0; dt < 3; dt++)
     for (int vec = 0; vec < 2; vec++)
       for (int cols : {512, 1024, 2048, 4096, 8192, 16384, 32768})

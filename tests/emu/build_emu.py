@@ -39,7 +39,7 @@ def build() -> str:
     for name in ("alcop_api.cpp", "alcop_model.cpp", "alcop_linear.cpp"):
         jobs.append((os.path.join(CSRC, name), os.path.join(OUT, name + ".o"), []))
     lin = os.path.join(HERE, "emu_linear.cpp")
-    jobs += [(lin, os.path.join(OUT, "emu_linear%d.o" % p), ["-DEMU_PART=%d" % p]) for p in range(4)]
+    jobs += [(lin, os.path.join(OUT, "emu_linear%d.o" % p), ["-DEMU_PART=%d" % p]) for p in range(5)]
     with cf.ThreadPoolExecutor(max_workers=8) as ex:
         objs = list(ex.map(_compile, jobs))
     if not os.path.exists(LIB) or any(os.path.getmtime(o) > os.path.getmtime(LIB) for o in objs):

@@ -482,6 +482,11 @@ struct Emu {
     return acc;
   }
 
+  static f32x16 mma64(u32x4 x0, u32x4 x1, u32x4 y0, u32x4 y1, f32x16 acc)
+  {
+    return mma<2>(x1, y1, mma<2>(x0, y0, acc));
+  }
+
   template <int DT>
   static f32x4 mma16(u32x4 x, u32x4 y, f32x4 acc)
   {
@@ -622,7 +627,7 @@ struct Emu {
     else
       fail("global store outside the output: block %u,%u thread %d", blk()->bx, blk()->by, blk()->cur);
   }
-  static void global_store16_through(void* ptr, u32x4 v) { global_store16(ptr, v); }
+  static void global_store16_through(void* ptr, u32x4 v) { global_store16_any(ptr, v); }
   static void global_store16_keep(void* ptr, u32x4 v) { global_store16(ptr, v); }
   template <class V>
   static void global_store(void* ptr, V v)
@@ -654,15 +659,23 @@ struct Emu {
     else
       fail("element store outside the output: block %u,%u thread %d", blk()->bx, blk()->by, blk()->cur);
   }
-  static u32x2 global_load8(const void* ptr)
+  static u32x2 global_load8_any(const void* ptr)
   {
     u32x2 v = {0, 0};
-    if ((uintptr_t)ptr % 8) fail("8-byte global load from an unaligned address (thread %d)", blk()->cur);
+    if ((uintptr_t)ptr % 2) fail("8-byte global load from an odd address (thread %d)", blk()->cur);
     if (in_buffer(ptr, 8, false))
       memcpy(&v, ptr, 8);
     else
       fail("global load outside every operand (thread %d)", blk()->cur);
     return v;
+  }
+  static void global_store8_any(void* ptr, u32x2 v)
+  {
+    if ((uintptr_t)ptr % 2) fail("8-byte store to an odd address (thread %d)", blk()->cur);
+    if (in_buffer(ptr, 8, true))
+      memcpy(ptr, &v, 8);
+    else
+      fail("global store outside the output: block %u,%u thread %d", blk()->bx, blk()->by, blk()->cur);
   }
   static void global_store_u8(void* ptr, uint8_t v) { global_store_elem<uint8_t>(ptr, v); }
   static float f16_bits(uint16_t b) { return f16_to_float(b); }

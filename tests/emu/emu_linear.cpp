@@ -25,18 +25,18 @@ static hipError_t launch_linear(const LinearArgs& a, dim3 grid, hipStream_t)
 }
 static hipError_t prepare_none() { return hipSuccess; }
 
-template <int DT, int BM, int BN, int BK, int WM, int WN, int S, int R, int F, int BL>
+template <int CL, int DT, int BM, int BN, int BK, int WM, int WN, int S, int R, int F, int BL>
 void add_linear(std::vector<LinearKernel>& t)
 {
-  using C = LCfg<DT, BM, BN, BK, WM, WN, S, R, F, BL>;
-  t.push_back(LinearKernel{DT, BL, alcop_sched{BM, BN, BK, WM, WN, S, R, F, 1, 0, 0}, C::NT, C::LDS_BYTES,
+  using C = LCfg<CL, DT, BM, BN, BK, WM, WN, S, R, F, BL>;
+  t.push_back(LinearKernel{CL, DT, BL, alcop_sched{BM, BN, BK, WM, WN, S, R, F, 1, 0, 0}, C::NT, C::LDS_BYTES,
                            &launch_linear<C, &tile_entry<C>>, &prepare_none});
 }
-template <int DT, int BM, int BN, int NW, int BL>
+template <int CL, int DT, int BM, int BN, int NW, int BL>
 void add_linear_ksplit(std::vector<LinearKernel>& t)
 {
-  using C = LWCfg<DT, BM, BN, NW, 2, BL>;
-  t.push_back(LinearKernel{DT, BL, alcop_sched{BM, BN, 64, BM, BN, 2, 1, 0, 1, 0, 3}, C::NT, C::LDS_BYTES,
+  using C = LWCfg<CL, DT, BM, BN, NW, 2, BL>;
+  t.push_back(LinearKernel{CL, DT, BL, alcop_sched{BM, BN, 64, BM, BN, 2, 1, 0, 1, 0, 3}, C::NT, C::LDS_BYTES,
                            &launch_linear<C, &ksplit_entry<C>>, &prepare_none});
 }
 
@@ -56,6 +56,13 @@ void register_linear_bf16(std::vector<LinearKernel>& t)
 void register_linear_e4m3(std::vector<LinearKernel>& t)
 {
   ALCOP_LINEAR_KERNELS(t, 2, 1)
+}
+#elif EMU_PART == 4
+void register_linear_f8(std::vector<LinearKernel>& t)
+{
+  ALCOP_LINEAR_F8(t, CLASS_PLAIN)
+  ALCOP_LINEAR_F8(t, CLASS_SIGMOID)
+  ALCOP_LINEAR_F8(t, CLASS_ERF)
 }
 #elif EMU_PART == 3
 template <class C>
@@ -95,10 +102,14 @@ hipError_t launch_column_sums(const ColumnSumArgs& a, hipStream_t)
   emu::run_grid(&sums_entry, &a, SUM_THREADS, SUM_THREADS * 4, (unsigned)((a.cols + SUM_COLS - 1) / SUM_COLS), 1, 1);
   return hipSuccess;
 }
-static void act_entry(const void* p) { alcop_act_grad<emu::Emu>(*(const ActGradArgs*)p); }
-hipError_t launch_act_grad(const ActGradArgs& a, hipStream_t)
+template <int DT>
+static void act_entry(const void* p)
 {
-  emu::run_grid(&act_entry, &a, 256, 4 * ACT_COLS * 4, (unsigned)((a.N + ACT_COLS - 1) / ACT_COLS),
+  alcop_act_grad<DT, emu::Emu>(*(const ActGradArgs*)p);
+}
+hipError_t launch_act_grad(const ActGradArgs& a, int dt, hipStream_t)
+{
+  emu::run_grid(dt ? &act_entry<1> : &act_entry<0>, &a, 256, 4 * ACT_COLS * 4, (unsigned)((a.N + ACT_COLS - 1) / ACT_COLS),
                 (unsigned)((a.M + a.rows_per_block - 1) / a.rows_per_block), 1);
   return hipSuccess;
 }

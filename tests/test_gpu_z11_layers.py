@@ -11,7 +11,8 @@ from gpu_util import DEV
 from layers_util import DT, HALF, ULP, check, check_e4m3, linear64, norm64, norm_grad64, slope64
 
 pytestmark = pytest.mark.gpu
-KERNELS = 10
+F8_KERNELS = 6          # and on e4m3 operands with a 16-bit result (ALCOP_LINEAR_F8)
+KERNELS = 10            # per operand type, layout and class of activation (ALCOP_LINEAR_CLASS)
 
 
 def matrix(rows, cols, dtype, seed, pad=0, scale=1.0, offset=0):
@@ -41,7 +42,7 @@ def run_linear(M, N, K, dtype, transB, out="bf16", act=0, bias=True, residual=Tr
     r = (C if in_place else matrix(M, N, out, 5, pad, offset=offset)) if residual else None
     z = matrix(M, N, out, 6, pad, offset=offset) if pre else None
     sa, sw = (vector(M, 7, True), vector(N, 8, True)) if scales else (None, None)
-    ref, zref, ez, ec = linear64(A, W, transB, alpha, b, act, r, sa, sw)
+    ref, zref, ez, ec = linear64(A, W, transB, alpha, b, act, r, sa, sw, dtype == "e4m3" and out != "f32")
     al.alcop_linear(A, W, C, transB=transB, alpha=alpha, bias=b, act=act, residual=r, pre=z, scale_a=sa, scale_w=sw)
     torch.cuda.synchronize()
     what = str((M, N, K, dtype, transB, out, act))
@@ -60,6 +61,16 @@ def test_every_kernel_of_a_linear_layer(kernel, dtype, transB, monkeypatch):
     run_linear(300, 408, 208, dtype, transB, out=("f16", "bf16", "f32")[i % 3], act=i % 5, scales=dtype == "e4m3" or i % 2 == 0,
                pad=16)
     run_linear(513, 776, 1040, dtype, transB, out=("f16", "bf16", "f32")[(i + 1) % 3], act=(i + 2) % 5, residual=False)
+
+
+@pytest.mark.parametrize("kernel", range(KERNELS, KERNELS + F8_KERNELS))
+@pytest.mark.parametrize("act", [0, 2, 4])
+def test_every_kernel_that_multiplies_8_bits_as_they_are(kernel, act, monkeypatch):
+    monkeypatch.setenv("ALCOP_LINEAR_KERNEL", str(kernel))
+    run_linear(300, 413, 720, "e4m3", True, out=("f16", "bf16")[kernel % 2], act=act, scales=True, pad=16)
+    run_linear(513, 776, 2064, "e4m3", True, out="bf16", act=act, residual=False)
+    with pytest.raises(al.AlcopError):            # fp32 results get fp32 sums
+        run_linear(8, 16, 16, "e4m3", True, out="f32")
 
 
 @pytest.mark.parametrize("act", range(5))

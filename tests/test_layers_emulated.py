@@ -10,7 +10,8 @@ import emu_util as emu
 import paper_2210_16691_amd as al
 from layers_util import DT, HALF, ULP, check, check_e4m3, linear64, norm64, norm_grad64, slope64
 
-KERNELS = 10            # per operand type and layout (ALCOP_LINEAR_KERNELS)
+F8_KERNELS = 6          # and on e4m3 operands with a 16-bit result (ALCOP_LINEAR_F8)
+KERNELS = 10            # per operand type, layout and class of activation (ALCOP_LINEAR_CLASS)
 
 
 def matrix(rows, cols, dtype, seed, pad=0, scale=1.0, offset=0):
@@ -83,6 +84,16 @@ def test_there_are_no_more_kernels(monkeypatch):
     with pytest.raises(al.AlcopError) as e:
         run_linear(8, 8, 16, "f16", True)
     assert e.value.code == al.ERR_SCHED
+
+
+@pytest.mark.parametrize("kernel", range(KERNELS, KERNELS + F8_KERNELS))
+@pytest.mark.parametrize("act", [0, 2, 4])
+def test_every_kernel_that_multiplies_8_bits_as_they_are(kernel, act, monkeypatch):
+    monkeypatch.setenv("ALCOP_LINEAR_KERNEL", str(kernel))
+    run_linear(140, 200, 272, "e4m3", True, out=("f16", "bf16")[kernel % 2], act=act, scales=True, pad=16)
+    run_linear(20, 43, 16, "e4m3", True, out="bf16", act=act, residual=False)
+    with pytest.raises(al.AlcopError):            # fp32 results get fp32 sums
+        run_linear(8, 16, 16, "e4m3", True, out="f32")
 
 
 @pytest.mark.parametrize("act", range(5))
