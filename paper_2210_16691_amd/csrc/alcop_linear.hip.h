@@ -425,6 +425,9 @@ __device__ __forceinline__ void linear_bands(const LinearParams& p, LinearAhead<
   const int r0 = lane / L::LPR, c8 = lane % L::LPR * 8;
   const LanePlace c_at = lane_place<DT>(p.C, p.ldc, m0, n0, r0, c8), p_at = lane_place<DT>(p.pre, p.ldp, m0, n0, r0, c8);
   const LanePlace r_at = lane_place<DT>(p.residual, p.ldr, m0, n0, r0, c8);
+  const bool tail_here = (p.N & 7) != 0 && (p.N & ~7) >= n0 && (p.N & ~7) < n0 + C::WN;
+  LinearColumns<1> last = {};
+  if (tail_here && (p.N & ~7) + (lane & 7) < p.N) last = linear_columns<1, HW>(p, (p.N & ~7) + (lane & 7));
 #pragma unroll
   for (int j = 0; j < TM; j++) {
     if (!L::EARLY && j + 1 < TM) ahead.template load_band<HW>(p, m0, n0, lane, j + 1);
@@ -465,14 +468,32 @@ __device__ __forceinline__ void linear_bands(const LinearParams& p, LinearAhead<
                                           ahead.sa[j % L::BANDS][t], res[q]);
       }
     }
-    // columns behind the last whole chunk: at most seven, element by element
-    const int tail = p.N - (p.N & ~7), c0 = (p.N & ~7) - n0;
-    if ((tail > 0) & (c0 >= 0) & (c0 < C::WN)) {
-#pragma unroll 1
-      for (int k = lane; k < 32 * 8; k += 64) {
-        const int r = k >> 3, c = k & 7, m = m0 + j * 32 + r;
-        const uint32_t bits = HW::lds_read4(ebase + r * RS + (c0 + c) * 4);
-        if ((c < tail) & (m < p.M)) linear_element<DT, C::CLASS, HW>(p, m, n0 + c0 + c, __builtin_bit_cast(float, bits));
+    // columns behind the last whole chunk, at most seven: eight rows of them at a time, element by element
+    if (tail_here) {
+      const int c = lane & 7, n1 = (p.N & ~7) + c;
+      float r1[4], s1[4];
+      bool in[4];
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
+        const int m = m0 + j * 32 + q * 8 + (lane >> 3);
+        in[q] = (n1 < p.N) & (m < p.M);
+        r1[q] = 0.f;
+        s1[q] = 1.f;
+        if (in[q]) {
+          if (p.residual != nullptr) r1[q] = load_element<DT, HW>(p.residual, (long)m * p.ldr + n1);
+          s1[q] = row_scale<HW>(p, m);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < 4; q++) {
+        const int r = q * 8 + (lane >> 3), m = m0 + j * 32 + r;
+        const uint32_t bits = HW::lds_read4(ebase + r * RS + ((p.N & ~7) - n0 + c) * 4);
+        if (in[q]) {
+          float v[1] = {__builtin_bit_cast(float, bits) * (last.scale[0] * s1[q]) + last.bias[0]};
+          if (p.pre != nullptr) store_element<DT, HW>(p.pre, (long)m * p.ldp + n1, v[0]);
+          activate<C::CLASS, HW>(v, p.act);
+          store_element<DT, HW>(p.C, (long)m * p.ldc + n1, v[0] + r1[q]);
+        }
       }
     }
   }

@@ -232,6 +232,10 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_rows(const NormArgs p)
   const int out = p.flags & 3;
 
   const Raw<C> x = load_raw<C, HW>(row_at<DT>(p.x, row, p.ldx), me, p.cols);
+  // ahead of the sum that it does not depend on, where there are registers for it
+  constexpr bool GAIN_AHEAD = C::TPR < 1024 || NV < 4;
+  float g[NV][8];
+  if (GAIN_AHEAD && norm) load_gain<C, HW>(p.gain, me, p.cols, g);
   float h[NV][8];
   if (p.residual != nullptr) {
     const Raw<C> r = load_raw<C, HW>(row_at<DT>(p.residual, row, p.ldr), me, p.cols);
@@ -255,9 +259,8 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_rows(const NormArgs p)
       for (int e = 0; e < 8; e++) s += h[i][e] * h[i][e];
     s = row_sum<C::TPR, HW>(s, lds);
     const float rstd = 1.0f / HW::sqrt(s / (float)p.cols + p.eps);
+    if (!GAIN_AHEAD) load_gain<C, HW>(p.gain, me, p.cols, g);
     if (p.rstd != nullptr && me == 0) HW::global_store_u32(p.rstd + row, __builtin_bit_cast(uint32_t, rstd));
-    float g[NV][8];
-    load_gain<C, HW>(p.gain, me, p.cols, g);
 #pragma unroll
     for (int i = 0; i < NV; i++)
 #pragma unroll
