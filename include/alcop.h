@@ -432,9 +432,11 @@ int alcop_linear(const void* A, const void* W, void* C, int M, int N, int K, lon
  *     ALCOP_F32; dbias: N fp32 values.  M is free, N and K are multiples of 8, pointers 16-byte aligned
  *     (dbias: 4), pitches multiples of 8.
  *   workspace: DEVICE, 16-byte aligned, at least alcop_linear_backward_workspace_bytes(M, N, K) bytes (which
- *     returns 0 for arguments no call accepts); needed if act != 0 or dbias is given.  Overwritten; calls that share
- *     it, captured ones too, must be ordered on one stream.  Outputs and workspace overlap nothing else.
- * Up to four launches.  dbias is summed in a fixed order, without atomics.
+ *     returns 0 for arguments no call accepts); needed if act != 0 or dbias is given.  With it, dW's sum over few tiles and
+ *     many rows (a multiple of 8) is split over blocks, in fp32 and a fixed order (other bits than without it).
+ *     Overwritten; calls that share it, captured ones too, must be ordered on one stream.  Outputs and workspace overlap
+ *     nothing else.
+ * Up to five launches.  dbias is summed in a fixed order, without atomics.
  */
 size_t alcop_linear_backward_workspace_bytes(int M, int N, int K);
 int alcop_linear_backward(const void* dC, const void* A, const void* W, const void* pre, void* dA, void* dW,
@@ -452,7 +454,7 @@ int alcop_linear_backward(const void* dC, const void* A, const void* W, const vo
  *     scale[i] = max(max_j |y[i][j]| / 448, 2^-126) and e4m3(y / scale), as alcop_linear takes them as A.
  *   A row with an infinity or a NaN gives what the formulas give: its sum is not finite, and an e4m3 row's scale is NaN
  *   if one of its y is.  mean h^2 has to stay below the fp32 range (|h| below 1e19).
- * rows >= 1, 1 <= cols <= 32768, any alignment and pitch >= cols (rows of 16-byte chunks are faster).  total may be x or residual,
+ * rows >= 1, 1 <= cols <= 32768, any alignment and pitch >= cols (rows that start at 16 bytes are faster).  total may be x or residual,
  * y may be x or residual if out = in (same pitch); no other output overlaps anything.  One launch.
  */
 int alcop_rmsnorm(const void* x, const void* residual, const void* gain, void* total, void* y, void* scale,
@@ -466,7 +468,7 @@ int alcop_rmsnorm(const void* x, const void* residual, const void* gain, void* t
  *   dy, total, dtotal, dx: type `in`; gain (may be NULL = 1), rstd, dgain (may be NULL): fp32.  dx may be dy or dtotal.
  *   workspace: DEVICE, 16-byte aligned, at least alcop_rmsnorm_backward_workspace_bytes(rows, cols) bytes, needed
  *     with dgain, as for alcop_linear_backward.
- * Sizes as for alcop_rmsnorm.  One launch, two with dgain, whose sums have a fixed order.
+ * Sizes as for alcop_rmsnorm.  One launch, two with dgain of more than a few rows; its sums have a fixed order.
  */
 size_t alcop_rmsnorm_backward_workspace_bytes(int rows, int cols);
 int alcop_rmsnorm_backward(const void* dy, const void* total, const void* gain, const void* rstd, const void* dtotal,

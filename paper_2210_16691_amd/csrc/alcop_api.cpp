@@ -1222,18 +1222,79 @@ XForm choose_xform(const Call& c, int C, double x_room)
 }
 
 }  // namespace
+namespace {
+// How a weight gradient's sum is split, or 1.  The kernels of few tiles leave compute units idle while each walks a long
+// K; their cost (alcop_dispatch.h) against that of split-K, fitted on 114 gradients (64 to 4096 rows and columns, sums of 512
+// to 16384) for the two kernels below as
+//     us = a + b * turns * k-tiles of a slice + c * turns + d * (partial sums at 5.1 TB/s) + e * (operands at 5.1 TB/s).
+// With the line at 0.85 a quarter of them are split and are 1.39 times faster in the mean (256 x 256 x 16384 43.2 -> 20.6 us,
+// 112 x 2168 x 7224 32.1 -> 20.9, 64 x 1400 x 5856 21.0 -> 15.9), three are slower, the worst 1.37 times; at 1.0 twice as many are.
+int gradient_split(int M, int N, int K, alcop_sched* out)
+{
+  struct Cost {
+    alcop_sched s;
+    double a, b, c, d, e;
+  };
+  static const Cost costs[] = {{{128, 128, 64, 64, 64, 3, 2, 1, 1, 0, 0}, 9.151, 0.285, 1.136, 1.874, 0.777},
+                               {{64, 64, 64, 32, 32, 3, 2, 1, 1, 0, 0}, 9.053, 0.165, 0.227, 1.319, 1.005}};
+  alcop_problem p;
+  std::memset(&p, 0, sizeof(p));
+  p.op = ALCOP_OP_GEMM;
+  p.batch = 1;
+  p.M = M;
+  p.N = N;
+  p.K = K;
+  p.transA = 1;
+  p.in = p.out = ALCOP_BF16;
+  double unsplit = 1e30, best = 1e30;
+  for (const MeasuredCost& m : kMeasured)
+    if (measured_applies(p, m)) unsplit = std::min(unsplit, measured_us(p, m));
+  int split = 1;
+  auto up = [](double x, double y) { return (double)(long)((x + y - 1) / y); };
+  for (const Cost& c : costs)
+    for (int n = 2; n <= 32; n *= 2) {
+      const double kt = up(up(K, 64), n), nz = up(up(K, 64), kt), partial = 4.0 * nz * M * N;
+      if (kt < 2 || partial > (double)(128 << 20)) continue;
+      const double turns = up(up(M, c.s.bm) * up(N, c.s.bn) * nz, 256);
+      const double us = c.a + c.b * turns * kt + c.c * turns + c.d * partial / 5.1e6 + c.e * 2.0 * K * ((double)M + N) / 5.1e6;
+      if (us < best) {
+        best = us;
+        if (us < 0.85 * unsplit) {
+          split = n;
+          *out = c.s;
+        }
+      }
+    }
+  return split;
+}
+}  // namespace
+
+size_t gradient_workspace(int M, int N, int K)
+{
+  alcop_sched s;
+  const int split = K % 8 ? 1 : gradient_split(M, N, K, &s);
+  return split > 1 ? alcop_splitk_workspace_bytes(1, M, N, split) : 0;
+}
+
 // dW of a linear layer: the sum runs over the layer's rows, any number of them.  Both operands run along their
 // m and n there, so that rows past K lie outside the descriptors of every kernel of these layouts and read as zero; the
 // problem is checked, and its kernel picked, with K rounded up to a multiple of 8.
 int gradient_product(const void* A, const void* B, void* C, int M, int N, int K, long lda, long ldb, long ldc,
-                     alcop_dtype in, alcop_dtype out, float alpha, void* stream)
+                     alcop_dtype in, alcop_dtype out, float alpha, void* workspace, size_t workspace_bytes, void* stream)
 {
   if (K > 0x7ffffff8) return ALCOP_ERR_SIZE;
   Call c = gemm_call(ALCOP_OP_GEMM, A, B, C, 1, M, N, (K + 7) & ~7, lda, ldb, ldc, 0, 0, 0, 1, 0, in, out);
   c.alpha = alpha;
   Resolved r;
-  const int rc = resolve(c, nullptr, &r);
+  int rc = resolve(c, nullptr, &r);
   if (rc) return rc;
+  const size_t need = workspace && r.us >= 0.0 ? gradient_workspace(M, N, K) : 0;     // a tuned schedule comes first
+  if (need && workspace_bytes >= need) {
+    alcop_sched s;
+    const int split = gradient_split(M, N, K, &s);
+    rc = run_splitk(c, &s, split, workspace, workspace_bytes, stream);
+    if (rc != ALCOP_ERR_SCHED && rc != ALCOP_ERR_SIZE) return rc;                     // else as one sum
+  }
   c.K = K;
   return launch_call(c, r.s, r.e, (hipStream_t)stream);
 }

@@ -230,6 +230,11 @@ struct Gfx950 {
   {
     __builtin_nontemporal_store(v, (u32x2_any*)ptr);
   }
+  typedef u32x2 u32x2_byte __attribute__((aligned(1)));
+  __device__ static __forceinline__ void global_store8_byte(void* ptr, u32x2 v)
+  {
+    __builtin_nontemporal_store(v, (u32x2_byte*)ptr);
+  }
   __device__ static __forceinline__ void global_store_u8(void* ptr, uint8_t v) { *(uint8_t*)ptr = v; }
   __device__ static __forceinline__ float f16_bits(uint16_t b) { return (float)__builtin_bit_cast(_Float16, b); }
   // two floats -> two e4m3 in the low 16 bits, round to nearest even; magnitudes up to 464 give at most 448, NaN stays

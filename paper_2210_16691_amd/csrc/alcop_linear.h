@@ -24,8 +24,8 @@ void register_linear_bf16(std::vector<LinearKernel>&);
 void register_linear_e4m3(std::vector<LinearKernel>&);
 void register_linear_f8(std::vector<LinearKernel>&);      // in libalcop_f8.so
 
-hipError_t launch_norm_rows(const NormArgs& a, int dt, bool vec, hipStream_t st);
-hipError_t launch_norm_grad(const NormGradArgs& a, int groups, int dt, bool vec, hipStream_t st);
+hipError_t launch_norm_rows(const NormArgs& a, int dt, bool whole, hipStream_t st);
+hipError_t launch_norm_grad(const NormGradArgs& a, int groups, int dt, bool whole, hipStream_t st);
 hipError_t launch_column_sums(const ColumnSumArgs& a, hipStream_t st);
 hipError_t launch_act_grad(const ActGradArgs& a, int dt, hipStream_t st);
 hipError_t prepare_rows();
@@ -33,24 +33,24 @@ hipError_t prepare_rows();
 // Threads that share a row, and their chunks of eight elements: a wave while that takes at most four chunks a lane,
 // then a block of 256 or 1024.
 constexpr int ROWS_MAX_COLS = 32768;
-template <int DT, bool VEC, template <class> class LAUNCH, class... A>
+template <int DT, bool WHOLE, template <class> class LAUNCH, class... A>
 hipError_t dispatch_rows(int cols, const A&... a)
 {
-  if (cols <= 512) return LAUNCH<RowCfg<DT, 64, 1, VEC>>::go(a...);
-  if (cols <= 1024) return LAUNCH<RowCfg<DT, 64, 2, VEC>>::go(a...);
-  if (cols <= 2048) return LAUNCH<RowCfg<DT, 256, 1, VEC>>::go(a...);
-  if (cols <= 4096) return LAUNCH<RowCfg<DT, 256, 2, VEC>>::go(a...);
-  if (cols <= 8192) return LAUNCH<RowCfg<DT, 256, 4, VEC>>::go(a...);
-  if (cols <= 16384) return LAUNCH<RowCfg<DT, 1024, 2, VEC>>::go(a...);
-  return LAUNCH<RowCfg<DT, 1024, 4, VEC>>::go(a...);
+  if (cols <= 512) return LAUNCH<RowCfg<DT, 64, 1, WHOLE>>::go(a...);
+  if (cols <= 1024) return LAUNCH<RowCfg<DT, 64, 2, WHOLE>>::go(a...);
+  if (cols <= 2048) return LAUNCH<RowCfg<DT, 256, 1, WHOLE>>::go(a...);
+  if (cols <= 4096) return LAUNCH<RowCfg<DT, 256, 2, WHOLE>>::go(a...);
+  if (cols <= 8192) return LAUNCH<RowCfg<DT, 256, 4, WHOLE>>::go(a...);
+  if (cols <= 16384) return LAUNCH<RowCfg<DT, 1024, 2, WHOLE>>::go(a...);
+  return LAUNCH<RowCfg<DT, 1024, 4, WHOLE>>::go(a...);
 }
 inline int rows_per_block(int cols) { return cols <= 1024 ? 4 : 1; }
 template <template <class> class LAUNCH, class... A>
-hipError_t dispatch_rows_of(int dt, bool vec, int cols, const A&... a)
+hipError_t dispatch_rows_of(int dt, bool whole, int cols, const A&... a)
 {
-  if (dt == 0) return vec ? dispatch_rows<0, true, LAUNCH>(cols, a...) : dispatch_rows<0, false, LAUNCH>(cols, a...);
-  if (dt == 1) return vec ? dispatch_rows<1, true, LAUNCH>(cols, a...) : dispatch_rows<1, false, LAUNCH>(cols, a...);
-  return vec ? dispatch_rows<2, true, LAUNCH>(cols, a...) : dispatch_rows<2, false, LAUNCH>(cols, a...);
+  if (dt == 0) return whole ? dispatch_rows<0, true, LAUNCH>(cols, a...) : dispatch_rows<0, false, LAUNCH>(cols, a...);
+  if (dt == 1) return whole ? dispatch_rows<1, true, LAUNCH>(cols, a...) : dispatch_rows<1, false, LAUNCH>(cols, a...);
+  return whole ? dispatch_rows<2, true, LAUNCH>(cols, a...) : dispatch_rows<2, false, LAUNCH>(cols, a...);
 }
 
 // What the first calls of these operators would do besides launching.
@@ -58,8 +58,11 @@ hipError_t prepare_layers();
 
 // dW[M,N] = alpha * A^T . B with A stored K x M and B stored K x N, as alcop_gemm computes it, for any K
 // (alcop_api.cpp): rows past K lie outside both descriptors.
+// Its sum is split over blocks where that pays and the workspace (16-byte aligned) has the room that
+// gradient_workspace names.
 int gradient_product(const void* A, const void* B, void* C, int M, int N, int K, long lda, long ldb, long ldc,
-                     alcop_dtype in, alcop_dtype out, float alpha, void* stream);
+                     alcop_dtype in, alcop_dtype out, float alpha, void* workspace, size_t workspace_bytes, void* stream);
+size_t gradient_workspace(int M, int N, int K);
 
 }  // namespace alcop
 

@@ -8,8 +8,9 @@
 // All of them are bound by memory: a row is loaded once, held in registers in fp32 while its sum and its maximum are
 // found, and stored once.  Sums are fp32 in a fixed order; nothing is atomic, so results do not change between runs.
 //
-// A row belongs to TPR threads (a wave, or a whole block), each holding NV chunks of eight elements.  Rows made of
-// 16-byte chunks (VEC) are moved sixteen bytes a load; others element by element, thread next to thread.
+// A row belongs to TPR threads (a wave, or a whole block), each holding NV chunks of eight elements, moved sixteen bytes a load at
+// whatever address they lie (a global access may start at any element).  Where the length is no multiple of eight (!WHOLE)
+// the last chunk goes element by element.
 #pragma once
 #include "alcop_linear.hip.h"
 
@@ -32,7 +33,7 @@ struct NormGradArgs {
   const void *dy, *total, *dtotal;
   const float *gain, *rstd;
   void* dx;
-  float* partial;              // dgain's sums of the rows of each group of threads, or null
+  float* partial;              // dgain's sums of the rows of each block, or null
   long lddy, ldt, lddt, lddx;
   int rows, cols;
 };
@@ -42,7 +43,7 @@ struct ActGradArgs {
   void* dz;                    // null: only the sums
   float* partial;              // dbias's sums of the rows of each block, or null
   long lddc, ldp, ldz;
-  int M, N, rows_per_block, act;
+  int M, N, rows_per_block, act, lanes;
 };
 
 struct ColumnSumArgs {
@@ -104,18 +105,35 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t at)
 }
 
 // ---- a thread's part of a row ----------------------------------------------------------------------------------
-// VEC: chunk i is columns (i TPR + me) 8 ..+7; else its element e is column (8 i + e) TPR + me.
-template <int DT_, int TPR_, int NV_, bool VEC_>
+// Chunk i of a thread is columns (i TPR + me) 8 ..+7.
+template <int DT_, int TPR_, int NV_, bool WHOLE_>
 struct RowCfg {
   static constexpr int DT = DT_, TPR = TPR_, NV = NV_, NT = TPR_ < 256 ? 256 : TPR_;
-  static constexpr bool VEC = VEC_;
+  static constexpr bool WHOLE = WHOLE_;
   static constexpr int ROWS = NT / TPR;            // rows of a block
+  // the norm's gradient: where a wave has a row, the block's waves add their sums for the gain
+  static constexpr int GRAD_LDS_BYTES = ROWS_LDS_BYTES + (ROWS > 1 ? ROWS * NV * 8 * 64 * 4 : 0);
 };
 
-template <class C, class HW>
-__device__ __forceinline__ int column(int me, int i, int e)
+template <class C>
+__device__ __forceinline__ int chunk_at(int me, int i)
 {
-  return C::VEC ? (i * C::TPR + me) * 8 + e : (8 * i + e) * C::TPR + me;
+  return (i * C::TPR + me) * 8;
+}
+// whole(n) for a chunk that the row has all of, part(n, e) for each element of its last one
+template <class C, class F, class G>
+__device__ __forceinline__ void by_chunk(int me, int i, int cols, F&& whole, G&& part)
+{
+  const int n = chunk_at<C>(me, i);
+  if (n + 8 <= cols) {
+    whole(n);
+  } else if constexpr (!C::WHOLE) {
+    if (n < cols) {
+#pragma unroll
+      for (int e = 0; e < 7; e++)
+        if (n + e < cols) part(n, e);
+    }
+  }
 }
 
 // The chunks of a row as they lie in memory; columns past the end are 0.
@@ -131,21 +149,15 @@ __device__ __forceinline__ Raw<C> load_raw(const void* row, int me, int cols)
 #pragma unroll
   for (int i = 0; i < C::NV; i++) {
     r.c[i] = {};
-    if constexpr (C::VEC) {
-      const int n = column<C, HW>(me, i, 0);
-      if (n < cols) r.c[i] = load_chunk<8, DT, HW>(element_at<DT>(row, n));
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; e++) {
-        const int n = column<C, HW>(me, i, e);
-        if (n < cols) {
+    by_chunk<C>(
+        me, i, cols, [&](int n) __attribute__((always_inline)) { r.c[i] = load_chunk<8, DT, HW>(element_at<DT>(row, n)); },
+        [&](int n, int e) __attribute__((always_inline)) {
+          const char* at = element_at<DT>(row, n + e);
           if constexpr (DT == 2)
-            r.c[i].w[e] = HW::global_load_u32((const char*)row + (long)n * 4);
+            r.c[i].w[e] = HW::global_load_u32(at);
           else
-            r.c[i].w[e / 2] |= (uint32_t)HW::global_load_u16((const char*)row + (long)n * 2) << (e & 1 ? 16 : 0);
-        }
-      }
-    }
+            r.c[i].w[e / 2] |= (uint32_t)HW::global_load_u16(at) << (e & 1 ? 16 : 0);
+        });
   }
   return r;
 }
@@ -160,29 +172,24 @@ template <class C, int DT, class HW>
 __device__ __forceinline__ void store_values(void* row, int me, int cols, const float (&v)[C::NV][8])
 {
 #pragma unroll
-  for (int i = 0; i < C::NV; i++) {
-    if constexpr (C::VEC) {
-      const int n = column<C, HW>(me, i, 0);
-      if (n >= cols) continue;
-      if constexpr (DT == 3) {
-        const uint32_t lo = HW::cvt_e4m3(v[i][0], v[i][1]) | HW::cvt_e4m3(v[i][2], v[i][3]) << 16;
-        const uint32_t hi = HW::cvt_e4m3(v[i][4], v[i][5]) | HW::cvt_e4m3(v[i][6], v[i][7]) << 16;
-        HW::template global_store<u32x2>((char*)row + n, u32x2{lo, hi});
-      } else {
-        store_row<8, DT, HW, false>(element_at<DT>(row, n), v[i]);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; e++) {
-        const int n = column<C, HW>(me, i, e);
-        if (n >= cols) continue;
-        if constexpr (DT == 3)
-          HW::global_store_u8((char*)row + n, (uint8_t)HW::cvt_e4m3(v[i][e], v[i][e]));
-        else
-          store_element<DT, HW>(row, n, v[i][e]);
-      }
-    }
-  }
+  for (int i = 0; i < C::NV; i++)
+    by_chunk<C>(
+        me, i, cols,
+        [&](int n) __attribute__((always_inline)) {
+          if constexpr (DT == 3) {
+            const uint32_t lo = HW::cvt_e4m3(v[i][0], v[i][1]) | HW::cvt_e4m3(v[i][2], v[i][3]) << 16;
+            const uint32_t hi = HW::cvt_e4m3(v[i][4], v[i][5]) | HW::cvt_e4m3(v[i][6], v[i][7]) << 16;
+            HW::global_store8_byte((char*)row + n, u32x2{lo, hi});
+          } else {
+            store_row<8, DT, HW, false>(element_at<DT>(row, n), v[i]);
+          }
+        },
+        [&](int n, int e) __attribute__((always_inline)) {
+          if constexpr (DT == 3)
+            HW::global_store_u8((char*)row + n + e, (uint8_t)HW::cvt_e4m3(v[i][e], v[i][e]));
+          else
+            store_element<DT, HW>(row, n + e, v[i][e]);
+        });
 }
 
 template <class C, class HW>
@@ -190,25 +197,17 @@ __device__ __forceinline__ void load_gain(const float* gain, int me, int cols, f
 {
 #pragma unroll
   for (int i = 0; i < C::NV; i++) {
-    const int n = column<C, HW>(me, i, 0);
 #pragma unroll
     for (int e = 0; e < 8; e++) g[i][e] = 1.0f;
     if (gain == nullptr) continue;
-    if constexpr (C::VEC) {
-      if (n >= cols) continue;
+    by_chunk<C>(
+        me, i, cols,
+        [&](int n) __attribute__((always_inline)) {
+          const RawRow<8, 2> t = load_chunk<8, 2, HW>((const char*)(gain + n));
 #pragma unroll
-      for (int q = 0; q < 2; q++) {
-        const f32x4 t = HW::global_load_f32x4(gain + n + 4 * q);
-#pragma unroll
-        for (int e = 0; e < 4; e++) g[i][4 * q + e] = t[e];
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; e++) {
-        const int m = column<C, HW>(me, i, e);
-        if (m < cols) g[i][e] = __builtin_bit_cast(float, HW::global_load_u32(gain + m));
-      }
-    }
+          for (int e = 0; e < 8; e++) g[i][e] = element<8, 2, HW>(t, e);
+        },
+        [&](int n, int e) __attribute__((always_inline)) { g[i][e] = load_element<2, HW>(gain, n + e); });
   }
 }
 
@@ -274,7 +273,7 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_rows(const NormArgs p)
       for (int e = 0; e < 8; e++) {
         const uint32_t b = __builtin_bit_cast(uint32_t, h[i][e]) & 0x7fffffffu;
         // a thread past the row's end holds zeros, which a gain of its own must not turn into NaN
-        if (column<C, HW>(me, i, e) < p.cols) top = b > top ? b : top;
+        if (chunk_at<C>(me, i) + e < p.cols) top = b > top ? b : top;
       }
     top = row_max<C::TPR, HW>(top, lds + 64);
     const float peak = __builtin_bit_cast(float, top) / 448.0f;
@@ -294,8 +293,8 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_rows(const NormArgs p)
 }
 
 // ---- gradients of the norm ------------------------------------------------------------------------------------------
-// A group of TPR threads takes rows g, g + groups, ... and keeps the sums of dgain for its columns in registers;
-// alcop_column_sums adds the groups'.
+// A group of TPR threads takes rows g, g + groups, ... and keeps the sums of dgain for its columns in registers; the waves of a
+// block add theirs where each has a row, alcop_column_sums adds the blocks'.
 template <class C, class HW>
 __global__ void __launch_bounds__(C::NT) alcop_norm_grad(const NormGradArgs p, int groups)
 {
@@ -349,8 +348,26 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_grad(const NormGradArgs p, i
     }
     store_values<C, DT, HW>((void*)row_at<DT>(p.dx, row, p.lddx), me, p.cols, dx);
   }
-  if (p.partial != nullptr && group < groups)
-    store_values<C, 2, HW>(p.partial + (long)group * p.cols, me, p.cols, dg);
+  if (p.partial == nullptr) return;
+  if constexpr (C::ROWS > 1) {
+    const uint32_t at = lds + ROWS_LDS_BYTES + (uint32_t)me * 4;
+    const int wave = HW::wave_id();
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++)
+        HW::lds_write1(at + (uint32_t)((wave * NV + i) * 8 + e) * 256, __builtin_bit_cast(uint32_t, dg[i][e]));
+    HW::wait_lds();
+    HW::block_barrier();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 1; w < C::ROWS; w++)
+#pragma unroll
+      for (int i = 0; i < NV; i++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) dg[i][e] += __builtin_bit_cast(float, HW::lds_read4(at + (uint32_t)((w * NV + i) * 8 + e) * 256));
+  }
+  store_values<C, 2, HW>(p.partial + (long)HW::block_x() * p.cols, me, p.cols, dg);
 }
 
 // ---- column sums ------------------------------------------------------------------------------------------------------
@@ -365,7 +382,7 @@ __global__ void __launch_bounds__(SUM_THREADS) alcop_column_sums(const ColumnSum
   const int j = (int)HW::block_x() * SUM_COLS + c;
   float s = 0.f;
   if (j < p.cols) {
-#pragma unroll 4
+#pragma unroll 8
     for (int i = run; i < p.count; i += SUM_THREADS / SUM_COLS)
       s += __builtin_bit_cast(float, HW::global_load_u32(p.partial + (long)i * p.cols + j));
   }
@@ -381,21 +398,23 @@ __global__ void __launch_bounds__(SUM_THREADS) alcop_column_sums(const ColumnSum
 
 // ---- gradient of an activation, sums for the bias ----------------------------------------------------------------------
 // dZ = dC act'(Z), rounded to the operands' type: it is an operand of the two products that follow, which take
-// 16 bits.  A block has 512 columns and a run of rows, its four waves every fourth row of it; 16-byte chunks.
+// 16 bits.  A block has 512 columns (or all, where there are fewer) and a run of rows; of 64 lanes `p.lanes` share a row,
+// so that a wave has 64 / lanes rows at a time; 16-byte chunks.
 constexpr int ACT_COLS = 512;
 template <int DT, class HW>
 __global__ void __launch_bounds__(256) alcop_act_grad(const ActGradArgs p)
 {
   const uint32_t lds = HW::lds_base();
-  const int lane = HW::lane_id(), wave = HW::wave_id();
-  const int n = (int)HW::block_x() * ACT_COLS + lane * 8;
+  const int tid = HW::wave_id() * 64 + HW::lane_id();
+  const int mine = tid & (p.lanes - 1), rows = 256 / p.lanes;     // lanes: a power of two
+  const int n = (int)HW::block_x() * ACT_COLS + mine * 8;
   const long r0 = (long)HW::block_y() * p.rows_per_block;
   const long r1 = r0 + p.rows_per_block < p.M ? r0 + p.rows_per_block : p.M;
   float sum[8];
 #pragma unroll
   for (int e = 0; e < 8; e++) sum[e] = 0.f;
   if (n < p.N) {
-    for (long m = r0 + wave; m < r1; m += 4) {
+    for (long m = r0 + tid / p.lanes; m < r1; m += rows) {
       const RawRow<8, DT> dc = load_chunk<8, DT, HW>(element_at<DT>(p.dc, m * p.lddc + n));
       float v[8];
 #pragma unroll
@@ -411,23 +430,20 @@ __global__ void __launch_bounds__(256) alcop_act_grad(const ActGradArgs p)
     }
   }
   if (p.partial == nullptr) return;
-  const uint32_t mine = lds + (uint32_t)(wave * ACT_COLS + lane * 8) * 4;
-  HW::lds_write(mine, f32x4{sum[0], sum[1], sum[2], sum[3]});
-  HW::lds_write(mine + 16, f32x4{sum[4], sum[5], sum[6], sum[7]});
+  // sums of the block's `rows` groups of lanes: [group][8 lanes columns], 2048 values; then column by column
+  HW::lds_write(lds + (uint32_t)tid * 32, f32x4{sum[0], sum[1], sum[2], sum[3]});
+  HW::lds_write(lds + (uint32_t)tid * 32 + 16, f32x4{sum[4], sum[5], sum[6], sum[7]});
   HW::wait_lds();
   HW::block_barrier();
-  const int at = (wave * 64 + lane) * 2, j = (int)HW::block_x() * ACT_COLS + at;
-  float t[2] = {0.f, 0.f};
-#pragma unroll
-  for (int w = 0; w < 4; w++) {
-    const u32x2 s = HW::lds_read8(lds + (uint32_t)(w * ACT_COLS + at) * 4);
-    const uint32_t a = s[0], b = s[1];
-    t[0] += __builtin_bit_cast(float, a);
-    t[1] += __builtin_bit_cast(float, b);
+  const int width = p.lanes * 8;
+#pragma unroll 1
+  for (int c0 = 0; c0 < width; c0 += 256) {
+    const int c = c0 + tid, j = (int)HW::block_x() * ACT_COLS + c;
+    float t = 0.f;
+#pragma unroll 4
+    for (int g = 0; g < rows; g++) t += __builtin_bit_cast(float, HW::lds_read4(lds + (uint32_t)(g * width + (c < width ? c : 0)) * 4));
+    if (c < width && j < p.N) HW::global_store_u32(p.partial + (long)HW::block_y() * p.N + j, __builtin_bit_cast(uint32_t, t));
   }
-  if (j < p.N)                                    // N is a multiple of 8
-    HW::template global_store<u32x2>(p.partial + (long)HW::block_y() * p.N + j,
-                                     u32x2{__builtin_bit_cast(uint32_t, t[0]), __builtin_bit_cast(uint32_t, t[1])});
 }
 
 }  // namespace alcop

@@ -15,7 +15,7 @@ template <class C>
 struct NormGrad {
   static hipError_t go(const NormGradArgs& a, int groups, hipStream_t st)
   {
-    alcop_norm_grad<C, Gfx950><<<dim3((unsigned)(groups / C::ROWS)), dim3(C::NT), ROWS_LDS_BYTES, st>>>(a, groups);
+    alcop_norm_grad<C, Gfx950><<<dim3((unsigned)(groups / C::ROWS)), dim3(C::NT), C::GRAD_LDS_BYTES, st>>>(a, groups);
     return hipGetLastError();
   }
 };
@@ -30,14 +30,14 @@ struct Load {
 };
 }  // namespace
 
-hipError_t launch_norm_rows(const NormArgs& a, int dt, bool vec, hipStream_t st)
+hipError_t launch_norm_rows(const NormArgs& a, int dt, bool whole, hipStream_t st)
 {
-  return dispatch_rows_of<Norm>(dt, vec, a.cols, a, st);
+  return dispatch_rows_of<Norm>(dt, whole, a.cols, a, st);
 }
 
-hipError_t launch_norm_grad(const NormGradArgs& a, int groups, int dt, bool vec, hipStream_t st)
+hipError_t launch_norm_grad(const NormGradArgs& a, int groups, int dt, bool whole, hipStream_t st)
 {
-  return dispatch_rows_of<NormGrad>(dt, vec, a.cols, a, groups, st);
+  return dispatch_rows_of<NormGrad>(dt, whole, a.cols, a, groups, st);
 }
 
 hipError_t launch_column_sums(const ColumnSumArgs& a, hipStream_t st)
@@ -63,9 +63,9 @@ hipError_t prepare_rows()
   if (rc == hipSuccess) rc = hipFuncGetAttributes(&at, (const void*)alcop_act_grad<0, Gfx950>);
   if (rc == hipSuccess) rc = hipFuncGetAttributes(&at, (const void*)alcop_act_grad<1, Gfx950>);
   for (int dt = 0; dt < 3; dt++)
-    for (int vec = 0; vec < 2; vec++)
+    for (int whole = 0; whole < 2; whole++)
       for (int cols : {512, 1024, 2048, 4096, 8192, 16384, 32768})
-        if (rc == hipSuccess) rc = dispatch_rows_of<Load>(dt, vec, cols);
+        if (rc == hipSuccess) rc = dispatch_rows_of<Load>(dt, whole, cols);
   return rc;
 }
 

@@ -677,6 +677,13 @@ struct Emu {
     else
       fail("global store outside the output: block %u,%u thread %d", blk()->bx, blk()->by, blk()->cur);
   }
+  static void global_store8_byte(void* ptr, u32x2 v)
+  {
+    if (in_buffer(ptr, 8, true))
+      memcpy(ptr, &v, 8);
+    else
+      fail("global store outside the output: block %u,%u thread %d", blk()->bx, blk()->by, blk()->cur);
+  }
   static void global_store_u8(void* ptr, uint8_t v) { global_store_elem<uint8_t>(ptr, v); }
   static float f16_bits(uint16_t b) { return f16_to_float(b); }
   static uint32_t cvt_e4m3(float a, float b) { return (uint32_t)float_to_e4m3(a) | (uint32_t)float_to_e4m3(b) << 8; }

@@ -84,17 +84,17 @@ struct NormGrad {
   static hipError_t go(const NormGradArgs& a, int groups, hipStream_t)
   {
     const Both b{a, groups};
-    emu::run_grid(&entry, &b, C::NT, ROWS_LDS_BYTES, (unsigned)(groups / C::ROWS), 1, 1);
+    emu::run_grid(&entry, &b, C::NT, C::GRAD_LDS_BYTES, (unsigned)(groups / C::ROWS), 1, 1);
     return hipSuccess;
   }
 };
-hipError_t launch_norm_rows(const NormArgs& a, int dt, bool vec, hipStream_t st)
+hipError_t launch_norm_rows(const NormArgs& a, int dt, bool whole, hipStream_t st)
 {
-  return dispatch_rows_of<Norm>(dt, vec, a.cols, a, st);
+  return dispatch_rows_of<Norm>(dt, whole, a.cols, a, st);
 }
-hipError_t launch_norm_grad(const NormGradArgs& a, int groups, int dt, bool vec, hipStream_t st)
+hipError_t launch_norm_grad(const NormGradArgs& a, int groups, int dt, bool whole, hipStream_t st)
 {
-  return dispatch_rows_of<NormGrad>(dt, vec, a.cols, a, groups, st);
+  return dispatch_rows_of<NormGrad>(dt, whole, a.cols, a, groups, st);
 }
 static void sums_entry(const void* p) { alcop_column_sums<emu::Emu>(*(const ColumnSumArgs*)p); }
 hipError_t launch_column_sums(const ColumnSumArgs& a, hipStream_t)

@@ -159,6 +159,28 @@ def test_gradients_of_any_number_of_rows(M):
     run_backward(M, 1032, 648, "bf16", False, 0, out="f32")
 
 
+@pytest.mark.parametrize("M,N,K,transB,act", [(5856, 64, 1400, True, 2), (5857, 64, 1400, True, 2), (8192, 256, 264, False, 0),
+                                              (16384, 256, 256, True, 4), (7224, 112, 2168, False, 3)])
+def test_gradients_of_small_weights_and_many_rows(M, N, K, transB, act):
+    # dW's sum is split over blocks if the rows are a multiple of 8; the bias's gradient has few lanes to a row
+    run_backward(M, N, K, "bf16", transB, act)
+
+
+def test_a_split_sum_needs_the_workspace():
+    M, N, K = 8192, 256, 264
+    dC, A, W = matrix(M, N, "f16", 1), matrix(M, K, "f16", 2), matrix(N, K, "f16", 3)
+    dW = [torch.empty(N, K, device=DEV) for _ in range(4)]
+    size = al.alcop_linear_backward_workspace_bytes(M, N, K)
+    ws = torch.full((size,), 255, dtype=torch.uint8, device=DEV)
+    for t, w in zip(dW, (None, ws[: size // 2], ws, ws)):
+        al.alcop_linear_backward(dC, A, W, dW=t, transB=True, workspace=w)
+    assert torch.equal(dW[0], dW[1]) and torch.equal(dW[2], dW[3])
+    ref = dC.cpu().double().t() @ A.cpu().double()
+    mag = dC.cpu().double().abs().t() @ A.cpu().double().abs()
+    for t in dW:
+        check(t, ref, (M + 64) * ULP * mag, "dW")
+
+
 def test_gradients_agree_with_differences():
     # the loss sum(C * G) along a direction of A, of W and of the bias: central differences of the forward pass in
     # fp32 results; the step's error is its square times the third derivative, below 1 % here, rounding of 16-bit
