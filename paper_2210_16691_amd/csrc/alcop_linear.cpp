@@ -11,20 +11,27 @@
 namespace alcop {
 namespace {
 
-const std::vector<LinearKernel>& linear_kernels()
-{
-  static const std::vector<LinearKernel> table = [] {
-    std::vector<LinearKernel> t;
-    register_linear_f16(t);
-    register_linear_bf16(t);
-    register_linear_e4m3(t);
-    register_linear_f8(t);
-    for (LinearKernel& k : t)
+// All kernels, and those of one class of activation, operand type (of a call: e4m3 as 2) and layout.
+struct LinearTable {
+  std::vector<LinearKernel> all;
+  std::vector<const LinearKernel*> of[3][3][2];
+  LinearTable()
+  {
+    register_linear_f16(all);
+    register_linear_bf16(all);
+    register_linear_e4m3(all);
+    register_linear_f8(all);
+    for (LinearKernel& k : all) {
       for (const LinearCost& m : kLinearCost)
         if (m.dt == (k.dt == 0 ? 1 : k.dt) && m.bl == k.bl && std::memcmp(&m.s, &k.s, sizeof(k.s)) == 0) k.cost = &m;
-    return t;
-  }();
-  return table;
+      of[k.cls][std::min(k.dt, 2)][k.bl].push_back(&k);
+    }
+  }
+};
+const LinearTable& linear_table()
+{
+  static const LinearTable t;
+  return t;
 }
 
 int size_of(alcop_dtype t) { return t == ALCOP_F32 ? 4 : t == ALCOP_E4M3 ? 1 : 2; }
@@ -61,8 +68,9 @@ const LinearKernel* pick(int cls, int dt, int bl, bool fine, int M, int N, int K
   double best_us = 0;
   const char* env = std::getenv("ALCOP_LINEAR_KERNEL");       // a tuning and test knob: its number among those of the layout
   int nr = 0;
-  for (const LinearKernel& k : linear_kernels()) {
-    if (k.cls != cls || k.bl != bl || !(k.dt == dt || (dt == 2 && k.dt == 3 && !fine))) continue;
+  for (const LinearKernel* e : linear_table().of[cls][dt][bl]) {
+    const LinearKernel& k = *e;
+    if (k.dt == 3 && fine) continue;
     if (env && *env) {
       if (nr++ == std::atoi(env)) return &k;
       continue;
@@ -111,7 +119,7 @@ size_t backward_sums(int M, int N) { return r256(2.0 * M * N); }
 
 hipError_t prepare_layers()
 {
-  for (const LinearKernel& k : linear_kernels()) {
+  for (const LinearKernel& k : linear_table().all) {
     const hipError_t rc = k.prepare();
     if (rc != hipSuccess) return rc;
   }

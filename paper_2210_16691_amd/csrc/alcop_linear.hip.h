@@ -117,9 +117,10 @@ template <int CLASS, class HW, int W>
 __device__ __forceinline__ void activate(float (&v)[W], int act)
 {
   if constexpr (CLASS == CLASS_PLAIN) {
-    const float floor = act == ACT_RELU ? 0.f : -__builtin_inff();
+    if (act == ACT_RELU) {
 #pragma unroll
-    for (int e = 0; e < W; e++) v[e] = v[e] < floor ? 0.f : v[e];
+      for (int e = 0; e < W; e++) v[e] = v[e] < 0.f ? 0.f : v[e];
+    }
   } else if constexpr (CLASS == CLASS_ERF) {
 #pragma unroll
     for (int e = 0; e < W; e++) {
@@ -301,8 +302,14 @@ template <int W, int DT, int CLASS, class HW>
 __device__ __forceinline__ void linear_row(const LinearParams& p, const LinearColumns<W>& c, const char* at_c, const char* at_p,
                                            float (&v)[W], float sa, const RawRow<W, DT>& res)
 {
+  // branches that all lanes take alike: an epilogue's vector instructions are not covered by anything
+  if (p.sa != nullptr) {
 #pragma unroll
-  for (int e = 0; e < W; e++) v[e] = v[e] * (c.scale[e] * sa) + c.bias[e];
+    for (int e = 0; e < W; e++) v[e] = v[e] * (c.scale[e] * sa) + c.bias[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < W; e++) v[e] = v[e] * c.scale[e] + c.bias[e];
+  }
   if (p.pre != nullptr) store_row<W, DT, HW, false>(at_p, v);
   activate<CLASS, HW>(v, p.act);
   if (p.residual != nullptr) {
@@ -354,6 +361,7 @@ struct LinearAhead {
   static constexpr int TM = C::TM;
   static constexpr bool EARLY = TM * NIT <= 8;
   static constexpr int BANDS = EARLY ? TM : 2;
+  static constexpr int TOUCH = 2;                  // k-tiles from the end at which the residual's lines are asked for
   static_assert(64 % LPR == 0 && 32 % RPI == 0, "a wave reads whole rows");
   LinearColumns<8> cols;
   float sa[BANDS][NIT];
@@ -401,6 +409,19 @@ struct LinearAhead {
       load_columns<HW>(p, n0, lane);
 #pragma unroll
       for (int j = 0; j < BANDS; j++) load_band<HW>(p, m0, n0, lane, j);
+    }
+  }
+  // The residual's lines of this wave's tile into L2: a 4-byte load of each to a landing pad nobody reads.
+  template <class HW>
+  __device__ __forceinline__ void touch(const LinearParams& p, int m0, int n0, int lane, uint32_t pad)
+  {
+    if constexpr (!EARLY && C::WN == 64) {
+      if (p.residual == nullptr || p.out_dtype == 2 || n0 + C::WN > p.N || (((uint32_t)(uintptr_t)p.residual >> 1 | p.ldr) & 1)) return;
+#pragma unroll
+      for (int i = 0; i < C::WM / 64; i++) {
+        const int m = m0 + i * 64 + lane;
+        HW::touch4(element_at<0>(p.residual, (long)(m < p.M ? m : p.M - 1) * p.ldr + n0), pad);
+      }
     }
   }
   template <class HW>
@@ -565,6 +586,11 @@ struct LCfg : KCfg<DT, BM, BN, BK, WM, WN, S, R, FUSE, BL, 0> {
   static constexpr bool LINEAR = true;
   using Ahead = LinearAhead<LCfg>;
   static constexpr int CLASS = CLASS_;
+  using Base = KCfg<DT, BM, BN, BK, WM, WN, S, R, FUSE, BL, 0>;
+  // with the landing pads of LinearAhead::touch, where it is used
+  static constexpr int TOUCH_END = Base::TM * WN / 16 <= 8 ? 0 : Base::RING_BYTES + Base::NWAVES * 256;
+  static constexpr int LDS_BYTES = Base::LDS_BYTES > TOUCH_END ? Base::LDS_BYTES : TOUCH_END;
+  static_assert(LDS_BYTES <= 160 * 1024, "LDS");
   static_assert(DT < 2 || BL == 1, "the transposing read moves 16-bit elements");
 };
 template <class C, class HW>
