@@ -224,6 +224,11 @@ struct Gfx950 {
   }
 
   // ---- operations of the epilogue of linear layers and of the row kernels ---------------------------------
+  // of data that is read once: the line is the first to be evicted
+  __device__ static __forceinline__ u32x4 global_load16_once(const void* ptr)
+  {
+    return __builtin_nontemporal_load((const u32x4_any*)ptr);
+  }
   typedef u32x2 u32x2_any __attribute__((aligned(2)));
   __device__ static __forceinline__ u32x2 global_load8_any(const void* ptr) { return *(const u32x2_any*)ptr; }
   __device__ static __forceinline__ void global_store8_any(void* ptr, u32x2 v)

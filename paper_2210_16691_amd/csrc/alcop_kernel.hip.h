@@ -1040,12 +1040,6 @@ __device__ __forceinline__ void mainloop_body(const P& p)
     load_frags(0, fa[0], fb[0]);
     int rslot = 0, wslot = S - 1;
     for (int ko = 0; ko < nko; ko++) {
-      if constexpr (C::LINEAR) {
-        // what the epilogue reads comes into L2 during the last k-tiles (the waits below then wait for these
-        // loads too)
-        if (ko + C::Ahead::TOUCH == nko)
-          ahead.template touch<HW>(p, tm * BM + wm * WM, tn * BN + wn * WN, lane, lds0 + C::RING_BYTES + (uint32_t)wave * 256u);
-      }
       stage_begin(ko + S - 1, wslot);
       wslot = (wslot + 1 == S) ? 0 : wslot + 1;
 #pragma unroll

@@ -176,7 +176,8 @@ template <int W, int DT>
 struct RawRow {
   uint32_t w[DT == 2 ? W : W / 2];
 };
-template <int W, int DT, class HW>
+// ONCE: the caches need not keep the lines
+template <int W, int DT, class HW, bool ONCE = false>
 __device__ __forceinline__ RawRow<W, DT> load_chunk(const char* ptr)
 {
   constexpr int WORDS = DT == 2 ? W : W / 2;
@@ -184,7 +185,7 @@ __device__ __forceinline__ RawRow<W, DT> load_chunk(const char* ptr)
   if constexpr (WORDS % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < WORDS / 4; i++) {
-      const u32x4 t = HW::global_load16_any(ptr + 16 * i);
+      const u32x4 t = ONCE ? HW::global_load16_once(ptr + 16 * i) : HW::global_load16_any(ptr + 16 * i);
 #pragma unroll
       for (int e = 0; e < 4; e++) r.w[4 * i + e] = t[e];
     }
@@ -351,8 +352,10 @@ __device__ __forceinline__ LanePlace lane_place(const void* base, int ld, int m0
 // What a wave's lanes need for the epilogue of their tile: columns' bias and scale, rows' scales, the residual
 // (16-bit types).  Tiles of up to eight reads fetch all of it ahead of the main loop, so that its latency is not the
 // epilogue's; larger ones, which have no registers for that, fetch the columns' values and a band behind the loop and
-// every other band while the one before it is worked on.  Each band fetched where it is used, the residual cost 2 us a
-// band: a layer of 8192 x 8192 x 4096 on e4m3 302 us, without a residual 259.
+// every other band while the one before it is worked on.
+//   The residual is fetched past the caches (ONCE): 8192 x 8192 x 4096 on e4m3, operands fresh from memory, takes 263 us so,
+// 298 with ordinary loads, 251 without a residual; its 134 MB evict the panels of A and W that other compute units are about
+// to read again.  Bringing its lines into L2 during the last k-tiles is no faster than ordinary loads.
 template <class C>
 struct LinearAhead {
   static constexpr int LPR = C::WN / 8;            // lanes per row when reading a band back
@@ -361,7 +364,6 @@ struct LinearAhead {
   static constexpr int TM = C::TM;
   static constexpr bool EARLY = TM * NIT <= 8;
   static constexpr int BANDS = EARLY ? TM : 2;
-  static constexpr int TOUCH = 2;                  // k-tiles from the end at which the residual's lines are asked for
   static_assert(64 % LPR == 0 && 32 % RPI == 0, "a wave reads whole rows");
   LinearColumns<8> cols;
   float sa[BANDS][NIT];
@@ -399,7 +401,7 @@ struct LinearAhead {
       const LanePlace r = lane_place<0>(p.residual, p.ldr, m0, n0, lane / LPR, lane % LPR * 8);
 #pragma unroll
       for (int t = 0; t < NIT; t++)
-        if (there(p, m0, n0, lane, j, t)) res[j % BANDS][t] = load_chunk<8, 0, HW>(r.at(j * 32 + t * RPI));
+        if (there(p, m0, n0, lane, j, t)) res[j % BANDS][t] = load_chunk<8, 0, HW, true>(r.at(j * 32 + t * RPI));
     }
   }
   template <class HW>
@@ -409,19 +411,6 @@ struct LinearAhead {
       load_columns<HW>(p, n0, lane);
 #pragma unroll
       for (int j = 0; j < BANDS; j++) load_band<HW>(p, m0, n0, lane, j);
-    }
-  }
-  // The residual's lines of this wave's tile into L2: a 4-byte load of each to a landing pad nobody reads.
-  template <class HW>
-  __device__ __forceinline__ void touch(const LinearParams& p, int m0, int n0, int lane, uint32_t pad)
-  {
-    if constexpr (!EARLY && C::WN == 64) {
-      if (p.residual == nullptr || p.out_dtype == 2 || n0 + C::WN > p.N || (((uint32_t)(uintptr_t)p.residual >> 1 | p.ldr) & 1)) return;
-#pragma unroll
-      for (int i = 0; i < C::WM / 64; i++) {
-        const int m = m0 + i * 64 + lane;
-        HW::touch4(element_at<0>(p.residual, (long)(m < p.M ? m : p.M - 1) * p.ldr + n0), pad);
-      }
     }
   }
   template <class HW>
@@ -468,7 +457,7 @@ __device__ __forceinline__ void linear_bands(const LinearParams& p, LinearAhead<
         const int t = t0 + q;
         if constexpr (DT == 2) {
           res[q] = {};
-          if (p.residual != nullptr && L::there(p, m0, n0, lane, j, t)) res[q] = load_chunk<8, DT, HW>(r_at.at(j * 32 + t * L::RPI));
+          if (p.residual != nullptr && L::there(p, m0, n0, lane, j, t)) res[q] = load_chunk<8, DT, HW, true>(r_at.at(j * 32 + t * L::RPI));
         } else {
 #pragma unroll
           for (int e = 0; e < 4; e++) res[q].w[e] = ahead.res[j % L::BANDS][t].w[e];
@@ -586,11 +575,6 @@ struct LCfg : KCfg<DT, BM, BN, BK, WM, WN, S, R, FUSE, BL, 0> {
   static constexpr bool LINEAR = true;
   using Ahead = LinearAhead<LCfg>;
   static constexpr int CLASS = CLASS_;
-  using Base = KCfg<DT, BM, BN, BK, WM, WN, S, R, FUSE, BL, 0>;
-  // with the landing pads of LinearAhead::touch, where it is used
-  static constexpr int TOUCH_END = Base::TM * WN / 16 <= 8 ? 0 : Base::RING_BYTES + Base::NWAVES * 256;
-  static constexpr int LDS_BYTES = Base::LDS_BYTES > TOUCH_END ? Base::LDS_BYTES : TOUCH_END;
-  static_assert(LDS_BYTES <= 160 * 1024, "LDS");
   static_assert(DT < 2 || BL == 1, "the transposing read moves 16-bit elements");
 };
 template <class C, class HW>

@@ -659,6 +659,7 @@ struct Emu {
     else
       fail("element store outside the output: block %u,%u thread %d", blk()->bx, blk()->by, blk()->cur);
   }
+  static u32x4 global_load16_once(const void* ptr) { return global_load16_any(ptr); }
   static u32x2 global_load8_any(const void* ptr)
   {
     u32x2 v = {0, 0};
