@@ -454,7 +454,7 @@ int alcop_linear_backward(const void* dC, const void* A, const void* W, const vo
  *     scale[i] = max(max_j |y[i][j]| / 448, 2^-126) and e4m3(y / scale), as alcop_linear takes them as A.
  *   A row with an infinity or a NaN gives what the formulas give: its sum is not finite, and an e4m3 row's scale is NaN
  *   if one of its y is.  mean h^2 has to stay below the fp32 range (|h| below 1e19).
- * rows >= 1, 1 <= cols <= 32768, any alignment and pitch >= cols (rows that start at 16 bytes are faster).  total may be x or residual,
+ * 1 <= rows < 2^22 (2^24 up to 1024 columns), 1 <= cols <= 32768, any alignment and pitch >= cols (rows that start at 16 bytes are faster).  total may be x or residual,
  * y may be x or residual if out = in (same pitch); no other output overlaps anything.  One launch.
  */
 int alcop_rmsnorm(const void* x, const void* residual, const void* gain, void* total, void* y, void* scale,

@@ -442,6 +442,8 @@ def _pitch(t):
 
 def _call_on(t, what, fn, *args, stream=None):
     """Calls fn(*args, stream) on t's device; without a stream on that device's current one."""
+    if not t.is_cuda and lib() is _marshal_lib:
+        raise ValueError("%s takes tensors on a GPU" % what)
     if t.is_cuda:
         import torch
         with torch.cuda.device(t.device):

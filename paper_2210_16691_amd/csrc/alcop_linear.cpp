@@ -101,15 +101,15 @@ int act_grad_rows(int M, int N)
 {
   const int strips = (N + ACT_COLS - 1) / ACT_COLS, at_once = 256 / act_grad_lanes(N);
   const int want = std::max(1, std::min(256, 2048 / strips));
-  return std::max(at_once, (M + want - 1) / want);
+  return std::max(at_once, (int)(((long)M + want - 1) / want));
 }
 
 // Blocks that walk the rows of a norm's gradient, each leaving a row of sums for dgain.  A single block writes dgain
 // itself: a second turn of it takes 1.8 us, a second launch 2.8.
 int norm_blocks(int rows, int cols)
 {
-  const int blocks = (rows + rows_per_block(cols) - 1) / rows_per_block(cols);
-  return blocks <= 2 ? 1 : std::min(blocks, 1024);
+  const long blocks = ((long)rows + rows_per_block(rows, cols) - 1) / rows_per_block(rows, cols);
+  return blocks <= 2 ? 1 : (int)std::min(blocks, 1024L);
 }
 
 // The workspace of a layer's gradients: dZ, the bias's partial sums from here on, dW's behind them.
@@ -152,6 +152,7 @@ int alcop_linear(const void* A, const void* W, void* C, int M, int N, int K, lon
   if (!aligned(t.bias, 16) || !aligned(t.scale_w, 16) || !aligned(t.scale_a, 4)) return ALCOP_ERR_ALIGN;
   const long far = 1L << 30;
   if (lda >= far || ldw >= far || ldc >= far || t.ldr >= far || t.ldp >= far) return ALCOP_ERR_SIZE;
+  if (std::max(M, N) > 0x7ffff000) return ALCOP_ERR_SIZE;     // rows and columns rounded up to tiles
 
   const int K16 = in == ALCOP_E4M3 ? K / 2 : K;              // in units of 16 bits
   const double c_bytes = (double)osz * M * N;
@@ -166,7 +167,7 @@ int alcop_linear(const void* A, const void* W, void* C, int M, int N, int K, lon
     return ALCOP_ERR_SIZE;
   if (osz * rows * (double)std::max(ldc, std::max(t.residual ? t.ldr : 0, t.pre ? t.ldp : 0)) >= 2147483648.0) return ALCOP_ERR_SIZE;
   const long ntm = ((long)M + k->s.bm - 1) / k->s.bm, ntn = ((long)N + k->s.bn - 1) / k->s.bn;
-  if (ntm * ntn > 0x7fffffffL) return ALCOP_ERR_SHAPE;
+  if (ntm * ntn >= (1L << 32) / k->threads) return ALCOP_ERR_SHAPE;      // threads of a launch are counted in 32 bits
 
   const Span c(C, M, N, ldc, osz), r(t.residual, M, N, t.ldr, osz), z(t.pre, M, N, t.ldp, osz);
   const Span read[] = {Span(A, M, K, lda, esz), Span(W, transB ? N : K, transB ? K : N, ldw, esz), Span(t.bias, 1, N, N, 4),
@@ -224,6 +225,7 @@ int alcop_linear_backward(const void* dC, const void* A, const void* W, const vo
   if (act && !pre) return ALCOP_ERR_NULL;
   if ((act || dbias) && !workspace) return ALCOP_ERR_NULL;
   if (M <= 0 || N <= 0 || K <= 0 || N % 8 || K % 8) return ALCOP_ERR_SHAPE;
+  if (std::max(M, std::max(N, K)) > 0x7ffff000) return ALCOP_ERR_SIZE;
   const int w_rows = transB ? N : K, w_cols = transB ? K : N;
   if (lddc < N || (dW && lda < K) || (dA && ldw < w_cols) || (act && ldp < N) || (dA && ldda < K) || (dW && lddw < w_cols))
     return ALCOP_ERR_SHAPE;
@@ -258,7 +260,7 @@ int alcop_linear_backward(const void* dC, const void* A, const void* W, const vo
     ActGradArgs g;
     std::memset(&g, 0, sizeof(g));
     g.rows_per_block = act_grad_rows(M, N);
-    const int blocks = (M + g.rows_per_block - 1) / g.rows_per_block;
+    const int blocks = (int)(((long)M + g.rows_per_block - 1) / g.rows_per_block);
     g.dc = dC;
     g.pre = act ? pre : nullptr;
     g.M = M;
@@ -306,6 +308,7 @@ static int norm_rows(const void* x, const void* residual, const void* gain, void
   if (rows <= 0 || cols <= 0) return ALCOP_ERR_SHAPE;
   if (ldx < cols || ldy < cols || (residual && ldr < cols) || (total && ldt < cols)) return ALCOP_ERR_SHAPE;
   if (cols > ROWS_MAX_COLS) return ALCOP_ERR_SIZE;
+  if (rows / rows_per_block(rows, cols) >= (1 << 22) - 1) return ALCOP_ERR_SIZE;    // threads of a launch: 32 bits, 1024 a block
   const int isz = size_of(in), osz = size_of(out);
   if (!aligned(x, isz) || !aligned(residual, isz) || !aligned(total, isz) || !aligned(y, osz) || !aligned(gain, 4) ||
       !aligned(scale, 4) || !aligned(rstd, 4))
@@ -406,7 +409,7 @@ int alcop_rmsnorm_backward(const void* dy, const void* total, const void* gain, 
   const int blocks = norm_blocks(rows, cols);
   if (dgain && blocks == 1) a.partial = (float*)dgain;
   hipStream_t st = (hipStream_t)hip_stream;
-  if (launch_norm_grad(a, blocks * rows_per_block(cols), (int)in, cols % 8 == 0, st) != hipSuccess) return ALCOP_ERR_LAUNCH;
+  if (launch_norm_grad(a, blocks * rows_per_block(rows, cols), (int)in, cols % 8 == 0, st) != hipSuccess) return ALCOP_ERR_LAUNCH;
   if (dgain && blocks > 1) {
     const ColumnSumArgs s{(const float*)workspace, (float*)dgain, blocks, cols};
     if (launch_column_sums(s, st) != hipSuccess) return ALCOP_ERR_LAUNCH;

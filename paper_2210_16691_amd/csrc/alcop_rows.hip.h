@@ -310,14 +310,20 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_grad(const NormGradArgs p, i
   for (int i = 0; i < NV; i++)
 #pragma unroll
     for (int e = 0; e < 8; e++) dg[i][e] = 0.f;
+  constexpr bool GAIN_HELD = NV <= 2 && C::TPR < 1024;      // as far as the registers go
+  float g[NV][8];
+  if (GAIN_HELD) load_gain<C, HW>(p.gain, me, p.cols, g);
   int turn = 0;
   for (long row = group; row < p.rows; row += groups, turn ^= 1) {
     const char *dy_row = row_at<DT>(p.dy, row, p.lddy), *h_row = row_at<DT>(p.total, row, p.ldt);
     Raw<C> dy = load_raw<C, HW>(dy_row, me, p.cols);
     Raw<C> h = load_raw<C, HW>(h_row, me, p.cols);
+    const char* dt_row = row_at<DT>(p.dtotal, row, p.lddt);
+    Raw<C> dt = {};
+    constexpr bool AHEAD = NV * C::TPR <= 1024;    // of the sum, where there are registers for it
+    if (AHEAD && p.dtotal != nullptr) dt = load_raw<C, HW>(dt_row, me, p.cols);
     const float rstd = __builtin_bit_cast(float, HW::global_load_u32(p.rstd + row));
-    float g[NV][8];
-    load_gain<C, HW>(p.gain, me, p.cols, g);
+    if (!GAIN_HELD) load_gain<C, HW>(p.gain, me, p.cols, g);
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; i++)
@@ -340,7 +346,7 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_grad(const NormGradArgs p, i
       for (int e = 0; e < 8; e++)
         dx[i][e] = rstd * (value<C, HW>(dy, i, e) * g[i][e] - value<C, HW>(h, i, e) * rstd * mean);
     if (p.dtotal != nullptr) {
-      const Raw<C> dt = load_raw<C, HW>(row_at<DT>(p.dtotal, row, p.lddt), me, p.cols);
+      if (!AHEAD) dt = load_raw<C, HW>(dt_row, me, p.cols);
 #pragma unroll
       for (int i = 0; i < NV; i++)
 #pragma unroll

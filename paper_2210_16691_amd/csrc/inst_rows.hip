@@ -32,12 +32,12 @@ struct Load {
 
 hipError_t launch_norm_rows(const NormArgs& a, int dt, bool whole, hipStream_t st)
 {
-  return dispatch_rows_of<Norm>(dt, whole, a.cols, a, st);
+  return dispatch_rows_of<Norm>(dt, whole, a.rows, a.cols, a, st);
 }
 
 hipError_t launch_norm_grad(const NormGradArgs& a, int groups, int dt, bool whole, hipStream_t st)
 {
-  return dispatch_rows_of<NormGrad>(dt, whole, a.cols, a, groups, st);
+  return dispatch_rows_of<NormGrad>(dt, whole, a.rows, a.cols, a, groups, st);
 }
 
 hipError_t launch_column_sums(const ColumnSumArgs& a, hipStream_t st)
@@ -65,7 +65,7 @@ hipError_t prepare_rows()
   for (int dt = 0; dt < 3; dt++)
     for (int whole = 0; whole < 2; whole++)
       for (int cols : {512, 1024, 2048, 4096, 8192, 16384, 32768})
-        if (rc == hipSuccess) rc = dispatch_rows_of<Load>(dt, whole, cols);
+        if (rc == hipSuccess) rc = dispatch_rows_of<Load>(dt, whole, 1, cols);
   return rc;
 }
 

@@ -90,11 +90,11 @@ struct NormGrad {
 };
 hipError_t launch_norm_rows(const NormArgs& a, int dt, bool whole, hipStream_t st)
 {
-  return dispatch_rows_of<Norm>(dt, whole, a.cols, a, st);
+  return dispatch_rows_of<Norm>(dt, whole, a.rows, a.cols, a, st);
 }
 hipError_t launch_norm_grad(const NormGradArgs& a, int groups, int dt, bool whole, hipStream_t st)
 {
-  return dispatch_rows_of<NormGrad>(dt, whole, a.cols, a, groups, st);
+  return dispatch_rows_of<NormGrad>(dt, whole, a.rows, a.cols, a, groups, st);
 }
 static void sums_entry(const void* p) { alcop_column_sums<emu::Emu>(*(const ColumnSumArgs*)p); }
 hipError_t launch_column_sums(const ColumnSumArgs& a, hipStream_t)

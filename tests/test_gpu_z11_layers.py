@@ -247,6 +247,39 @@ def test_norm_of_every_row_length(cols):
         assert padding(y).float().isnan().all()
 
 
+@pytest.mark.parametrize("cols", [7, 200, 1027, 5000])
+def test_a_gain_and_sums_that_start_anywhere(cols):
+    x, dy = matrix(9, cols, "bf16", 1), matrix(9, cols, "bf16", 2)
+    for start in (1, 3):
+        g, dg = vector(cols + 4, 3)[start:start + cols], vector(cols + 4, 4)
+        y, d = matrix(9, cols, "f32", 5), vector(9, 6)
+        al.alcop_rmsnorm(x, g, y, rstd=d)
+        yref, href, dref = norm64(x, None, g)
+        check(y, yref, (cols / 2 + 8) * ULP * yref.abs(), "y")
+        ws = torch.empty(al.alcop_rmsnorm_backward_workspace_bytes(9, cols), dtype=torch.uint8, device=DEV)
+        before, dx = dg.clone(), matrix(9, cols, "bf16", 7)
+        al.alcop_rmsnorm_backward(dy, x, g, d, dx, dgain=dg[start:start + cols], workspace=ws)
+        ref, gref, edx, edg = norm_grad64(dy, x, g, d)
+        check(dx, ref, edx, "dx")
+        check(dg[None, start:start + cols], gref[None], edg[None], "dgain")
+        assert torch.equal(dg[:start], before[:start]) and torch.equal(dg[start + cols:], before[start + cols:])
+
+
+def test_layers_on_two_streams_at_once():
+    jobs = []
+    for k, (M, N, K) in enumerate(((300, 520, 1040), (16, 2048, 2048))):
+        jobs.append((matrix(M, K, "bf16", 2 * k), matrix(N, K, "bf16", 2 * k + 1), torch.empty(M, N, device=DEV),
+                     torch.empty(M, N, device=DEV), torch.cuda.Stream()))
+    for A, W, C, D, s in jobs:
+        al.alcop_linear(A, W, D, transB=True, act=2)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for A, W, C, D, s in jobs:
+            al.alcop_linear(A, W, C, transB=True, act=2, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(C, D) for _, _, C, D, _ in jobs)
+
+
 def test_e4m3_of_every_kind_of_value():
     # all numbers of 8 bits, the halfway values between them, and the row's own largest at 448: as torch rounds them
     codes = torch.arange(0x7f, dtype=torch.int32).to(torch.uint8).view(torch.float8_e4m3fn).float()
@@ -296,7 +329,7 @@ def test_norm_gradient_of_every_row_length(cols):
             check(dg[None], gref[None], edg[None], "dgain")
 
 
-@pytest.mark.parametrize("rows,cols", [(5000, 72), (3001, 1000), (2500, 1027), (2100, 4096)])
+@pytest.mark.parametrize("rows,cols", [(5000, 72), (3001, 1000), (2500, 1027), (1536, 2048), (1535, 2048), (2001, 1603), (2100, 4096)])
 def test_norm_gradient_of_many_rows(rows, cols):
     dy, h, g = matrix(rows, cols, "bf16", 1), matrix(rows, cols, "bf16", 2), vector(cols, 3)
     rstd = (h.double().square().mean(1) + 1e-6).rsqrt().float()

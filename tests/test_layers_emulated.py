@@ -241,6 +241,14 @@ def test_norm_of_every_type(dtype, out, offset):
     run_norm(5, 72, dtype, out, pad=8, offset=offset)
 
 
+def test_rows_that_have_a_wave_each():
+    # 1537 to 2048 columns are a block's row, but a wave's from 1536 rows on
+    for rows, cols in ((1537, 1040), (1536, 1601)):
+        x, y, s = matrix(rows, cols, "bf16", 1, 8), matrix(rows, cols, "e4m3", 2), vector(rows, 3)
+        assert not emu.call(al.alcop_quantize_rows, x, y, s, reads=[x], writes=[y, s])
+        check_e4m3(y, s, x.double(), 0.0)
+
+
 def test_norm_in_place():
     for dtype in ("bf16", "f32"):
         x, r, g = matrix(5, 40, dtype, 1), matrix(5, 40, dtype, 2), vector(40, 3)

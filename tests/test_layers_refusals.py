@@ -31,6 +31,7 @@ def linear(A=P[0], W=P[1], C=P[2], M=64, N=64, K=64, lda=64, ldw=64, ldc=64, tra
     (dict(A=EIGHT), al.ERR_ALIGN), (dict(W=EIGHT), al.ERR_ALIGN), (dict(lda=68), al.ERR_ALIGN), (dict(ldw=68), al.ERR_ALIGN),
     (dict(i=al.E4M3, lda=72), al.ERR_ALIGN), (dict(C=ODD), al.ERR_ALIGN), (dict(residual=ODD), al.ERR_ALIGN),
     (dict(pre=ODD), al.ERR_ALIGN), (dict(bias=EIGHT), al.ERR_ALIGN), (dict(sw=EIGHT), al.ERR_ALIGN), (dict(sa=ODD), al.ERR_ALIGN),
+    (dict(M=0x7fffffff), al.ERR_SIZE), (dict(N=0x7fffffff, ldc=0x3fffffff), al.ERR_SHAPE),
     (dict(lda=1 << 30), al.ERR_SIZE), (dict(ldc=1 << 30), al.ERR_SIZE), (dict(ldr=1 << 30, residual=P[3]), al.ERR_SIZE),
     (dict(M=256, N=256, lda=1 << 26, ldc=256), al.ERR_SIZE), (dict(transB=0, K=4096, lda=4096, ldw=1 << 20), al.ERR_SIZE),
     # what is written overlaps what is read, or what else is written
@@ -79,6 +80,7 @@ def norm(x=P[0], r=P[1], g=P[2], h=P[3], y=P[4], s=P[5], d=P[6], rows=8, cols=64
     (dict(i=al.E4M3), al.ERR_DTYPE), (dict(o=4), al.ERR_DTYPE), (dict(rows=0), al.ERR_SHAPE), (dict(cols=0), al.ERR_SHAPE),
     (dict(ldx=63), al.ERR_SHAPE), (dict(ldr=63), al.ERR_SHAPE), (dict(ldt=63), al.ERR_SHAPE), (dict(ldy=63), al.ERR_SHAPE),
     (dict(cols=32769, ldx=40000, ldr=40000, ldt=40000, ldy=40000), al.ERR_SIZE),
+    (dict(rows=1 << 25), al.ERR_SIZE), (dict(rows=1 << 23, cols=4096, ldx=4096, ldr=4096, ldt=4096, ldy=4096), al.ERR_SIZE),
     (dict(x=ODD), al.ERR_ALIGN), (dict(r=ODD), al.ERR_ALIGN), (dict(h=ODD), al.ERR_ALIGN), (dict(y=ODD), al.ERR_ALIGN),
     (dict(g=ODD), al.ERR_ALIGN), (dict(d=ODD), al.ERR_ALIGN), (dict(s=ODD, o=al.E4M3), al.ERR_ALIGN),
     (dict(y=P[3]), al.ERR_UNSUPPORTED), (dict(y=P[2]), al.ERR_UNSUPPORTED), (dict(h=P[2]), al.ERR_UNSUPPORTED),
@@ -140,6 +142,16 @@ h = torch.float16
 def test_what_the_binding_says(args, kw, says):
     with pytest.raises(ValueError, match=says):
         al.alcop_linear(*args, **kw)
+
+
+def test_tensors_in_host_memory_are_refused():
+    x, w, s8 = torch.zeros(4, 8, dtype=h), torch.zeros(8, 16, dtype=h), torch.zeros(4, 8, dtype=torch.float8_e4m3fn)
+    for fn, args in ((al.alcop_linear, (x, w, torch.zeros(4, 16, dtype=h))), (al.alcop_rmsnorm, (x, None, x.clone())),
+                     (al.alcop_quantize_rows, (x, s8, torch.zeros(4))),
+                     (al.alcop_rmsnorm_backward, (x, x.clone(), None, torch.zeros(4), x.clone())),
+                     (al.alcop_linear_backward, (torch.zeros(4, 16, dtype=h), x, w, x.clone()))):
+        with pytest.raises(ValueError, match="on a GPU"):
+            fn(*args)
 
 
 def test_what_the_binding_says_of_rows():
