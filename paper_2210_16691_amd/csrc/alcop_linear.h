@@ -76,6 +76,7 @@ size_t gradient_workspace(int M, int N, int K);
   add_linear_ksplit<CL, DT, 16, 32, 8, BL>(T);                 \
   add_linear_ksplit<CL, DT, 32, 32, 8, BL>(T);                 \
   add_linear_ksplit<CL, DT, 32, 64, 4, BL>(T);                 \
+  add_linear_ksplit<CL, DT, 64, 64, 4, BL>(T);                 \
   add_linear<CL, DT, 64, 64, 64, 32, 32, 3, 2, 1, BL>(T);      \
   add_linear<CL, DT, 128, 64, 64, 64, 32, 3, 2, 1, BL>(T);     \
   add_linear<CL, DT, 128, 128, 64, 64, 64, 2, 2, 1, BL>(T);    \

@@ -12,7 +12,7 @@ from layers_util import DT, HALF, ULP, check, check_e4m3, linear64, norm64, norm
 
 pytestmark = pytest.mark.gpu
 F8_KERNELS = 6          # and on e4m3 operands with a 16-bit result (ALCOP_LINEAR_F8)
-KERNELS = 10            # per operand type, layout and class of activation (ALCOP_LINEAR_CLASS)
+KERNELS = 11            # per operand type, layout and class of activation (ALCOP_LINEAR_CLASS)
 
 
 def matrix(rows, cols, dtype, seed, pad=0, scale=1.0, offset=0):

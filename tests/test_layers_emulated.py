@@ -11,7 +11,7 @@ import paper_2210_16691_amd as al
 from layers_util import DT, HALF, ULP, check, check_e4m3, linear64, norm64, norm_grad64, slope64
 
 F8_KERNELS = 6          # and on e4m3 operands with a 16-bit result (ALCOP_LINEAR_F8)
-KERNELS = 10            # per operand type, layout and class of activation (ALCOP_LINEAR_CLASS)
+KERNELS = 11            # per operand type, layout and class of activation (ALCOP_LINEAR_CLASS)
 
 
 def matrix(rows, cols, dtype, seed, pad=0, scale=1.0, offset=0):
@@ -74,7 +74,7 @@ def test_every_kernel_of_a_linear_layer(kernel, dtype, transB, monkeypatch):
     monkeypatch.setenv("ALCOP_LINEAR_KERNEL", str(kernel))
     i = kernel + 10 * transB + 20 * (dtype == "bf16")
     # two tiles of rows at most, a last tile that is not full in either direction, a partial last k-tile
-    M, N, K = (37, 72, 144) if kernel < 5 else (140, 200, 80)
+    M, N, K = (37, 72, 144) if kernel < 4 else (140, 200, 80)
     run_linear(M, N, K, dtype, transB, out=("f16", "bf16", "f32")[i % 3], act=i % 5, scales=dtype == "e4m3" or i % 2 == 0, pad=16,
                policy=emu.POLICIES[i % 4])
 
