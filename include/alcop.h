@@ -436,6 +436,8 @@ int alcop_linear(const void* A, const void* W, void* C, int M, int N, int K, lon
  *     many rows (a multiple of 8) is split over blocks, in fp32 and a fixed order (other bits than without it).
  *     Overwritten; calls that share it, captured ones too, must be ordered on one stream.  Outputs and workspace overlap
  *     nothing else.
+ * dA and dW are subject to alcop_gemm's sizes: for dW, A and dZ (dC without an activation), their rows counted up to 128, span
+ * less than 2 GiB each, for dA with transB = 1 W does; else ALCOP_ERR_SIZE, before anything is launched.
  * Up to five launches.  dbias is summed in a fixed order, without atomics.
  */
 size_t alcop_linear_backward_workspace_bytes(int M, int N, int K);
@@ -454,8 +456,9 @@ int alcop_linear_backward(const void* dC, const void* A, const void* W, const vo
  *     scale[i] = max(max_j |y[i][j]| / 448, 2^-126) and e4m3(y / scale), as alcop_linear takes them as A.
  *   A row with an infinity or a NaN gives what the formulas give: its sum is not finite, and an e4m3 row's scale is NaN
  *   if one of its y is.  mean h^2 has to stay below the fp32 range (|h| below 1e19).
- * 1 <= rows < 2^22 (2^24 up to 1024 columns), 1 <= cols <= 32768, any alignment and pitch >= cols (rows that start at 16 bytes are faster).  total may be x or residual,
- * y may be x or residual if out = in (same pitch); no other output overlaps anything.  One launch.
+ * 1 <= rows < 2^22 (2^24 up to 1024 columns), 1 <= cols <= 32768, any alignment and pitch >= cols (rows that start at 16
+ * bytes are faster).  total may be x or residual, y may be x or residual if out = in (same pitch); no other output
+ * overlaps anything.  One launch.
  */
 int alcop_rmsnorm(const void* x, const void* residual, const void* gain, void* total, void* y, void* scale,
                   void* rstd, int rows, int cols, long ldx, long ldr, long ldt, long ldy, float eps, alcop_dtype in,

@@ -1276,6 +1276,14 @@ size_t gradient_workspace(int M, int N, int K)
   return split > 1 ? alcop_splitk_workspace_bytes(1, M, N, split) : 0;
 }
 
+int product_check(const void* A, const void* B, const void* C, int M, int N, int K, long lda, long ldb, long ldc, int transA,
+                  int transB, alcop_dtype in, alcop_dtype out)
+{
+  Resolved r;
+  return resolve(gemm_call(ALCOP_OP_GEMM, A, B, const_cast<void*>(C), 1, M, N, K, lda, ldb, ldc, 0, 0, 0, transA, transB, in, out),
+                 nullptr, &r);
+}
+
 // dW of a linear layer: the sum runs over the layer's rows, any number of them.  Both operands run along their
 // m and n there, so that rows past K lie outside the descriptors of every kernel of these layouts and read as zero; the
 // problem is checked, and its kernel picked, with K rounded up to a multiple of 8.

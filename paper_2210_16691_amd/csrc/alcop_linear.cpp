@@ -253,9 +253,22 @@ int alcop_linear_backward(const void* dC, const void* A, const void* W, const vo
       if (meet(o, outs[j])) return ALCOP_ERR_UNSUPPORTED;
   }
 
+  const bool own_dz = act && (dA || dW);
+  const void* dZ = own_dz ? workspace : dC;
+  const long lddz = own_dz ? N : lddc;
+  // a product that refuses its operands does so before anything is launched
+  if (dA) {
+    const int rc = product_check(dZ, W, dA, M, K, N, lddz, ldw, ldda, 0, transB ? 0 : 1, in, out);
+    if (rc) return rc;
+  }
+  if (dW) {
+    const int Mr = (M + 7) & ~7;                   // as gradient_product rounds it; M is below 2^31 - 4096
+    const int rc = transB ? product_check(dZ, A, dW, N, K, Mr, lddz, lda, lddw, 1, 0, in, out)
+                          : product_check(A, dZ, dW, K, N, Mr, lda, lddz, lddw, 1, 0, in, out);
+    if (rc) return rc;
+  }
+
   hipStream_t st = (hipStream_t)hip_stream;
-  const void* dZ = dC;
-  long lddz = lddc;
   if (act || dbias) {
     ActGradArgs g;
     std::memset(&g, 0, sizeof(g));
@@ -269,9 +282,9 @@ int alcop_linear_backward(const void* dC, const void* A, const void* W, const vo
     g.ldp = ldp;
     g.act = act;
     g.lanes = act_grad_lanes(N);
-    if (act && (dA || dW)) {
-      dZ = g.dz = workspace;
-      lddz = g.ldz = N;
+    if (own_dz) {
+      g.dz = workspace;
+      g.ldz = N;
     }
     float* sums = (float*)((char*)workspace + backward_sums(M, N));
     if (dbias) g.partial = blocks == 1 ? (float*)dbias : sums;

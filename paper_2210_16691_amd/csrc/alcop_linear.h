@@ -67,6 +67,9 @@ hipError_t prepare_layers();
 int gradient_product(const void* A, const void* B, void* C, int M, int N, int K, long lda, long ldb, long ldc,
                      alcop_dtype in, alcop_dtype out, float alpha, void* workspace, size_t workspace_bytes, void* stream);
 size_t gradient_workspace(int M, int N, int K);
+// What alcop_gemm would answer, without a launch.
+int product_check(const void* A, const void* B, const void* C, int M, int N, int K, long lda, long ldb, long ldc, int transA,
+                  int transB, alcop_dtype in, alcop_dtype out);
 
 }  // namespace alcop
 

@@ -70,6 +70,20 @@ def test_gradients_that_are_refused(kw, rc):
     assert backward(**kw) == rc
 
 
+@pytest.mark.parametrize("kw", [
+    # 2^20 rows of 1024 columns are the last that fit: the last row starts 2 KiB below 2^31
+    dict(M=(1 << 20) + 8, K=1024, lda=1024, ldda=1024, ldw=1024, lddw=1024, dA=None),          # dW: A spans more than 2 GiB
+    dict(M=(1 << 20) + 8, N=1024, lddc=1024, ldp=1024, dA=None),                               # dW: dZ does
+    dict(N=(1 << 20) + 8, K=1024, lddc=1 << 21, ldp=1 << 21, lda=1024, ldda=1024, ldw=1024, lddw=1024, dW=None),   # dA: W does
+])
+@pytest.mark.parametrize("db", [None, P[6]])
+def test_gradients_whose_products_are_refused_launch_nothing(kw, db):
+    # far apart, so that no two overlap; without a GPU a launch would be ALCOP_ERR_LAUNCH
+    far = {n: (i + 1) << 40 for i, n in enumerate(("dC", "A", "W", "pre", "dA", "dW", "ws"))}
+    kw = {**{n: p for n, p in far.items()}, **kw}
+    assert backward(db=db, bytes=1 << 39, **kw) == al.ERR_SIZE
+
+
 def norm(x=P[0], r=P[1], g=P[2], h=P[3], y=P[4], s=P[5], d=P[6], rows=8, cols=64, ldx=64, ldr=64, ldt=64, ldy=64, eps=1e-6, i=al.F16,
          o=al.F16):
     return al.lib().alcop_rmsnorm(x, r, g, h, y, s, d, rows, cols, ldx, ldr, ldt, ldy, eps, i, o, None)
