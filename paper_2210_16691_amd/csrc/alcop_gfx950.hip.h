@@ -251,6 +251,7 @@ struct Gfx950 {
   __device__ static __forceinline__ uint32_t xor_lanes(uint32_t v, int mask) { return (uint32_t)__shfl_xor((int)v, mask); }
   __device__ static __forceinline__ void lds_write1(uint32_t addr, uint32_t v) { *(ALCOP_LDS uint32_t*)(uintptr_t)addr = v; }
   __device__ static __forceinline__ float sqrt(float v) { return sqrtf(v); }
+  __device__ static __forceinline__ float fma(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
   __device__ static __forceinline__ float exp2(float v) { return __builtin_amdgcn_exp2f(v); }
   __device__ static __forceinline__ float rcp(float v) { return __builtin_amdgcn_rcpf(v); }    // within 1 ulp
   __device__ static __forceinline__ float erf(float v) { return erff(v); }

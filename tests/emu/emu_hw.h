@@ -703,6 +703,7 @@ struct Emu {
   }
   static void lds_write1(uint32_t addr, uint32_t v) { lds_write(addr, v); }
   static float sqrt(float v) { return __builtin_sqrtf(v); }
+  static float fma(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
   static float exp2(float v) { return __builtin_exp2f(v); }
   static float rcp(float v) { return 1.0f / v; }
   static float erf(float v) { return __builtin_erff(v); }
