@@ -56,6 +56,18 @@ hipError_t dispatch_rows_of(int dt, bool whole, int rows, int cols, const A&... 
   if (dt == 1) return whole ? dispatch_rows<1, true, LAUNCH>(rows, cols, a...) : dispatch_rows<1, false, LAUNCH>(rows, cols, a...);
   return whole ? dispatch_rows<2, true, LAUNCH>(rows, cols, a...) : dispatch_rows<2, false, LAUNCH>(rows, cols, a...);
 }
+// All of them: rows and columns that between them reach every line of dispatch_rows.
+template <template <class> class LAUNCH, class... A>
+hipError_t each_rows_kernel(const A&... a)
+{
+  static const int sizes[][2] = {{1, 512}, {1, 1024}, {1, 2048}, {1536, 2048}, {1, 4096}, {1, 8192}, {1, 16384}, {1, 32768}};
+  hipError_t rc = hipSuccess;
+  for (int dt = 0; dt < 3; dt++)
+    for (int whole = 0; whole < 2; whole++)
+      for (const auto& s : sizes)
+        if (rc == hipSuccess) rc = dispatch_rows_of<LAUNCH>(dt, whole, s[0], s[1], a...);
+  return rc;
+}
 
 // What the first calls of these operators would do besides launching.
 hipError_t prepare_layers();

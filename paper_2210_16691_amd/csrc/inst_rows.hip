@@ -62,10 +62,7 @@ hipError_t prepare_rows()
   hipError_t rc = hipFuncGetAttributes(&at, (const void*)alcop_column_sums<Gfx950>);
   if (rc == hipSuccess) rc = hipFuncGetAttributes(&at, (const void*)alcop_act_grad<0, Gfx950>);
   if (rc == hipSuccess) rc = hipFuncGetAttributes(&at, (const void*)alcop_act_grad<1, Gfx950>);
-  for (int dt = 0; dt < 3; dt++)
-    for (int whole = 0; whole < 2; whole++)
-      for (int cols : {512, 1024, 2048, 4096, 8192, 16384, 32768})
-        if (rc == hipSuccess) rc = dispatch_rows_of<Load>(dt, whole, 1, cols);
+  if (rc == hipSuccess) rc = each_rows_kernel<Load>();
   return rc;
 }
 

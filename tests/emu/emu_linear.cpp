@@ -2,6 +2,8 @@
 // tables whose launchers run the kernel templates on emu_hw.h.
 #include <hip/hip_runtime.h>
 
+#include <set>
+
 #include "emu_hw.h"
 #include "alcop_linear.h"
 
@@ -114,11 +116,39 @@ hipError_t launch_act_grad(const ActGradArgs& a, int dt, hipStream_t)
   return hipSuccess;
 }
 hipError_t prepare_rows() { return hipSuccess; }
+
+// the kernels that calls of these sizes launch, and those that are loaded ahead
+static std::set<const void*> reached;
+template <class C>
+struct Reach {
+  static hipError_t go()
+  {
+    reached.insert((const void*)&Norm<C>::entry);
+    return hipSuccess;
+  }
+};
 #endif
 
 }  // namespace alcop
 
 #if EMU_PART == 3
+// Kernels that are loaded ahead; those that `n` rows and columns reach; those of the latter that are not among the former.
+extern "C" void emu_rows_kernels(const int* sizes, int n, int* out)
+{
+  using namespace alcop;
+  reached.clear();
+  (void)each_rows_kernel<Reach>();
+  const std::set<const void*> loaded = reached;
+  reached.clear();
+  for (int i = 0; i < n; i++)
+    for (int dt = 0; dt < 3; dt++)
+      for (int whole = 0; whole < 2; whole++) (void)dispatch_rows_of<Reach>(dt, whole, sizes[2 * i], sizes[2 * i + 1]);
+  out[0] = (int)loaded.size();
+  out[1] = (int)reached.size();
+  out[2] = 0;
+  for (const void* k : reached) out[2] += !loaded.count(k);
+}
+
 // the model's conversions of 8-bit numbers, so that a test can pin them
 extern "C" uint8_t emu_f32_to_e4m3(float v) { return emu::float_to_e4m3(v); }
 extern "C" float emu_e4m3_to_f32(uint8_t b) { return emu::e4m3_to_float(b); }

@@ -1,5 +1,7 @@
 """Rows to 8 bits on the CPU model: scales and 8-bit numbers are those of the definition, bit for bit, as every step of
-it is one rounding of fp32."""
+it is one rounding of fp32.  And which of the rows' kernels alcop_init loads."""
+import ctypes
+
 import pytest
 import torch
 
@@ -61,3 +63,15 @@ def test_an_8_bit_norm_is_its_fp32_norm_divided(dtype):
     assert not emu.call(al.alcop_rmsnorm, x, g, y32, residual=r, reads=[x, r, g], writes=[y32])
     assert not emu.call(al.alcop_rmsnorm, x, g, y, residual=r, scale=s, reads=[x, r, g], writes=[y, s])
     same((y, s), plain(y32))
+
+
+def test_every_kernel_of_rows_is_loaded_ahead():
+    # what alcop_init loads against what calls of any number of rows and columns launch
+    sizes = [(r, c) for r in (1, 3, 4, 511, 1535, 1536, 5000) for c in
+             (1, 511, 512, 513, 1024, 1025, 1600, 2047, 2048, 2049, 4096, 4097, 8192, 8193, 16384, 16385, 32768)]
+    L = emu.lib()
+    L.emu_rows_kernels.argtypes, L.emu_rows_kernels.restype = [ctypes.POINTER(ctypes.c_int), ctypes.c_int,
+                                                               ctypes.POINTER(ctypes.c_int)], None
+    flat, out = (ctypes.c_int * (2 * len(sizes)))(*[v for s in sizes for v in s]), (ctypes.c_int * 3)()
+    L.emu_rows_kernels(flat, len(sizes), out)
+    assert list(out) == [48, 48, 0]
