@@ -106,16 +106,20 @@ struct Sigmoid {
 enum { CLASS_PLAIN = 0, CLASS_SIGMOID = 1, CLASS_ERF = 2 };
 inline int class_of(int act) { return act == ACT_GELU ? CLASS_ERF : act >= ACT_GELU_TANH ? CLASS_SIGMOID : CLASS_PLAIN; }
 
-// erfc(|z| / sqrt 2) within 1.5e-7: Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26.  Its form,
-// a polynomial of t = 1 / (1 + p x) times exp(-x^2), keeps its relative accuracy where erfc is small, which 1 + erf does
-// not; the library's erff, with a branch of its own on either side of 1, cost 50 us of 311 in a layer of 8192 x 8192.
+// erfc(|z| / sqrt 2) / 2, what the normal distribution leaves beyond |z|, and gauss = exp(-z^2 / 2): gauss times a polynomial of
+// t = 1 / (1 + 0.36 |z|), which is finite and smooth from 0 to infinity as the quotient of the two is.  Its coefficients are a
+// least-squares fit of the relative error with the weights moved to the largest errors until they are level: 7.9e-7 up to |z| = 13.5,
+// where gauss leaves the fp32 range.  In fp32 the relative error is at most (40 + 1.5 z^2) 2^-24, z^2 from the exponent's roundings:
+// GELU far left of 0 is this number times z, and one that is only absolutely near (1e-7) is off by half a step of fp16 at z = -4.
+// As many instructions as a degree of 5 in erfc's own argument and factor took: 8192 x 8192 x 2048 with `pre` 292 -> 294.5 us,
+// 507 x 2072 x 1000 11.07 -> 11.02; the library's erff, with a branch of its own on either side of 1, some 25 more.
 template <class HW>
-__device__ __forceinline__ float erfc_of(float z, float& gauss)
+__device__ __forceinline__ float half_erfc(float z, float& gauss)
 {
-  const float x = __builtin_fabsf(z) * 0.70710678119f;
-  const float t = HW::rcp(1.0f + 0.3275911f * x);
-  gauss = HW::exp2(-1.44269504089f * (x * x));
-  return gauss * (t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f)))));
+  const float t = HW::rcp(1.0f + 0.36f * __builtin_fabsf(z));
+  gauss = HW::exp2(-0.72134752044f * (z * z));
+  return gauss * (t * (0.143717438f + t * (0.141710728f + t * (0.140057132f + t * (0.0256246459f +
+                  t * (0.18229638f + t * (-0.180750787f + t * 0.0473443195f)))))));
 }
 
 template <int CLASS, class HW, int W>
@@ -130,7 +134,7 @@ __device__ __forceinline__ void activate(float (&v)[W], int act)
 #pragma unroll
     for (int e = 0; e < W; e++) {
       float gauss;
-      const float q = erfc_of<HW>(v[e], gauss), half = q == 0.f ? 0.f : 0.5f * v[e] * q;      // v may be infinite
+      const float q = half_erfc<HW>(v[e], gauss), half = q == 0.f ? 0.f : v[e] * q;      // v may be infinite
       v[e] = v[e] < 0.f ? half : v[e] - half;
     }
   } else {
@@ -147,7 +151,7 @@ __device__ __forceinline__ float slope(float z, int act)
   if (act == ACT_RELU) return z > 0.f ? 1.f : 0.f;
   if (act == ACT_GELU) {
     float gauss;                                                  // exp(-z^2 / 2)
-    const float half = 0.5f * erfc_of<HW>(z, gauss);
+    const float half = half_erfc<HW>(z, gauss);
     return (z < 0.f ? half : 1.0f - half) + (gauss == 0.f ? 0.f : z * gauss * 0.39894228040f);
   }
   if (act >= ACT_GELU_TANH) {

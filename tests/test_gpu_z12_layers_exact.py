@@ -1,9 +1,10 @@
-"""Rows to 8 bits on the GPU: scales and 8-bit numbers are those of the definition, bit for bit."""
+"""On the GPU: rows to 8 bits are those of the definition, bit for bit; activations and slopes are near relative to their size."""
 import pytest
 import torch
 
 import paper_2210_16691_amd as al
 from gpu_util import DEV
+from test_layers_accuracy import check_activation, check_slope
 from test_rows_exact import plain, same, values
 
 pytestmark = pytest.mark.gpu
@@ -43,3 +44,18 @@ def test_an_8_bit_norm_is_its_fp32_norm_divided(dtype, rows, cols):
     al.alcop_rmsnorm(x, g, y, residual=r, scale=s)
     torch.cuda.synchronize()
     same((y.cpu(), s.cpu()), plain(y32.cpu()))
+
+
+def on_the_gpu(fn, *args, reads=None, writes=None, **kw):
+    fn(*args, **kw)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("act", [2, 3, 4])
+def test_activations_are_near_relative_to_their_value(act):
+    check_activation(on_the_gpu, act, DEV)
+
+
+@pytest.mark.parametrize("act", [2, 3, 4])
+def test_slopes_are_near_relative_to_their_terms(act):
+    check_slope(on_the_gpu, act, DEV)
