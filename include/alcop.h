@@ -388,8 +388,8 @@ int alcop_splitk_auto(const alcop_problem* prob /* host */, int split,
  * A linear layer with what stands between its product and the next operator in the epilogue:
  *     Z[i][j] = alpha * scale_a[i] * scale_w[j] * sum_k A(i,k) W(k,j) + bias[j]
  *     C[i][j] = act(Z[i][j]) + residual[i][j]
- * all of it in fp32 on the accumulators, rounded once to the output type.  `pre` receives Z rounded to that type
- * (what alcop_linear_backward asks for); the activation sees Z before the rounding.
+ * all of it in fp32 on the accumulators (but see FP32_SUMS), rounded once to the output type.  `pre` receives Z rounded to that
+ * type (what alcop_linear_backward asks for); the activation sees Z before the rounding.
  *   A: row-major M x K.  W: transB = 0 row-major K x N, transB = 1 stored N x K (a layer's weights: out x in).
  *   in: ALCOP_F16, ALCOP_BF16, or ALCOP_E4M3 for both operands (transB = 1), whose values stand for
  *     e4m3 * scale_a[i] and e4m3 * scale_w[j]; scale_a, scale_w: DEVICE, M and N fp32 values, or NULL = 1.  Scales may
@@ -397,21 +397,28 @@ int alcop_splitk_auto(const alcop_problem* prob /* host */, int split,
  *   out: ALCOP_F16, ALCOP_BF16 or ALCOP_F32, the type of C, residual and pre.
  *   act: 0 identity, 1 ReLU, 2 GELU (0.5 z (1 + erf(z / sqrt 2))), 3 GELU (0.5 z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)))),
  *     4 SiLU (z / (1 + exp(-z))).
+ *     + ALCOP_FP32_SUMS: sums of ALCOP_E4M3 operands are fp32 whatever the result's type and the layer's size.  Without it they are
+ *     if `out` is ALCOP_F32, and in layers so small that it costs nothing; larger ones with a 16-bit result use the 8-bit matrix
+ *     instruction, 1.5 to 1.7 times as fast, which of every eight products (k = 8 g .. 8 g + 7) cuts off
+ *     what lies below 2^-13 of the largest (of its exponents' sum, numbers below 2^-6 counting as 2^-6).  Z, and C and pre with it, is then off by at
+ *     most 7 * 2^-13 * sum_g max_{k in g} |A(i,k) W(k,j)| times alpha and the scales more, below 2^-10 of the sum of the magnitudes; of normally
+ *     distributed numbers by 2^-16 of Z's standard deviation.  What can show it is a sum of which a few large products cancel.
  *   residual, pre: DEVICE, M x N, row pitches ldr, ldp >= N, or NULL.  residual may be C itself (same pitch); otherwise C
  *     and pre overlap nothing that is read, nor each other (columns of one wider matrix do not overlap).
  *   tail == NULL: alpha = 1 and nothing else.
  * M is free; N is free with transB = 1, else a multiple of 8; K is a multiple of 8 (ALCOP_E4M3: 16).  A, W: 16-byte aligned,
  * pitches multiples of 8 (16) elements; bias and scale_w 16-byte aligned.  C, residual and pre may lie at any element
- * and have any pitch; rows made of 16-byte chunks are faster.  Sums are fp32 and their order fixed: the same
+ * and have any pitch; rows made of 16-byte chunks are faster.  Sums have a fixed order: the same
  * call gives the same bits.  Errors as for alcop_gemm; ALCOP_ERR_UNSUPPORTED for an unknown act, overlaps, or
  * ALCOP_E4M3 with transB = 0.  No schedule argument: the kernel is picked by measured cost.  The environment variable
  * ALCOP_LINEAR_KERNEL (a number, read at every call) takes that one of the operand type's and layout's kernels instead,
  * and ALCOP_ERR_SCHED is returned where there are fewer.
  */
+#define ALCOP_FP32_SUMS 16
 typedef struct {
   float alpha;
   const void* bias;           /* N fp32 values or NULL */
-  int act;
+  int act;                    /* 0 .. 4, + ALCOP_FP32_SUMS */
   const void* residual;
   long ldr;
   void* pre;
@@ -453,7 +460,7 @@ int alcop_linear_backward(const void* dC, const void* A, const void* W, const vo
  *   x, residual, total: type `in` (ALCOP_F16, ALCOP_BF16, ALCOP_F32); gain: cols fp32 values; residual, total, gain (= 1), rstd
  *     may be NULL.  y is computed from h before its rounding.
  *   out = ALCOP_F16, ALCOP_BF16, ALCOP_F32: y is stored so.  out = ALCOP_E4M3: 8 bits and a scale per row,
- *     scale[i] = max(max_j |y[i][j]| / 448, 2^-126) and e4m3(y / scale), as alcop_linear takes them as A.
+ *     scale[i] = max(max_j |y[i][j]| / 448, 2^-126) and e4m3(y / scale), each quotient rounded to fp32, as alcop_linear takes them as A.
  *   A row with an infinity or a NaN gives what the formulas give: its sum is not finite, and an e4m3 row's scale is NaN
  *   if one of its y is.  mean h^2 has to stay below the fp32 range (|h| below 1e19).
  * 1 <= rows < 2^22 (2^24 up to 1024 columns), 1 <= cols <= 32768, any alignment and pitch >= cols (rows that start at 16

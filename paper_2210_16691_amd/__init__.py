@@ -17,6 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libalcop.so")
 
 F16, BF16, F32, E4M3 = 0, 1, 2, 3
+FP32_SUMS = 16           # added to alcop_linear_tail's act
 OP_GEMM, OP_BMM, OP_CONV2D = 0, 1, 2
 
 OK = 0
@@ -455,12 +456,18 @@ def _call_on(t, what, fn, *args, stream=None):
 
 
 def alcop_linear(A, W, C, transB=False, alpha=1.0, bias=None, act=0, residual=None, pre=None, scale_a=None, scale_w=None,
-                 stream=None):
+                 stream=None, fp32_sums=False):
     """C = act(Z) + residual with Z = alpha * scale_a[i] * scale_w[j] * A.W + bias[j]; `pre` receives Z.
 
     A is [M,K], W [K,N] or, with transB, [N,K] (a layer's weights); both fp16, bf16 or, with transB, e4m3
     (torch.float8_e4m3fn).  C, residual and pre are [M,N] of one type: fp16, bf16 or fp32; residual may be C.  bias,
-    scale_w (N) and scale_a (M) are fp32 vectors.  act: 0 none, 1 ReLU, 2 GELU (erf), 3 GELU (tanh), 4 SiLU."""
+    scale_w (N) and scale_a (M) are fp32 vectors.  act: 0 none, 1 ReLU, 2 GELU (erf), 3 GELU (tanh), 4 SiLU.
+
+    Sums are fp32, but for e4m3 operands, a 16-bit C and a layer that is not small: the 8-bit matrix instruction cuts off, of
+    every eight products (k = 8g .. 8g+7), what lies below 2^-13 of the largest.  Z is then off by up to 2^-10 of the sum of its terms'
+    magnitudes, of normally distributed numbers by 2^-16 of its standard deviation.  fp32_sums=True has fp32 sums there too."""
+    if fp32_sums:
+        act = int(act) | FP32_SUMS
     if _marshal_lib is _lib is not None:
         rc = _marshal.linear(A, W, C, transB, alpha, bias, act, residual, pre, scale_a, scale_w, stream)
         if rc is not None:

@@ -60,8 +60,8 @@ bool meet(const Span& a, const Span& b)
 }
 bool same(const Span& a, const Span& b) { return a.p == b.p && (a.rows < 2 || a.pitch == b.pitch) && a.row == b.row; }
 
-// The kernel of the lowest measured cost.  fine: e4m3 operands may be multiplied as they are (a sum of the 8-bit matrix
-// instruction is not one of fp32, which a result in fp32 is worth; 8192 x 8192 x 4096 without a residual 228 us so, 412 widened).
+// The kernel of the lowest measured cost.  fine: sums are to be fp32, which those of the 8-bit matrix instruction are not
+// (8192 x 8192 x 4096 without a residual 228 us, 412 on widened operands): asked for, or a result in fp32, which is worth it.
 const LinearKernel* pick(int cls, int dt, int bl, bool fine, int M, int N, int K, double bytes)
 {
   const LinearKernel* best = nullptr;
@@ -139,6 +139,8 @@ int alcop_linear(const void* A, const void* W, void* C, int M, int N, int K, lon
   std::memset(&t, 0, sizeof(t));
   t.alpha = 1.0f;
   if (tail) t = *tail;
+  const bool fine = out == ALCOP_F32 || (t.act & ALCOP_FP32_SUMS);
+  t.act &= ~ALCOP_FP32_SUMS;
   transB = transB ? 1 : 0;
   if (!A || !W || !C) return ALCOP_ERR_NULL;
   if (!is_half(in) && in != ALCOP_E4M3) return ALCOP_ERR_DTYPE;
@@ -157,8 +159,7 @@ int alcop_linear(const void* A, const void* W, void* C, int M, int N, int K, lon
   const int K16 = in == ALCOP_E4M3 ? K / 2 : K;              // in units of 16 bits
   const double c_bytes = (double)osz * M * N;
   const double bytes = 2.0 * K16 * ((double)M + N) + c_bytes * (1 + (t.residual ? 1 : 0) + (t.pre ? 1 : 0));
-  const LinearKernel* k = pick(class_of(t.act), in == ALCOP_E4M3 ? 2 : in == ALCOP_BF16 ? 1 : 0, transB, out == ALCOP_F32, M, N, K16,
-                               bytes);
+  const LinearKernel* k = pick(class_of(t.act), in == ALCOP_E4M3 ? 2 : in == ALCOP_BF16 ? 1 : 0, transB, fine, M, N, K16, bytes);
   if (!k) return ALCOP_ERR_SCHED;
   // 32-bit byte offsets from a tile's origin, rows past the end of a partial k-tile included
   const double rows = std::min(k->s.bm, M), cols = std::min(k->s.bn, N);

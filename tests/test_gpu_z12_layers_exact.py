@@ -1,9 +1,12 @@
-"""On the GPU: rows to 8 bits are those of the definition, bit for bit; activations and slopes are near relative to their size."""
+"""On the GPU: rows to 8 bits are those of the definition, bit for bit; activations and slopes are near relative to
+their size; sums of layers on e4m3 operands are within the bound of the 8-bit matrix instruction, or fp32."""
 import pytest
 import torch
 
 import paper_2210_16691_amd as al
 from gpu_util import DEV
+from layers_util import check, linear64
+from sums8_util import cancelling, check_sums, quantized_pair
 from test_layers_accuracy import check_activation, check_slope
 from test_rows_exact import plain, same, values
 
@@ -59,3 +62,53 @@ def test_activations_are_near_relative_to_their_value(act):
 @pytest.mark.parametrize("act", [2, 3, 4])
 def test_slopes_are_near_relative_to_their_terms(act):
     check_slope(on_the_gpu, act, DEV)
+
+
+KERNELS, F8_KERNELS = 11, 6
+
+
+@pytest.mark.parametrize("kernel", range(KERNELS, KERNELS + F8_KERNELS))
+def test_sums_of_the_8_bit_instruction(kernel, monkeypatch):
+    monkeypatch.setenv("ALCOP_LINEAR_KERNEL", str(kernel))
+    M, N, K = 513, 776, 2064
+    A, W, sa, sw = quantized_pair(M, N, K, kernel, DEV)
+    for out, act in ((torch.float16, 0), (torch.float16, 2), (torch.bfloat16, 4)):
+        C, z = torch.empty(M, N, dtype=out, device=DEV), torch.empty(M, N, dtype=out, device=DEV)
+        al.alcop_linear(A, W, C, transB=True, act=act, pre=z, scale_a=sa, scale_w=sw)
+        torch.cuda.synchronize()
+        check_sums(C, z, A, W, act=act, sa=sa, sw=sw)
+    A, W, exact = cancelling(300, 264, 1024, DEV)
+    C = torch.empty(300, 264, dtype=torch.float16, device=DEV)
+    al.alcop_linear(A, W, C, transB=True)
+    torch.cuda.synchronize()
+    check_sums(C, None, A, W, random=False)
+    assert C.eq(0).all()
+
+
+def test_sums_of_every_8_bit_number(monkeypatch):
+    # all exponents, numbers below 2^-6 among them
+    monkeypatch.setenv("ALCOP_LINEAR_KERNEL", str(KERNELS))
+    g = torch.Generator().manual_seed(1)
+    for low, span in ((0, 127), (0, 24), (70, 57)):
+        A, W = ((torch.randint(0, span, (256, 512), generator=g) + low + 128 * torch.randint(0, 2, (256, 512), generator=g))
+                .to(torch.uint8).view(torch.float8_e4m3fn).to(DEV) for _ in range(2))
+        C = torch.empty(256, 256, dtype=torch.bfloat16, device=DEV)
+        al.alcop_linear(A, W, C, transB=True)
+        torch.cuda.synchronize()
+        check_sums(C, None, A, W, random=False)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 264, 1024), (40, 264, 1024), (300, 520, 1024), (2048, 2056, 1040)])
+def test_fp32_sums_that_are_asked_for(M, N, K):
+    A, W, exact = cancelling(M, N, K // 8 * 8, DEV)
+    for act in (0, 4):
+        C, z = torch.empty(M, N, dtype=torch.float16, device=DEV), torch.empty(M, N, dtype=torch.float16, device=DEV)
+        al.alcop_linear(A, W, C, transB=True, act=act, pre=z, fp32_sums=True)
+        torch.cuda.synchronize()
+        assert z.eq(exact).all()
+        check(C, *linear64(A, W, True, act=act)[::3])
+    A, W, sa, sw = quantized_pair(M, N, K, 3, DEV)
+    C = torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+    al.alcop_linear(A, W, C, transB=True, scale_a=sa, scale_w=sw, fp32_sums=True)
+    torch.cuda.synchronize()
+    check(C, *linear64(A, W, True, sa=sa, sw=sw)[::3])
