@@ -230,6 +230,8 @@ struct Gfx950 {
   {
     return __builtin_nontemporal_load((const u32x4_any*)ptr);
   }
+  // written through as global_store16_through does, at any element
+  __device__ static __forceinline__ void global_store16_through_any(void* ptr, u32x4 v) { global_store16_through(ptr, v); }
   typedef u32x2 u32x2_any __attribute__((aligned(2)));
   __device__ static __forceinline__ u32x2 global_load8_any(const void* ptr) { return *(const u32x2_any*)ptr; }
   __device__ static __forceinline__ void global_store8_any(void* ptr, u32x2 v)

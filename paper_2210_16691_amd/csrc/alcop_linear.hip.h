@@ -220,7 +220,7 @@ __device__ __forceinline__ void store_row(const char* at, const float (&v)[W])
   char* ptr = const_cast<char*>(at);
   auto put16 = [&](char* dst, u32x4 t) __attribute__((always_inline)) {
     if constexpr (KEEP)
-      HW::global_store16_through(dst, t);
+      HW::global_store16_through_any(dst, t);
     else
       HW::global_store16_any(dst, t);
   };

@@ -149,6 +149,29 @@ extern "C" void emu_rows_kernels(const int* sizes, int n, int* out)
   for (const void* k : reached) out[2] += !loaded.count(k);
 }
 
+// One thread's 16-byte stores of each kind to `ptr`, for the test of what the model reports.
+namespace {
+struct Stores {
+  void* ptr;
+  int kind;
+};
+void stores_entry(const void* p)
+{
+  const Stores& s = *(const Stores*)p;
+  const alcop::u32x4 v = {1, 2, 3, 4};
+  if (emu::Emu::lane_id() != 0) return;
+  if (s.kind == 0) emu::Emu::global_store16(s.ptr, v);
+  if (s.kind == 1) emu::Emu::global_store16_through(s.ptr, v);
+  if (s.kind == 2) emu::Emu::global_store16_keep(s.ptr, v);
+  if (s.kind == 3) emu::Emu::global_store16_any(s.ptr, v);
+  if (s.kind == 4) emu::Emu::global_store16_through_any(s.ptr, v);
+}
+}  // namespace
+extern "C" void emu_store16(void* ptr, int kind)
+{
+  const Stores s{ptr, kind};
+  emu::run_grid(&stores_entry, &s, 64, 1024, 1, 1, 1);
+}
 // the model's conversions of 8-bit numbers, so that a test can pin them
 extern "C" uint8_t emu_f32_to_e4m3(float v) { return emu::float_to_e4m3(v); }
 extern "C" float emu_e4m3_to_f32(uint8_t b) { return emu::e4m3_to_float(b); }
