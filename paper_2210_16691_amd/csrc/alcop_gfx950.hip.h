@@ -257,7 +257,6 @@ struct Gfx950 {
   __device__ static __forceinline__ float fma(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
   __device__ static __forceinline__ float exp2(float v) { return __builtin_amdgcn_exp2f(v); }
   __device__ static __forceinline__ float rcp(float v) { return __builtin_amdgcn_rcpf(v); }    // within 1 ulp
-  __device__ static __forceinline__ float erf(float v) { return erff(v); }
 };
 
 }  // namespace alcop

@@ -738,7 +738,6 @@ struct Emu {
   static float fma(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
   static float exp2(float v) { return __builtin_exp2f(v); }
   static float rcp(float v) { return 1.0f / v; }
-  static float erf(float v) { return __builtin_erff(v); }
   static uint16_t global_load_u16(const void* ptr) { return global_load_elem<uint16_t>(ptr); }
   static uint32_t global_load_u32(const void* ptr) { return global_load_elem<uint32_t>(ptr); }
   static void global_store_u16(void* ptr, uint16_t v) { global_store_elem<uint16_t>(ptr, v); }
