@@ -5,8 +5,9 @@ import torch
 
 import paper_2210_16691_amd as al
 from gpu_util import DEV
-from layers_util import check, linear64
+from layers_util import ULP, check, check_e4m3, linear64, norm64
 from sums8_util import cancelling, check_sums, quantized_pair
+from test_gpu_z11_layers import matrix, padding, run_backward, vector
 from test_layers_accuracy import check_activation, check_slope
 from test_rows_exact import plain, same, values
 
@@ -112,3 +113,61 @@ def test_fp32_sums_that_are_asked_for(M, N, K):
     al.alcop_linear(A, W, C, transB=True, scale_a=sa, scale_w=sw, fp32_sums=True)
     torch.cuda.synchronize()
     check(C, *linear64(A, W, True, sa=sa, sw=sw)[::3])
+
+
+# ---- rows that have a wave each --------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,cols", [(1535, 2048), (1536, 2048), (1537, 1025), (2001, 1603), (3000, 1536)])
+@pytest.mark.parametrize("dtype,out", [("f16", "e4m3"), ("bf16", "e4m3"), ("f32", "e4m3"), ("f16", "f16"), ("bf16", "bf16"), ("f32", "f32"),
+                                       ("bf16", "f32")])
+def test_norms_of_many_rows(rows, cols, dtype, out):
+    pad = 3 if cols % 8 else 8
+    x, r, h = (matrix(rows, cols, dtype, s, pad, 2.0) for s in (1, 2, 3))
+    g, d, s = vector(cols, 4), vector(rows, 5), vector(rows, 6) if out == "e4m3" else None
+    y = matrix(rows, cols, out, 7, pad)
+    yref, href, dref = norm64(x, r, g)
+    al.alcop_rmsnorm(x, g, y, residual=r, total=h, scale=s, rstd=d)
+    torch.cuda.synchronize()
+    err = (cols / 2 + 8) * ULP
+    check(d[:, None], dref[:, None], err * dref[:, None], "rstd")
+    check(h, href, ULP * href.abs(), "total")
+    if out == "e4m3":
+        # h is rounded once to fp32 before its norm
+        check_e4m3(y, s, yref, err + ULP, "y")
+    else:
+        check(y, yref, err * yref.abs() + ULP * href.abs() * dref[:, None] * g.cpu().double().abs(), "y")
+    for t in (h, y):
+        assert padding(t).float().isnan().all()
+    # without residual, sum and gain; the sum in the residual's place
+    y32, total = torch.empty(rows, cols, device=DEV), r.clone()
+    al.alcop_rmsnorm(x, None, y32)
+    check(y32, norm64(x)[0], err * norm64(x)[0].abs(), "y")
+    al.alcop_rmsnorm(x, g, matrix(rows, cols, out, 8, pad), residual=total, total=total, scale=s)
+    assert torch.equal(total, h)
+
+
+def test_rows_that_have_a_wave_each_in_a_captured_graph():
+    rows, cols = 2000, 1600
+    x, r, h, y = (matrix(rows, cols, "bf16", s) for s in (1, 2, 3, 4))
+    g, q, s = vector(cols, 5), torch.empty(rows, cols, dtype=torch.float8_e4m3fn, device=DEV), vector(rows, 6)
+    al.alcop_init()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        al.alcop_rmsnorm(x, g, y, residual=r, total=h)
+        al.alcop_quantize_rows(y, q, s)
+    for k in range(3):
+        x.copy_(matrix(rows, cols, "bf16", 10 + k))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (h, y, s)] + [q.view(torch.uint8).clone()]
+        al.alcop_rmsnorm(x, g, y, residual=r, total=h)
+        al.alcop_quantize_rows(y, q, s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (h, y, s, q.view(torch.uint8))))
+
+
+# ---- split sums ------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("M,N,K,transB,act", [(5856, 64, 1400, True, 0), (8192, 256, 264, False, 3), (16384, 256, 256, True, 2)])
+@pytest.mark.parametrize("alpha", [0.5, -1.75])
+def test_split_weight_gradients_with_a_factor(M, N, K, transB, act, alpha):
+    run_backward(M, N, K, "bf16", transB, act, alpha=alpha)
+    run_backward(M, N, K, "f16", transB, act, out="f32", alpha=alpha, bias=False)

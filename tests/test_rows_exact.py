@@ -7,6 +7,7 @@ import torch
 
 import emu_util as emu
 import paper_2210_16691_amd as al
+from test_layers_emulated import run_norm
 
 DT = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
 TINY = 2.0 ** -126
@@ -75,3 +76,9 @@ def test_every_kernel_of_rows_is_loaded_ahead():
     flat, out = (ctypes.c_int * (2 * len(sizes)))(*[v for s in sizes for v in s]), (ctypes.c_int * 3)()
     L.emu_rows_kernels(flat, len(sizes), out)
     assert list(out) == [48, 48, 0]
+
+
+@pytest.mark.parametrize("dtype,out,rows,cols", [("f16", "e4m3", 1536, 1032), ("f32", "f32", 1537, 1025), ("bf16", "bf16", 1536, 2048)])
+def test_norms_of_rows_that_have_a_wave_each(dtype, out, rows, cols):
+    # 1025 to 2048 columns are a block's row, but a wave's from 1536 rows on
+    run_norm(rows, cols, dtype, out, pad=3 if cols % 8 else 8)
