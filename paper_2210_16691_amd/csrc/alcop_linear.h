@@ -32,9 +32,9 @@ hipError_t prepare_rows();
 
 // Threads that share a row, and their chunks of eight elements: a wave, or a block of 256 or 1024.
 constexpr int ROWS_MAX_COLS = 32768;
-// Whether a wave has a row: up to 1024 columns, and up to 2048 where there are rows enough to fill the card.  1600 columns to 8
-// bits, 2048 rows: 5.2 us with a block for each, 4.8 with a wave; 32768 rows 43.8 and 29.7; 512 rows 3.8 and 4.2, norms 4.9 and
-// 6.0.  The norm's gradients of 1600 columns: 2048 rows 13.3 and 12.2, 512 rows 8.3 and 9.4.
+// Whether a wave has a row: up to 1024 columns, and up to 2048 where there are rows enough to fill the card.  1600 columns of
+// bf16 with a block for each row and with a wave, us: to 8 bits 512 rows 3.5 and 3.7, 2048 rows 5.1 and 5.3, 32768 rows 43.1 and 31.6;
+// norms 3.8 and 4.2, 5.5 and 5.6, 53.9 and 53.9; the norm's gradients 7.8 and 9.1, 12.3 and 10.6, 62.0 and 66.5.
 inline bool wave_rows(int rows, int cols) { return cols <= 1024 || (cols <= 2048 && rows >= 1536); }
 template <int DT, bool WHOLE, template <class> class LAUNCH, class... A>
 hipError_t dispatch_rows(int rows, int cols, const A&... a)

@@ -5,7 +5,7 @@ import torch
 
 import paper_2210_16691_amd as al
 from gpu_util import DEV
-from layers_util import ULP, check, check_e4m3, linear64, norm64
+from layers_util import ULP, check, check_e4m3, linear64, norm64, norm_grad64
 from sums8_util import cancelling, check_sums, quantized_pair
 from test_gpu_z11_layers import matrix, padding, run_backward, vector
 from test_layers_accuracy import check_activation, check_slope
@@ -171,3 +171,57 @@ def test_rows_that_have_a_wave_each_in_a_captured_graph():
 def test_split_weight_gradients_with_a_factor(M, N, K, transB, act, alpha):
     run_backward(M, N, K, "bf16", transB, act, alpha=alpha)
     run_backward(M, N, K, "f16", transB, act, out="f32", alpha=alpha, bias=False)
+
+
+# ---- every kernel there is ---------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,transB", [("f16", False), ("f16", True), ("bf16", False), ("bf16", True), ("e4m3", True)])
+@pytest.mark.parametrize("act", [1, 2, 3])        # one of each class of activation: a kernel each
+def test_every_kernel_of_every_class_of_activation(dtype, transB, act, monkeypatch):
+    M, N, K = 270, 264, 208
+    A, W = matrix(M, K, dtype, 1, 16), matrix(*((N, K) if transB else (K, N)), dtype, 2, 16, scale=K ** -0.5)
+    b, r = vector(N, 3), {o: matrix(M, N, o, 4) for o in ("f16", "bf16", "f32")}
+    for kernel in range(KERNELS + (F8_KERNELS if dtype == "e4m3" else 0)):
+        monkeypatch.setenv("ALCOP_LINEAR_KERNEL", str(kernel))
+        for out in ("f16", "bf16", "f32"):
+            if kernel >= KERNELS and out == "f32":
+                continue
+            C, z = matrix(M, N, out, 5, 8), matrix(M, N, out, 6, 8)
+            al.alcop_linear(A, W, C, transB=transB, bias=b, act=act, residual=r[out], pre=z)
+            torch.cuda.synchronize()
+            what = "kernel %d %s" % (kernel, out)
+            if kernel >= KERNELS:
+                check_sums(C, z, A, W, bias=b, act=act, residual=r[out], random=False, what=what)
+            else:
+                ref, zref, ez, ec = linear64(A, W, transB, 1.0, b, act, r[out])
+                check(C, ref, ec, "C " + what)
+                check(z, zref, ez, "pre " + what)
+            assert padding(C).isnan().all() and padding(z).isnan().all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("whole", [True, False])
+@pytest.mark.parametrize("rows,cols", [(9, 512), (9, 1024), (5, 2048), (1536, 2048), (5, 4096), (5, 8192), (3, 16384), (3, 32768)])
+def test_every_kernel_of_rows(dtype, whole, rows, cols):
+    cols -= 0 if whole else 3
+    x, r, h = (matrix(rows, cols, dtype, s, 5, 2.0) for s in (1, 2, 3))
+    g, d = vector(cols, 4), vector(rows, 5)
+    err = (cols / 2 + 8) * ULP
+    yref, href, dref = norm64(x, r, g)
+    for out in ("f16", "bf16", "f32", "e4m3"):
+        y, s = matrix(rows, cols, out, 6, 5), vector(rows, 7) if out == "e4m3" else None
+        al.alcop_rmsnorm(x, g, y, residual=r, total=h, scale=s, rstd=d)
+        torch.cuda.synchronize()
+        if out == "e4m3":
+            check_e4m3(y, s, yref, err + ULP, out)
+        else:
+            check(y, yref, err * yref.abs() + ULP * href.abs() * dref[:, None] * g.cpu().double().abs(), out)
+        assert padding(y).float().isnan().all()
+    check(h, href, ULP * href.abs(), "total")
+    dy, dt, dx, dg = matrix(rows, cols, dtype, 8, 5), matrix(rows, cols, dtype, 9, 5), matrix(rows, cols, dtype, 10, 5), vector(cols, 11)
+    ws = torch.full((al.alcop_rmsnorm_backward_workspace_bytes(rows, cols),), 255, dtype=torch.uint8, device=DEV)
+    al.alcop_rmsnorm_backward(dy, h, g, d, dx, dgain=dg, dtotal=dt, workspace=ws)
+    torch.cuda.synchronize()
+    ref, gref, edx, edg = norm_grad64(dy, h, g, d, dt)
+    check(dx, ref, edx, "dx")
+    check(dg[None], gref[None], edg[None], "dgain")
+    assert padding(dx).isnan().all()
