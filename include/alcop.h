@@ -401,7 +401,7 @@ int alcop_splitk_auto(const alcop_problem* prob /* host */, int split,
  *     if `out` is ALCOP_F32, and in layers so small that it costs nothing; larger ones with a 16-bit result use the 8-bit matrix
  *     instruction, 1.5 to 1.7 times as fast, which of every eight products (k = 8 g .. 8 g + 7) cuts off
  *     what lies below 2^-13 of the largest (of its exponents' sum, numbers below 2^-6 counting as 2^-6).  Z, and C and pre with it, is then off by at
- *     most 7 * 2^-13 * sum_g max_{k in g} |A(i,k) W(k,j)| times alpha and the scales more, below 2^-10 of the sum of the magnitudes; of normally
+ *     most 7 * 2^-13 * sum_g max_{k in g} |A(i,k) W(k,j)| times alpha and the scales more, below 2^-10 of the sum of the magnitudes counted so; of normally
  *     distributed numbers by 2^-16 of Z's standard deviation.  What can show it is a sum of which a few large products cancel.
  *   residual, pre: DEVICE, M x N, row pitches ldr, ldp >= N, or NULL.  residual may be C itself (same pitch); otherwise C
  *     and pre overlap nothing that is read, nor each other (columns of one wider matrix do not overlap).
