@@ -50,8 +50,9 @@ typedef enum {
   ALCOP_F16 = 0,
   ALCOP_BF16 = 1,
   ALCOP_F32 = 2,              /* products: output only                                       */
-  ALCOP_E4M3 = 3              /* alcop_linear's operands, results of alcop_rmsnorm and        */
-                              /* alcop_quantize_rows: 8 bits, no infinities, largest 448     */
+  ALCOP_E4M3 = 3              /* operands of alcop_linear and alcop_grouped_linear, results  */
+                              /* of the norms and alcop_quantize_rows: 8 bits, no            */
+                              /* infinities, largest 448                                     */
 } alcop_dtype;
 
 typedef enum {
@@ -491,6 +492,38 @@ int alcop_rmsnorm_backward(const void* dy, const void* total, const void* gain, 
  */
 int alcop_quantize_rows(const void* x, void* y, void* scale, int rows, int cols, long ldx, long ldy, alcop_dtype in,
                         void* hip_stream);
+
+/*
+ * Layer norm of rows, with the residual's addition in front of it:
+ *     h = x + residual;   mean[i] = mean_j h[i][j];   rstd[i] = 1 / sqrt(mean_j (h[i][j] - mean[i])^2 + eps);
+ *     y[i][j] = (h[i][j] - mean[i]) * rstd[i] * gain[j] + shift[j]
+ * in fp32, the mean and the variance of a row that lies far from 0 without cancellation; total receives h, mean and
+ * rstd (rows fp32 values each) what the backward pass asks for.
+ *   gain (NULL = 1), shift (NULL = 0): cols fp32 values; residual, total, mean, rstd may be NULL.  Types, y in 8 bits with a scale per
+ *     row, sizes, alignment and what may be the same matrix: as for alcop_rmsnorm.  A row with an infinity or a NaN
+ *     gives NaN throughout.
+ * One launch.
+ */
+int alcop_layernorm(const void* x, const void* residual, const void* gain, const void* shift, void* total, void* y, void* scale,
+                    void* mean, void* rstd, int rows, int cols, long ldx, long ldr, long ldt, long ldy, float eps,
+                    alcop_dtype in, alcop_dtype out, void* hip_stream);
+
+/*
+ * Its gradients: with xh = (total - mean) * rstd and t = gain * dy,
+ *     dx = dtotal + rstd * (t - mean_j(t) - xh * mean_j(t * xh)),
+ *     dgain[j] = sum_i dy[i][j] * xh[i][j],   dshift[j] = sum_i dy[i][j].
+ * dx is the gradient of x and of the residual; dtotal (may be NULL) is what arrives at total from behind.
+ *   dy, total, dtotal, dx: type `in`; gain (may be NULL = 1), mean, rstd, dgain, dshift (may be NULL): fp32.  dx may be dy or
+ *     dtotal.
+ *   workspace: DEVICE, 16-byte aligned, at least alcop_layernorm_backward_workspace_bytes(rows, cols) bytes, needed
+ *     with dgain or dshift, as for alcop_linear_backward.
+ * Sizes as for alcop_rmsnorm.  One launch, two with dgain or dshift of more than a few rows; sums have a fixed order.
+ */
+size_t alcop_layernorm_backward_workspace_bytes(int rows, int cols);
+int alcop_layernorm_backward(const void* dy, const void* total, const void* gain, const void* mean, const void* rstd,
+                             const void* dtotal, void* dx, void* dgain, void* dshift, int rows, int cols, long lddy, long ldt,
+                             long lddt, long lddx, alcop_dtype in, void* workspace, size_t workspace_bytes,
+                             void* hip_stream);
 
 /*
  * Feasibility of a schedule for a problem, without launching (the checks the paper's

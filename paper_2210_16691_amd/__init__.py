@@ -175,6 +175,12 @@ def _declare(L: ctypes.CDLL) -> ctypes.CDLL:
     L.alcop_rmsnorm_backward.argtypes = [vp] * 7 + [i, i] + [l] * 4 + [i, vp, sz, vp]
     L.alcop_quantize_rows.restype = i
     L.alcop_quantize_rows.argtypes = [vp, vp, vp, i, i, l, l, i, vp]
+    L.alcop_layernorm.restype = i
+    L.alcop_layernorm.argtypes = [vp] * 9 + [i, i] + [l] * 4 + [f, i, i, vp]
+    L.alcop_layernorm_backward_workspace_bytes.restype = sz
+    L.alcop_layernorm_backward_workspace_bytes.argtypes = [i, i]
+    L.alcop_layernorm_backward.restype = i
+    L.alcop_layernorm_backward.argtypes = [vp] * 9 + [i, i] + [l] * 4 + [i, vp, sz, vp]
     L.alcop_init.restype = i
     L.alcop_init.argtypes = []
     L.alcop_strerror.restype = ctypes.c_char_p
@@ -200,6 +206,7 @@ def lib() -> ctypes.CDLL:
         m.init_layers(*[ctypes.cast(f, ctypes.c_void_p).value for f in
                         (L.alcop_linear, L.alcop_linear_backward, L.alcop_rmsnorm, L.alcop_rmsnorm_backward,
                          L.alcop_quantize_rows)])
+        m.init_more(*[ctypes.cast(f, ctypes.c_void_p).value for f in (L.alcop_layernorm, L.alcop_layernorm_backward)])
         _lib, _marshal, _marshal_lib = L, m, L
     return _lib
 
@@ -581,6 +588,61 @@ def alcop_rmsnorm_backward(dy, total, gain, rstd, dx, dgain=None, dtotal=None, w
     _call_on(dy, "alcop_rmsnorm_backward", lib().alcop_rmsnorm_backward, _ptr(dy), _ptr(total), _ptr(gain), _ptr(rstd),
              _ptr(dtotal), _ptr(dx), _ptr(dgain), rows, cols, lddy, ldt, _pitch(dtotal), lddx, _kind(dy), ws, ws_bytes,
              stream=stream)
+    return dx
+
+
+def alcop_layernorm(x, gain, shift, y, residual=None, total=None, scale=None, mean=None, rstd=None, eps=1e-5, stream=None):
+    """y = (h - mean) * rstd * gain + shift with h = x + residual, mean and 1 / rstd^2 = variance + eps per row; total receives h.
+
+    x, residual and total are [rows, cols] of one type (fp16, bf16, fp32); gain and shift (cols), mean, rstd and scale
+    (rows) are fp32 vectors; residual, total, gain, shift, mean and rstd may be None.  y is fp16, bf16, fp32 or e4m3, which
+    needs scale: max(max |y| / 448, 2^-126) of the row, y then holding y / scale."""
+    if _marshal_lib is _lib is not None:
+        rc = _marshal.layernorm(x, gain, shift, y, residual, total, scale, mean, rstd, eps, stream)
+        if rc is not None:
+            _check(rc, "alcop_layernorm")
+            return y
+    rows, cols, ldx = _rows("x", x)
+    _, _, ldy = _rows("y", y, rows, cols)
+    for name, t in (("residual", residual), ("total", total)):
+        if t is not None:
+            _rows(name, t, rows, cols, like=x)
+    for name, t, n in (("gain", gain, cols), ("shift", shift, cols), ("scale", scale, rows), ("mean", mean, rows),
+                       ("rstd", rstd, rows)):
+        _vector(name, t, n)
+    _same_place(x, y, gain, shift, residual, total, scale, mean, rstd)
+    _call_on(x, "alcop_layernorm", lib().alcop_layernorm, _ptr(x), _ptr(residual), _ptr(gain), _ptr(shift), _ptr(total), _ptr(y),
+             _ptr(scale), _ptr(mean), _ptr(rstd), rows, cols, ldx, _pitch(residual), _pitch(total), ldy, float(eps), _kind(x),
+             _kind(y), stream=stream)
+    return y
+
+
+def alcop_layernorm_backward_workspace_bytes(rows: int, cols: int) -> int:
+    return int(lib().alcop_layernorm_backward_workspace_bytes(rows, cols))
+
+
+def alcop_layernorm_backward(dy, total, gain, mean, rstd, dx, dgain=None, dshift=None, dtotal=None, workspace=None, stream=None):
+    """Gradients of alcop_layernorm: dx (of x and of the residual), to which the gradient dtotal that arrives at total
+    is added, dgain and dshift.  dy, total, dtotal and dx have one type; dx may be dy or dtotal.  workspace: at least
+    alcop_layernorm_backward_workspace_bytes(rows, cols) bytes, for dgain or dshift."""
+    if _marshal_lib is _lib is not None:
+        rc = _marshal.layernorm_backward(dy, total, gain, mean, rstd, dx, dgain, dshift, dtotal, workspace, stream)
+        if rc is not None:
+            _check(rc, "alcop_layernorm_backward")
+            return dx
+    rows, cols, lddy = _rows("dy", dy)
+    _, _, ldt = _rows("total", total, rows, cols, like=dy)
+    _, _, lddx = _rows("dx", dx, rows, cols, like=dy)
+    if dtotal is not None:
+        _rows("dtotal", dtotal, rows, cols, like=dy)
+    for name, t, n in (("gain", gain, cols), ("dgain", dgain, cols), ("dshift", dshift, cols), ("mean", mean, rows),
+                       ("rstd", rstd, rows)):
+        _vector(name, t, n)
+    _same_place(dy, total, dx, dtotal, gain, mean, rstd, dgain, dshift, workspace)
+    ws, ws_bytes = _workspace(workspace)
+    _call_on(dy, "alcop_layernorm_backward", lib().alcop_layernorm_backward, _ptr(dy), _ptr(total), _ptr(gain), _ptr(mean),
+             _ptr(rstd), _ptr(dtotal), _ptr(dx), _ptr(dgain), _ptr(dshift), rows, cols, lddy, ldt, _pitch(dtotal), lddx, _kind(dy),
+             ws, ws_bytes, stream=stream)
     return dx
 
 

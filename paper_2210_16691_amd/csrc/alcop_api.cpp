@@ -19,6 +19,7 @@
 #include "alcop_model.h"
 #include "alcop_registry.h"
 #include "alcop_convres.hip.h"
+#include "alcop_layernorm.h"
 #include "alcop_linear.h"
 
 namespace alcop {
@@ -1559,7 +1560,7 @@ int alcop_init(void)
   for (const KernelEntry& e : registry())
     if (e.prepare && e.prepare() != hipSuccess) return ALCOP_ERR_LAUNCH;
   if (prepare_direct() != hipSuccess || prepare_copies() != hipSuccess) return ALCOP_ERR_LAUNCH;
-  if (prepare_layers() != hipSuccess) return ALCOP_ERR_LAUNCH;
+  if (prepare_layers() != hipSuccess || prepare_layernorm() != hipSuccess) return ALCOP_ERR_LAUNCH;
   void* scratch = nullptr;
   size_t bytes = 0;
   if (splitk_scratch(&scratch, &bytes) != hipSuccess) return ALCOP_ERR_LAUNCH;

@@ -1,0 +1,239 @@
+// Layer norm of rows and its gradients.
+//
+//   norm      h = x + residual;  mean, var of h over the row;  rstd = 1 / sqrt(var + eps);  y = (h - mean) rstd gain + shift
+//   gradient  with xh = (total - mean) rstd, t = gain dy:  dx = dtotal + rstd (t - mean(t) - xh mean(t xh)),
+//             dgain = sum over rows of dy xh,  dshift = sum over rows of dy
+//
+// As the root-mean-square norm (alcop_rows.hip.h), whose layout of a row this takes over: bound by memory, a row loaded once,
+// held in fp32 registers and stored once, past the caches.
+//
+// The mean is found in two steps.  m = sum(h) / n is off by some 2^-24 of |h|'s mean, which where rows lie far from 0 is not small
+// beside their spread; so the second turn sums d = h - m and d^2 together: mean = m + sum(d) / n, var = mean(d^2) - mean(d)^2, where
+// mean(d) is tiny.  No sum of squares of h itself is formed, and a row needs two turns of the block, as many as the plain
+// two-pass form.  The gradient's two means share a turn.
+#pragma once
+#include "alcop_rows.hip.h"
+
+namespace alcop {
+
+struct LayerNormArgs {
+  const void *x, *residual;
+  const float *gain, *shift;
+  void *total, *y;
+  float *scale, *mean, *rstd;
+  long ldx, ldr, ldt, ldy;
+  int rows, cols;
+  float eps;
+  int out;                     // type of y (3: e4m3)
+};
+
+struct LayerNormGradArgs {
+  const void *dy, *total, *dtotal;
+  const float *gain, *mean, *rstd;
+  void* dx;
+  float *dgain, *dshift;       // sums of the rows of each block, a row of them per block, or null
+  long lddy, ldt, lddt, lddx;
+  int rows, cols;
+};
+
+// gain (1) and shift (0): `none` where there is no vector or no column
+template <class C, class HW>
+__device__ __forceinline__ void load_columns(const float* from, float none, int me, int cols, float (&g)[C::NV][8])
+{
+  if (from != nullptr) {
+    load_gain<C, HW>(from, me, cols, g);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < C::NV; i++)
+#pragma unroll
+    for (int e = 0; e < 8; e++) g[i][e] = none;
+}
+
+constexpr int LAYERNORM_LDS_BYTES = 512;      // two floats per wave and reduction, two reductions, twice
+
+template <class C, class HW>
+__global__ void __launch_bounds__(C::NT) alcop_layernorm_rows(const LayerNormArgs p)
+{
+  constexpr int NV = C::NV, DT = C::DT;
+  const uint32_t lds = HW::lds_base();
+  const int tid = HW::wave_id() * 64 + HW::lane_id();
+  const int me = tid % C::TPR;
+  const long row = (long)HW::block_x() * C::ROWS + tid / C::TPR;
+  if (row >= p.rows) return;                       // a whole wave, where a wave has a row; else never
+
+  const Raw<C> x = load_raw<C, HW>(row_at<DT>(p.x, row, p.ldx), me, p.cols);
+  // ahead of the sums that they do not depend on, where there are registers for them
+  constexpr bool AHEAD = C::TPR < 1024 && NV < 4;
+  float g[NV][8], b[NV][8];
+  if (AHEAD) {
+    load_columns<C, HW>(p.gain, 1.0f, me, p.cols, g);
+    load_columns<C, HW>(p.shift, 0.0f, me, p.cols, b);
+  }
+  float h[NV][8];
+  if (p.residual != nullptr) {
+    const Raw<C> r = load_raw<C, HW>(row_at<DT>(p.residual, row, p.ldr), me, p.cols);
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) h[i][e] = value<C, HW>(x, i, e) + value<C, HW>(r, i, e);
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) h[i][e] = value<C, HW>(x, i, e);
+  }
+  if (p.total != nullptr) store_values<C, DT, HW>((void*)row_at<DT>(p.total, row, p.ldt), me, p.cols, h);
+
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; i++)
+#pragma unroll
+    for (int e = 0; e < 8; e++) s += h[i][e];
+  const float n = (float)p.cols;
+  const float m = row_sum<C::TPR, HW>(s, lds) / n;
+  float sd = 0.f, sdd = 0.f;
+#pragma unroll
+  for (int i = 0; i < NV; i++)
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      // columns past the end hold 0, which is not their part of a sum over h - m
+      const bool there = C::WHOLE ? chunk_at<C>(me, i) < p.cols : chunk_at<C>(me, i) + e < p.cols;
+      h[i][e] = there ? h[i][e] - m : 0.f;
+      sd += h[i][e];
+      sdd += h[i][e] * h[i][e];
+    }
+  row_sums<C::TPR, HW>(sd, sdd, lds + 128);
+  const float off = sd / n, var = sdd / n - off * off;
+  const float rstd = 1.0f / HW::sqrt((var < 0.f ? 0.f : var) + p.eps);       // NaN stays
+  if (!AHEAD) load_columns<C, HW>(p.gain, 1.0f, me, p.cols, g);
+  if (me == 0) {
+    if (p.mean != nullptr) HW::global_store_u32(p.mean + row, __builtin_bit_cast(uint32_t, m + off));
+    if (p.rstd != nullptr) HW::global_store_u32(p.rstd + row, __builtin_bit_cast(uint32_t, rstd));
+  }
+  if (!AHEAD) load_columns<C, HW>(p.shift, 0.0f, me, p.cols, b);
+#pragma unroll
+  for (int i = 0; i < NV; i++)
+#pragma unroll
+    for (int e = 0; e < 8; e++) h[i][e] = HW::fma((h[i][e] - off) * rstd, g[i][e], b[i][e]);
+  store_result<C, HW>(h, p.y, p.ldy, p.out, p.scale, row, me, p.cols, lds + 256);
+}
+
+// A group of TPR threads takes rows g, g + groups, ... and keeps the sums of dgain and dshift for its columns in registers; the
+// waves of a block add theirs where each has a row, alcop_column_sums adds the blocks'.
+template <class C, class HW>
+__global__ void __launch_bounds__(C::NT) alcop_layernorm_grad(const LayerNormGradArgs p, int groups)
+{
+  constexpr int NV = C::NV, DT = C::DT;
+  // rows of more elements than the registers have room for are read again behind the sums
+  constexpr bool HOLD = NV * C::TPR <= 2048;
+  const uint32_t lds = HW::lds_base();
+  const int tid = HW::wave_id() * 64 + HW::lane_id();
+  const int me = tid % C::TPR;
+  const int group = (int)HW::block_x() * C::ROWS + tid / C::TPR;
+  float dg[NV][8], ds[NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; i++)
+#pragma unroll
+    for (int e = 0; e < 8; e++) dg[i][e] = ds[i][e] = 0.f;
+  constexpr bool GAIN_HELD = NV <= 2 && C::TPR < 1024;      // as far as the registers go
+  float g[NV][8];
+  if (GAIN_HELD) load_columns<C, HW>(p.gain, 1.0f, me, p.cols, g);
+  const float n = (float)p.cols;
+  int turn = 0;
+  for (long row = group; row < p.rows; row += groups, turn ^= 1) {
+    const char *dy_row = row_at<DT>(p.dy, row, p.lddy), *h_row = row_at<DT>(p.total, row, p.ldt);
+    Raw<C> dy = load_raw<C, HW>(dy_row, me, p.cols);
+    Raw<C> h = load_raw<C, HW>(h_row, me, p.cols);
+    const char* dt_row = row_at<DT>(p.dtotal, row, p.lddt);
+    Raw<C> dt = {};
+    constexpr bool AHEAD = NV * C::TPR <= 1024;    // of the sums, where there are registers for it
+    if (AHEAD && p.dtotal != nullptr) dt = load_raw<C, HW>(dt_row, me, p.cols);
+    const float mean = __builtin_bit_cast(float, HW::global_load_u32(p.mean + row));
+    const float rstd = __builtin_bit_cast(float, HW::global_load_u32(p.rstd + row));
+    if (!GAIN_HELD) load_columns<C, HW>(p.gain, 1.0f, me, p.cols, g);
+    float st = 0.f, stx = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        // past the end dy is 0 (the mean may be infinite, which 0 times is not 0)
+        const bool there = C::WHOLE ? chunk_at<C>(me, i) < p.cols : chunk_at<C>(me, i) + e < p.cols;
+        const float d = value<C, HW>(dy, i, e), xh = there ? (value<C, HW>(h, i, e) - mean) * rstd : 0.f;
+        st += d * g[i][e];
+        stx += d * g[i][e] * xh;
+        dg[i][e] += d * xh;
+        ds[i][e] += d;
+      }
+    row_sums<C::TPR, HW>(st, stx, lds + 128 * turn);
+    st /= n;
+    stx /= n;
+    if constexpr (!HOLD) {
+      dy = load_raw<C, HW>(dy_row, me, p.cols);
+      h = load_raw<C, HW>(h_row, me, p.cols);
+      load_columns<C, HW>(p.gain, 1.0f, me, p.cols, g);
+    }
+    float dx[NV][8];
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++)
+        dx[i][e] = rstd * (value<C, HW>(dy, i, e) * g[i][e] - st - (value<C, HW>(h, i, e) - mean) * rstd * stx);
+    if (p.dtotal != nullptr) {
+      if (!AHEAD) dt = load_raw<C, HW>(dt_row, me, p.cols);
+#pragma unroll
+      for (int i = 0; i < NV; i++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) dx[i][e] += value<C, HW>(dt, i, e);
+    }
+    store_values<C, DT, HW>((void*)row_at<DT>(p.dx, row, p.lddx), me, p.cols, dx);
+  }
+  // the sums of a block: of dgain, then in the same LDS of dshift
+  auto leave = [&](float(&v)[NV][8], float* to, bool again) __attribute__((always_inline)) {
+    if (to == nullptr) return;
+    if constexpr (C::ROWS > 1) {
+      const uint32_t at = lds + LAYERNORM_LDS_BYTES + (uint32_t)me * 4;
+      const int wave = HW::wave_id();
+      if (again) HW::block_barrier();
+#pragma unroll
+      for (int i = 0; i < NV; i++)
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+          HW::lds_write1(at + (uint32_t)((wave * NV + i) * 8 + e) * 256, __builtin_bit_cast(uint32_t, v[i][e]));
+      HW::wait_lds();
+      HW::block_barrier();
+      if (wave == 0) {
+#pragma unroll
+        for (int w = 1; w < C::ROWS; w++)
+#pragma unroll
+          for (int i = 0; i < NV; i++)
+#pragma unroll
+            for (int e = 0; e < 8; e++)
+              v[i][e] += __builtin_bit_cast(float, HW::lds_read4(at + (uint32_t)((w * NV + i) * 8 + e) * 256));
+      }
+      HW::wait_lds();
+      if (wave > 0) return;
+    }
+    store_values<C, 2, HW>(to + (long)HW::block_x() * p.cols, me, p.cols, v);
+  };
+  leave(dg, p.dgain, false);
+  leave(ds, p.dshift, p.dgain != nullptr);
+}
+
+// the sums of both gradients in one launch (blocks y = 0 and 1)
+struct TwoColumnSums {
+  ColumnSumArgs of[2];
+};
+template <class HW>
+__global__ void __launch_bounds__(SUM_THREADS) alcop_two_column_sums(const TwoColumnSums p)
+{
+  column_sums<HW>(HW::block_y() ? p.of[1] : p.of[0]);
+}
+
+template <class C>
+constexpr int layernorm_grad_lds()
+{
+  return LAYERNORM_LDS_BYTES + (C::ROWS > 1 ? C::ROWS * C::NV * 8 * 64 * 4 : 0);
+}
+
+}  // namespace alcop

@@ -91,6 +91,26 @@ __device__ __forceinline__ float row_sum(float v, uint32_t at)
   }
   return v;
 }
+// two sums for one turn of the block; `at`: 8 bytes a wave
+template <int TPR, class HW>
+__device__ __forceinline__ void row_sums(float& a, float& b, uint32_t at)
+{
+  a = wave_sum<HW>(a);
+  b = wave_sum<HW>(b);
+  if constexpr (TPR > 64) {
+    HW::lds_write(at + 8 * HW::wave_id(), u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)});
+    HW::wait_lds();
+    HW::block_barrier();
+    a = b = 0.f;
+#pragma unroll
+    for (int w = 0; w < TPR / 64; w++) {
+      const u32x2 t = HW::lds_read8(at + 8 * w);
+      const uint32_t ta = t[0], tb = t[1];         // a cast of t[1] itself takes t[0]
+      a += __builtin_bit_cast(float, ta);
+      b += __builtin_bit_cast(float, tb);
+    }
+  }
+}
 template <int TPR, class HW>
 __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t at)
 {
@@ -254,6 +274,35 @@ __device__ __forceinline__ void divide_row(float (&v)[NV][8], float scale)
 }
 
 // ---- norm, 8 bits ------------------------------------------------------------------------------------------------
+// A row h of the result, in type `out` (3: e4m3, whose scale goes to scale[row]); `at`: LDS of the row's maximum.
+template <class C, class HW>
+__device__ __forceinline__ void store_result(float (&h)[C::NV][8], void* base, long ld, int out, float* scale_of, long row, int me,
+                                             int cols, uint32_t at)
+{
+  constexpr int NV = C::NV;
+  if (out == 3) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const uint32_t b = __builtin_bit_cast(uint32_t, h[i][e]) & 0x7fffffffu;
+        // a thread past the row's end holds zeros, which a gain of its own must not turn into NaN
+        if (chunk_at<C>(me, i) + e < cols) top = b > top ? b : top;
+      }
+    top = row_max<C::TPR, HW>(top, at);
+    const float peak = __builtin_bit_cast(float, top) / 448.0f;
+    const float scale = peak < 1.17549435e-38f ? 1.17549435e-38f : peak;     // NaN stays
+    if (me == 0) HW::global_store_u32(scale_of + row, __builtin_bit_cast(uint32_t, scale));
+    divide_row<HW>(h, scale);
+  }
+  char* y = (char*)base + row * ld * (out == 3 ? 1 : out == 2 ? 4 : 2);
+  if (out == 3)
+    store_values<C, 3, HW>(y, me, cols, h);
+  else
+    by_type(out, [&](auto t) __attribute__((always_inline)) { store_values<C, decltype(t)::value, HW>(y, me, cols, h); });
+}
+
 template <class C, class HW>
 __global__ void __launch_bounds__(C::NT) alcop_norm_rows(const NormArgs p)
 {
@@ -301,27 +350,7 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_rows(const NormArgs p)
 #pragma unroll
       for (int e = 0; e < 8; e++) h[i][e] = h[i][e] * rstd * g[i][e];
   }
-  if (out == 3) {
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < NV; i++)
-#pragma unroll
-      for (int e = 0; e < 8; e++) {
-        const uint32_t b = __builtin_bit_cast(uint32_t, h[i][e]) & 0x7fffffffu;
-        // a thread past the row's end holds zeros, which a gain of its own must not turn into NaN
-        if (chunk_at<C>(me, i) + e < p.cols) top = b > top ? b : top;
-      }
-    top = row_max<C::TPR, HW>(top, lds + 64);
-    const float peak = __builtin_bit_cast(float, top) / 448.0f;
-    const float scale = peak < 1.17549435e-38f ? 1.17549435e-38f : peak;     // NaN stays
-    if (me == 0) HW::global_store_u32(p.scale + row, __builtin_bit_cast(uint32_t, scale));
-    divide_row<HW>(h, scale);
-  }
-  char* y = (char*)p.y + row * p.ldy * (out == 3 ? 1 : out == 2 ? 4 : 2);
-  if (out == 3)
-    store_values<C, 3, HW>(y, me, p.cols, h);
-  else
-    by_type(out, [&](auto t) __attribute__((always_inline)) { store_values<C, decltype(t)::value, HW>(y, me, p.cols, h); });
+  store_result<C, HW>(h, p.y, p.ldy, out, p.scale, row, me, p.cols, lds + 64);
 }
 
 // ---- gradients of the norm ------------------------------------------------------------------------------------------
@@ -412,7 +441,7 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_grad(const NormGradArgs p, i
 // out[j] = sum over i of partial[i][j], in a fixed order: 32 columns a block, 32 runs of rows, then the runs.
 constexpr int SUM_THREADS = 1024, SUM_COLS = 32;
 template <class HW>
-__global__ void __launch_bounds__(SUM_THREADS) alcop_column_sums(const ColumnSumArgs p)
+__device__ __forceinline__ void column_sums(const ColumnSumArgs& p)
 {
   const uint32_t lds = HW::lds_base();
   const int tid = HW::wave_id() * 64 + HW::lane_id();
@@ -432,6 +461,11 @@ __global__ void __launch_bounds__(SUM_THREADS) alcop_column_sums(const ColumnSum
 #pragma unroll 4
   for (int i = 0; i < SUM_THREADS / SUM_COLS; i++) t += __builtin_bit_cast(float, HW::lds_read4(lds + 4 * (i * SUM_COLS + c)));
   if (tid < SUM_COLS && j < p.cols) HW::global_store_u32(p.out + j, __builtin_bit_cast(uint32_t, t));
+}
+template <class HW>
+__global__ void __launch_bounds__(SUM_THREADS) alcop_column_sums(const ColumnSumArgs p)
+{
+  column_sums<HW>(p);
 }
 
 // ---- gradient of an activation, sums for the bias ----------------------------------------------------------------------

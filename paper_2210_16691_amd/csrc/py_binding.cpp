@@ -30,6 +30,8 @@ struct Api {
   decltype(&alcop_rmsnorm) rmsnorm = nullptr;
   decltype(&alcop_rmsnorm_backward) rmsnorm_backward = nullptr;
   decltype(&alcop_quantize_rows) quantize_rows = nullptr;
+  decltype(&alcop_layernorm) layernorm = nullptr;
+  decltype(&alcop_layernorm_backward) layernorm_backward = nullptr;
 } api;
 
 PyObject* sched_type = nullptr;   // the binding's ctypes mirror of alcop_sched
@@ -471,6 +473,62 @@ PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n)
   });
 }
 
+// layernorm(x, gain, shift, y, residual, total, scale, mean, rstd, eps, stream)
+PyObject* layernorm(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+  return guarded([&] {
+    need(api.layernorm && n == 11 && a[3] != Py_None);
+    const Rows x(a[0]), y(a[3], x.rows, x.cols, x, false), r(a[4], x.rows, x.cols, x, true), h(a[5], x.rows, x.cols, x, true);
+    const at::Tensor *g = floats(a[1], x.cols, x), *b = floats(a[2], x.cols, x), *s = floats(a[6], x.rows, x);
+    const at::Tensor *m = floats(a[7], x.rows, x), *d = floats(a[8], x.rows, x);
+    const float eps = number(a[9]);
+    void* st = stream_on(x, a[10]);
+    const void *px = x.in(), *pr = r.in(), *pg = in(g), *pb = in(b);
+    void *ph = h.out(), *py = y.out(), *ps = out(s), *pm = out(m), *pd = out(d);
+    return unlocked([&] {
+      return api.layernorm(px, pr, pg, pb, ph, py, ps, pm, pd, x.rows, x.cols, x.ld, r.ld, h.ld, y.ld, eps, x.type, y.type, st);
+    });
+  });
+}
+
+// layernorm_backward(dy, total, gain, mean, rstd, dx, dgain, dshift, dtotal, workspace, stream)
+PyObject* layernorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+  return guarded([&] {
+    need(api.layernorm_backward && n == 11 && a[1] != Py_None && a[5] != Py_None);
+    const Rows dy(a[0]);
+    const int R = dy.rows, N = dy.cols;
+    const Rows h(a[1], R, N, dy, true), dx(a[5], R, N, dy, true), dt(a[8], R, N, dy, true);
+    const at::Tensor *g = floats(a[2], N, dy), *m = floats(a[3], R, dy), *d = floats(a[4], R, dy);
+    const at::Tensor *dg = floats(a[6], N, dy), *db = floats(a[7], N, dy);
+    const Scratch ws(a[9], dy);
+    void* st = stream_on(dy, a[10]);
+    const void *py = dy.in(), *ph = h.in(), *pg = in(g), *pm = in(m), *pd = in(d), *pt = dt.in();
+    void *ox = dx.out(), *og = out(dg), *ob = out(db);
+    return unlocked([&] {
+      return api.layernorm_backward(py, ph, pg, pm, pd, pt, ox, og, ob, R, N, dy.ld, h.ld, dt.ld, dx.ld, dy.type, ws.p, ws.bytes, st);
+    });
+  });
+}
+
+// init_more(layernorm, layernorm_backward): addresses in the library
+PyObject* init_more(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+  constexpr int COUNT = 2;
+  if (n != COUNT) {
+    PyErr_Format(PyExc_TypeError, "init_more takes %d addresses", COUNT);
+    return nullptr;
+  }
+  void* f[COUNT];
+  for (int i = 0; i < COUNT; i++) {
+    f[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+  }
+  api.layernorm = (decltype(api.layernorm))f[0];
+  api.layernorm_backward = (decltype(api.layernorm_backward))f[1];
+  Py_RETURN_NONE;
+}
+
 // init_layers(linear, linear_backward, rmsnorm, rmsnorm_backward, quantize_rows): addresses in the library
 PyObject* init_layers(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
@@ -526,6 +584,9 @@ PyMethodDef methods[] = {
     {"rmsnorm", (PyCFunction)(void*)rmsnorm, METH_FASTCALL, "root-mean-square norm of rows"},
     {"rmsnorm_backward", (PyCFunction)(void*)rmsnorm_backward, METH_FASTCALL, "gradients of the norm"},
     {"quantize_rows", (PyCFunction)(void*)quantize_rows, METH_FASTCALL, "rows to 8 bits"},
+    {"init_more", (PyCFunction)(void*)init_more, METH_FASTCALL, "set the entry points of layer norm, experts and losses"},
+    {"layernorm", (PyCFunction)(void*)layernorm, METH_FASTCALL, "layer norm of rows"},
+    {"layernorm_backward", (PyCFunction)(void*)layernorm_backward, METH_FASTCALL, "gradients of the layer norm"},
     {"conv_any", (PyCFunction)(void*)conv_any, METH_FASTCALL, "convolution of unaligned operands"},
     {nullptr, nullptr, 0, nullptr}};
 

@@ -4,7 +4,6 @@ clang vector types), into _build/emu/libalcop_emu.so."""
 from __future__ import annotations
 
 import concurrent.futures as cf
-import glob
 import os
 import subprocess
 
@@ -18,16 +17,20 @@ FLAGS = [os.environ.get("EMU_OPT", "-O1"), "-std=c++17", "-fPIC", "-D__HIP_PLATF
          "-I" + HERE, "-D__launch_bounds__(...)=", "-Wno-psabi", "-Wno-pass-failed"]
 
 
-def _newest_dep() -> float:
-    deps = glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(HERE, "*.h")) + \
-        glob.glob(os.path.join(ROOT, "include", "*.h")) + [os.path.join(HERE, "emu_lib.cpp"), os.path.join(HERE, "emu_linear.cpp")]
-    return max(os.path.getmtime(d) for d in deps)
+def _newest_dep(obj: str) -> float:
+    """Newest modification time among the files this object was last compiled from (the compiler's own list; none yet: never
+    up to date)."""
+    if not os.path.exists(obj + ".d"):
+        return float("inf")
+    words = open(obj + ".d").read().replace("\\\n", " ").split()
+    files = [w for w in words[1:] if not w.endswith(":")]
+    return max((os.path.getmtime(f) if os.path.exists(f) else float("inf")) for f in files)
 
 
 def _compile(job) -> str:
     src, obj, extra = job
-    if not os.path.exists(obj) or os.path.getmtime(obj) < max(os.path.getmtime(src), _newest_dep()):
-        subprocess.check_call([CXX] + FLAGS + extra + ["-c", src, "-o", obj])
+    if not os.path.exists(obj) or os.path.getmtime(obj) < _newest_dep(obj):
+        subprocess.check_call([CXX] + FLAGS + extra + ["-MD", "-MF", obj + ".d", "-c", src, "-o", obj])
     return obj
 
 
@@ -36,10 +39,11 @@ def build() -> str:
     emu = os.path.join(HERE, "emu_lib.cpp")
     jobs = [(emu, os.path.join(OUT, "emu_part%d.o" % p), ["-DEMU_PART=%d" % p]) for p in range(8)]
     jobs.append((emu, os.path.join(OUT, "emu_main.o"), ["-DEMU_PART=-1"]))
-    for name in ("alcop_api.cpp", "alcop_model.cpp", "alcop_linear.cpp"):
+    for name in ("alcop_api.cpp", "alcop_model.cpp", "alcop_linear.cpp", "alcop_layernorm.cpp"):
         jobs.append((os.path.join(CSRC, name), os.path.join(OUT, name + ".o"), []))
     lin = os.path.join(HERE, "emu_linear.cpp")
     jobs += [(lin, os.path.join(OUT, "emu_linear%d.o" % p), ["-DEMU_PART=%d" % p]) for p in range(5)]
+    jobs.append((os.path.join(HERE, "emu_layernorm.cpp"), os.path.join(OUT, "emu_layernorm.o"), []))
     with cf.ThreadPoolExecutor(max_workers=8) as ex:
         objs = list(ex.map(_compile, jobs))
     if not os.path.exists(LIB) or any(os.path.getmtime(o) > os.path.getmtime(LIB) for o in objs):
