@@ -526,6 +526,80 @@ int alcop_layernorm_backward(const void* dy, const void* total, const void* gain
                              void* hip_stream);
 
 /*
+ * Products grouped by expert: the rows of A are sorted by group, and each group has weights of its own.  For the rows
+ * i = offsets[g] .. offsets[g + 1] - 1 of every group g
+ *     Z[i][j] = alpha * scale_a[i] * scale_w[g][j] * sum_k A(i,k) W_g(k,j) + bias[g][j];   C[i][j] = act(Z[i][j])
+ * as alcop_linear has it, `pre` receiving Z.  (scale_a holds, for instance, what a router weighs a row with.)
+ *   A: row-major rows x K.  W_g: at W + g * strideW elements, transB = 0 row-major K x N, transB = 1 stored N x K.
+ *   offsets: DEVICE, groups + 1 32-bit numbers that rise from 0 or more to `rows` or less; a group may have no row.  Rows
+ *     before the first and behind the last are not computed, and C and pre are left as they are there.  (Numbers that do not rise or
+ *     are out of range are taken as the nearest in range: which rows are then computed is not defined, no access is out of bounds.)
+ *   tail: bias and scale_w are groups x N fp32 values without gaps; residual is NULL.  ALCOP_E4M3 operands, ALCOP_FP32_SUMS, act,
+ *     types, alignment and pitches as for alcop_linear, but that bias and scale_w may start at any 4 bytes; strideW a multiple of 8
+ *     (ALCOP_E4M3: 16) elements, 0 if all groups have the same.  ALCOP_LINEAR_KERNEL names a kernel here too.
+ * One launch.  1 <= groups < 2^24.  The same call gives the same bits.
+ */
+int alcop_grouped_linear(const void* A, const void* W, const void* offsets, void* C, int rows, int groups, int N, int K,
+                         long lda, long ldw, long strideW, long ldc, int transB, alcop_dtype in, alcop_dtype out,
+                         const alcop_linear_tail* tail /* host, may be NULL */, void* hip_stream);
+
+/*
+ * Its gradients, as alcop_linear_backward has them.  With dZ = dC * act'(pre), rounded to the type `in`, for every group
+ *     dA = alpha * dZ . W_g^T,   dW_g = alpha * A_g^T . dZ_g  (stored as W_g is),   dbias[g][j] = sum of dZ over the group's rows
+ * before the rounding; dW_g and dbias[g] of a group without rows are 0, rows of no group are left as they are in dA.
+ *   dA, dW, dbias may be NULL (not all).  Types, alignment and pitches as for alcop_linear_backward; dW_g at dW + g * stridedW,
+ *     which do not overlap; dbias: groups x N fp32 values.  groups <= 65535.
+ *   workspace: DEVICE, 16-byte aligned, at least alcop_grouped_linear_backward_workspace_bytes(rows, groups, N, K) bytes,
+ *     needed if act != 0 or dbias is given; as for alcop_linear_backward.
+ * For dW, all rows of A and of dZ (dC without an activation), 128 more counted, span less than 2 GiB each; else ALCOP_ERR_SIZE,
+ * before anything is launched.  Up to four launches; sums have a fixed order, without atomics.
+ */
+size_t alcop_grouped_linear_backward_workspace_bytes(int rows, int groups, int N, int K);
+int alcop_grouped_linear_backward(const void* dC, const void* A, const void* W, const void* pre, const void* offsets,
+                                  void* dA, void* dW, void* dbias, int rows, int groups, int N, int K, long lddc, long lda,
+                                  long ldw, long strideW, long ldp, long ldda, long lddw, long stridedW, int transB,
+                                  alcop_dtype in, alcop_dtype out, float alpha, int act, void* workspace,
+                                  size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Cross entropy of rows against their product with a vocabulary's vectors, logits not kept:
+ *     z[t][v] = alpha * sum_k X(t,k) W(v,k);   lse[t] = log sum_v exp(z[t][v]);   loss[t] = lse[t] - z[t][labels[t]]
+ * in fp32 from the accumulators on.
+ *   X: row-major rows x K, W: vocab x K (a layer's weights: out x in), both ALCOP_F16 or ALCOP_BF16; alpha > 0.
+ *   labels: DEVICE, 64-bit numbers.  A row whose label is no column of the vocabulary (below 0, or vocab and more) does not count:
+ *     its loss is 0, and so is its gradient; its lse is that of its logits.
+ *   loss, lse (may be NULL): rows fp32 values.  An infinite logit makes them infinite or NaN as the formulas do.
+ *   workspace: DEVICE, 16-byte aligned, at least alcop_linear_cross_entropy_workspace_bytes(rows, vocab, K) bytes (which
+ *     returns 0 for arguments no call accepts): 8 bytes for each row and 64 columns at most.  Overwritten; calls that share it,
+ *     captured ones too, must be ordered on one stream.
+ * rows and vocab are free, K is a multiple of 8; X, W: 16-byte aligned, pitches multiples of 8 elements; labels 8-byte aligned.
+ * Outputs and workspace overlap nothing else.  Two launches; sums have a fixed order.
+ */
+size_t alcop_linear_cross_entropy_workspace_bytes(int rows, int vocab, int K);
+int alcop_linear_cross_entropy(const void* X, const void* W, const void* labels, void* loss, void* lse, int rows, int vocab,
+                               int K, long ldx, long ldw, float alpha, alcop_dtype in, void* workspace,
+                               size_t workspace_bytes, void* hip_stream);
+
+/*
+ * Its gradients: with G[t][v] = dloss[t] * (exp(z[t][v] - lse[t]) - (v == labels[t])), 0 in rows that do not count,
+ *     dX = alpha * G . W,   dW = alpha * G^T . X
+ * where G is rounded to the type `in` (the products take 16-bit operands), in fp16 times a power of two that takes the largest
+ * |dloss| to 2^14 and more, so that the small numbers of a large vocabulary and a mean over many rows are not lost.
+ *   lse: as alcop_linear_cross_entropy left it.  dloss: rows fp32 values, NULL = 1.
+ *   dX (rows x K), dW (vocab x K): type `out`, which is `in` or ALCOP_F32; one may be NULL.  16-byte aligned, pitches multiples of 8.
+ *   workspace: DEVICE, 16-byte aligned, at least alcop_linear_cross_entropy_backward_workspace_bytes(rows, vocab, K) bytes,
+ *     as above: G of a piece of the vocabulary (up to 256 MiB, or rows x 512 bytes if that is more) and, if there are several
+ *     pieces, dX in fp32.
+ * For dW, all rows of X and of a piece of G, 128 more counted, span less than 2 GiB each; else ALCOP_ERR_SIZE, before anything is
+ * launched.  Up to three launches a piece and two more; sums have a fixed order, without atomics.
+ */
+size_t alcop_linear_cross_entropy_backward_workspace_bytes(int rows, int vocab, int K);
+int alcop_linear_cross_entropy_backward(const void* X, const void* W, const void* labels, const void* lse, const void* dloss,
+                                        void* dX, void* dW, int rows, int vocab, int K, long ldx, long ldw, long lddx,
+                                        long lddw, float alpha, alcop_dtype in, alcop_dtype out, void* workspace,
+                                        size_t workspace_bytes, void* hip_stream);
+
+/*
  * Feasibility of a schedule for a problem, without launching (the checks the paper's
  * schedule rules and "compile fail" marks stand for, Sec. 3.1 and Fig. 9): a kernel with
  * these parameters is built; the LDS ring fits 160 KB; the outstanding-load count

@@ -181,6 +181,20 @@ def _declare(L: ctypes.CDLL) -> ctypes.CDLL:
     L.alcop_layernorm_backward_workspace_bytes.argtypes = [i, i]
     L.alcop_layernorm_backward.restype = i
     L.alcop_layernorm_backward.argtypes = [vp] * 9 + [i, i] + [l] * 4 + [i, vp, sz, vp]
+    L.alcop_grouped_linear.restype = i
+    L.alcop_grouped_linear.argtypes = [vp] * 4 + [i] * 4 + [l] * 4 + [i, i, i, tp, vp]
+    L.alcop_grouped_linear_backward_workspace_bytes.restype = sz
+    L.alcop_grouped_linear_backward_workspace_bytes.argtypes = [i] * 4
+    L.alcop_grouped_linear_backward.restype = i
+    L.alcop_grouped_linear_backward.argtypes = [vp] * 8 + [i] * 4 + [l] * 8 + [i, i, i, f, i, vp, sz, vp]
+    L.alcop_linear_cross_entropy_workspace_bytes.restype = sz
+    L.alcop_linear_cross_entropy_workspace_bytes.argtypes = [i] * 3
+    L.alcop_linear_cross_entropy.restype = i
+    L.alcop_linear_cross_entropy.argtypes = [vp] * 5 + [i] * 3 + [l, l, f, i, vp, sz, vp]
+    L.alcop_linear_cross_entropy_backward_workspace_bytes.restype = sz
+    L.alcop_linear_cross_entropy_backward_workspace_bytes.argtypes = [i] * 3
+    L.alcop_linear_cross_entropy_backward.restype = i
+    L.alcop_linear_cross_entropy_backward.argtypes = [vp] * 7 + [i] * 3 + [l] * 4 + [f, i, i, vp, sz, vp]
     L.alcop_init.restype = i
     L.alcop_init.argtypes = []
     L.alcop_strerror.restype = ctypes.c_char_p
@@ -206,7 +220,9 @@ def lib() -> ctypes.CDLL:
         m.init_layers(*[ctypes.cast(f, ctypes.c_void_p).value for f in
                         (L.alcop_linear, L.alcop_linear_backward, L.alcop_rmsnorm, L.alcop_rmsnorm_backward,
                          L.alcop_quantize_rows)])
-        m.init_more(*[ctypes.cast(f, ctypes.c_void_p).value for f in (L.alcop_layernorm, L.alcop_layernorm_backward)])
+        m.init_more(*[ctypes.cast(f, ctypes.c_void_p).value for f in
+                        (L.alcop_layernorm, L.alcop_layernorm_backward, L.alcop_grouped_linear,
+                         L.alcop_grouped_linear_backward, L.alcop_linear_cross_entropy, L.alcop_linear_cross_entropy_backward)])
         _lib, _marshal, _marshal_lib = L, m, L
     return _lib
 
@@ -644,6 +660,170 @@ def alcop_layernorm_backward(dy, total, gain, mean, rstd, dx, dgain=None, dshift
              _ptr(rstd), _ptr(dtotal), _ptr(dx), _ptr(dgain), _ptr(dshift), rows, cols, lddy, ldt, _pitch(dtotal), lddx, _kind(dy),
              ws, ws_bytes, stream=stream)
     return dx
+
+
+def _group_shapes(A, W, offsets, transB):
+    """Checks rows, groups of weights and their offsets; returns (rows, groups, N, K, lda, ldw, strideW)."""
+    import torch
+    rows, K, lda = _rows("A", A)
+    ldw, stride = _group_pitches("W", W)
+    if W.dtype != A.dtype:
+        raise ValueError("W is %s, expected %s" % (W.dtype, A.dtype))
+    N, Kw = (W.shape[1], W.shape[2]) if transB else (W.shape[2], W.shape[1])
+    if Kw != K:
+        raise ValueError("reduction extents differ: A has K = %d, W has K = %d" % (K, Kw))
+    if offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.shape[0] != W.shape[0] + 1 or not offsets.is_contiguous():
+        raise ValueError("offsets must be a contiguous int32 vector of groups + 1 = %d numbers" % (W.shape[0] + 1))
+    return rows, W.shape[0], N, K, lda, ldw, stride
+
+
+def _group_pitches(name, t):
+    if t.dim() != 3 or t.numel() == 0:
+        raise ValueError("%s must be a 3-D tensor with at least one element" % name)
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError("%s: the last dimension must be contiguous" % name)
+    ld = t.shape[2] if t.shape[1] == 1 else t.stride(1)
+    return ld, t.shape[1] * ld if t.shape[0] == 1 else t.stride(0)
+
+
+def _per_group(name, t, groups, n):
+    import torch
+    if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (groups, n) or not t.is_contiguous()):
+        raise ValueError("%s must be a contiguous fp32 matrix of %d x %d values" % (name, groups, n))
+
+
+def alcop_grouped_linear(A, W, offsets, C, transB=False, alpha=1.0, bias=None, act=0, pre=None, scale_a=None, scale_w=None,
+                         stream=None, fp32_sums=False):
+    """Rows offsets[g] .. offsets[g+1]-1 of C = act(Z) with Z = alpha * scale_a[i] * scale_w[g,j] * A.W[g] + bias[g,j]; `pre`
+    receives Z.  Rows of no group are left as they are.
+
+    A is [rows,K], sorted by group, W [groups,K,N] or, with transB, [groups,N,K]; both fp16, bf16 or, with transB, e4m3.
+    offsets: groups + 1 rising int32 numbers on the GPU, from 0 or more to `rows` or less.  C and pre are [rows,N] of one type:
+    fp16, bf16 or fp32.  bias and scale_w are fp32 [groups,N], scale_a an fp32 vector of rows values.  act and the sums of
+    e4m3 operands (fp32_sums): as for alcop_linear."""
+    if fp32_sums:
+        act = int(act) | FP32_SUMS
+    if _marshal_lib is _lib is not None:
+        rc = _marshal.grouped_linear(A, W, offsets, C, transB, alpha, bias, act, pre, scale_a, scale_w, stream)
+        if rc is not None:
+            _check(rc, "alcop_grouped_linear")
+            return C
+    rows, groups, N, K, lda, ldw, stride = _group_shapes(A, W, offsets, transB)
+    _, _, ldc = _rows("C", C, rows, N)
+    _dtype_code(C)
+    if pre is not None:
+        _rows("pre", pre, rows, N, like=C)
+    _per_group("bias", bias, groups, N)
+    _per_group("scale_w", scale_w, groups, N)
+    _vector("scale_a", scale_a, rows)
+    _same_place(A, W, offsets, C, bias, pre, scale_a, scale_w)
+    p = lambda t: None if t is None else t.data_ptr()
+    tail = LinearTail(float(alpha), p(bias), int(act), None, 0, p(pre), _pitch(pre), p(scale_a), p(scale_w))
+    _call_on(A, "alcop_grouped_linear", lib().alcop_grouped_linear, _ptr(A), _ptr(W), _ptr(offsets), _ptr(C), rows, groups, N, K,
+             lda, ldw, stride, ldc, int(transB), _kind(A), _kind(C), ctypes.byref(tail), stream=stream)
+    return C
+
+
+def alcop_grouped_linear_backward_workspace_bytes(rows: int, groups: int, N: int, K: int) -> int:
+    return int(lib().alcop_grouped_linear_backward_workspace_bytes(rows, groups, N, K))
+
+
+def alcop_grouped_linear_backward(dC, A, W, offsets, dA=None, dW=None, dbias=None, pre=None, act=0, alpha=1.0, transB=False,
+                                  workspace=None, stream=None):
+    """Gradients of alcop_grouped_linear: with dZ = dC * act'(pre), dA = alpha * dZ.W[g]^T, dW[g] = alpha * A_g^T.dZ_g (stored as
+    W[g] is) and dbias[g] the column sums of dZ over the group's rows (0 for a group without); what is None is left
+    out.  dC, A, W, pre have one type, fp16 or bf16; dA and dW that one or both fp32; dbias fp32 [groups,N].  workspace: at
+    least alcop_grouped_linear_backward_workspace_bytes(rows, groups, N, K) bytes, for an activation or dbias."""
+    if _marshal_lib is _lib is not None:
+        rc = _marshal.grouped_linear_backward(dC, A, W, offsets, dA, dW, dbias, pre, act, alpha, transB, workspace, stream)
+        if rc is not None:
+            _check(rc, "alcop_grouped_linear_backward")
+            return
+    rows, groups, N, K, lda, ldw, stride = _group_shapes(A, W, offsets, transB)
+    _, _, lddc = _rows("dC", dC, rows, N, like=A)
+    if dA is not None:
+        _rows("dA", dA, rows, K, like=dW)
+    lddw = stride_dw = 0
+    if dW is not None:
+        if tuple(dW.shape) != tuple(W.shape):
+            raise ValueError("dW is %s, expected %s" % (tuple(dW.shape), tuple(W.shape)))
+        lddw, stride_dw = _group_pitches("dW", dW)
+    if pre is not None:
+        _rows("pre", pre, rows, N, like=A)
+    _per_group("dbias", dbias, groups, N)
+    _same_place(dC, A, W, offsets, dA, dW, dbias, pre, workspace)
+    ws, ws_bytes = _workspace(workspace)
+    out = dA if dA is not None else dW
+    _call_on(dC, "alcop_grouped_linear_backward", lib().alcop_grouped_linear_backward, _ptr(dC), _ptr(A), _ptr(W), _ptr(pre),
+             _ptr(offsets), _ptr(dA), _ptr(dW), _ptr(dbias), rows, groups, N, K, lddc, lda, ldw, stride, _pitch(pre), _pitch(dA),
+             lddw, stride_dw, int(transB), _kind(dC), _kind(dC if out is None else out), float(alpha), int(act), ws, ws_bytes,
+             stream=stream)
+
+
+def _loss_shapes(X, W, labels):
+    """Checks rows, a vocabulary's vectors and labels; returns (rows, vocab, K, ldx, ldw)."""
+    import torch
+    rows, K, ldx = _rows("X", X)
+    vocab, Kw, ldw = _rows("W", W, like=X)
+    if Kw != K:
+        raise ValueError("reduction extents differ: X has K = %d, W has K = %d" % (K, Kw))
+    if labels.dtype != torch.int64 or labels.dim() != 1 or labels.shape[0] != rows or not labels.is_contiguous():
+        raise ValueError("labels must be a contiguous int64 vector of %d numbers" % rows)
+    return rows, vocab, K, ldx, ldw
+
+
+def alcop_linear_cross_entropy_workspace_bytes(rows: int, vocab: int, K: int) -> int:
+    return int(lib().alcop_linear_cross_entropy_workspace_bytes(rows, vocab, K))
+
+
+def alcop_linear_cross_entropy(X, W, labels, loss, lse=None, workspace=None, alpha=1.0, stream=None):
+    """loss = lse - z[label] with z = alpha * X.W^T and lse = log(sum(exp(z))) per row, without keeping z.
+
+    X is [rows,K], W [vocab,K] (a layer's weights), both fp16 or bf16; labels int64; loss and lse fp32 vectors of rows values,
+    lse may be None.  A row whose label is no column of the vocabulary does not count: its loss is 0.  workspace: at least
+    alcop_linear_cross_entropy_workspace_bytes(rows, vocab, K) bytes.  alpha > 0."""
+    if _marshal_lib is _lib is not None:
+        rc = _marshal.cross_entropy(X, W, labels, loss, lse, workspace, alpha, stream)
+        if rc is not None:
+            _check(rc, "alcop_linear_cross_entropy")
+            return loss
+    rows, vocab, K, ldx, ldw = _loss_shapes(X, W, labels)
+    _vector("loss", loss, rows)
+    _vector("lse", lse, rows)
+    _same_place(X, W, labels, loss, lse, workspace)
+    ws, ws_bytes = _workspace(workspace)
+    _call_on(X, "alcop_linear_cross_entropy", lib().alcop_linear_cross_entropy, _ptr(X), _ptr(W), _ptr(labels), _ptr(loss), _ptr(lse),
+             rows, vocab, K, ldx, ldw, float(alpha), _kind(X), ws, ws_bytes, stream=stream)
+    return loss
+
+
+def alcop_linear_cross_entropy_backward_workspace_bytes(rows: int, vocab: int, K: int) -> int:
+    return int(lib().alcop_linear_cross_entropy_backward_workspace_bytes(rows, vocab, K))
+
+
+def alcop_linear_cross_entropy_backward(X, W, labels, lse, workspace, dX=None, dW=None, dloss=None, alpha=1.0, stream=None):
+    """Gradients of alcop_linear_cross_entropy: with G = dloss * (exp(z - lse) - one(label)), 0 in rows that do not count,
+    dX = alpha * G.W and dW = alpha * G^T.X; what is None is left out.  lse as the forward call left it; dloss: an fp32 vector of rows
+    values, None = 1.  dX and dW have X's type, or one or both fp32.  workspace: at least
+    alcop_linear_cross_entropy_backward_workspace_bytes(rows, vocab, K) bytes."""
+    if _marshal_lib is _lib is not None:
+        rc = _marshal.cross_entropy_backward(X, W, labels, lse, workspace, dX, dW, dloss, alpha, stream)
+        if rc is not None:
+            _check(rc, "alcop_linear_cross_entropy_backward")
+            return
+    rows, vocab, K, ldx, ldw = _loss_shapes(X, W, labels)
+    if dX is not None:
+        _rows("dX", dX, rows, K, like=dW)
+    if dW is not None:
+        _rows("dW", dW, vocab, K)
+    _vector("lse", lse, rows)
+    _vector("dloss", dloss, rows)
+    _same_place(X, W, labels, lse, dloss, dX, dW, workspace)
+    ws, ws_bytes = _workspace(workspace)
+    out = dX if dX is not None else dW
+    _call_on(X, "alcop_linear_cross_entropy_backward", lib().alcop_linear_cross_entropy_backward, _ptr(X), _ptr(W), _ptr(labels),
+             _ptr(lse), _ptr(dloss), _ptr(dX), _ptr(dW), rows, vocab, K, ldx, ldw, _pitch(dX), _pitch(dW), float(alpha), _kind(X),
+             _kind(X if out is None else out), ws, ws_bytes, stream=stream)
 
 
 def alcop_quantize_rows(x, y, scale, stream=None):

@@ -19,8 +19,10 @@
 #include "alcop_model.h"
 #include "alcop_registry.h"
 #include "alcop_convres.hip.h"
+#include "alcop_grouped.h"
 #include "alcop_layernorm.h"
 #include "alcop_linear.h"
+#include "alcop_loss.h"
 
 namespace alcop {
 
@@ -1560,7 +1562,9 @@ int alcop_init(void)
   for (const KernelEntry& e : registry())
     if (e.prepare && e.prepare() != hipSuccess) return ALCOP_ERR_LAUNCH;
   if (prepare_direct() != hipSuccess || prepare_copies() != hipSuccess) return ALCOP_ERR_LAUNCH;
-  if (prepare_layers() != hipSuccess || prepare_layernorm() != hipSuccess) return ALCOP_ERR_LAUNCH;
+  if (prepare_layers() != hipSuccess || prepare_layernorm() != hipSuccess || prepare_grouped() != hipSuccess ||
+      prepare_loss() != hipSuccess)
+    return ALCOP_ERR_LAUNCH;
   void* scratch = nullptr;
   size_t bytes = 0;
   if (splitk_scratch(&scratch, &bytes) != hipSuccess) return ALCOP_ERR_LAUNCH;

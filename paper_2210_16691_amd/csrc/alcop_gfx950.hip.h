@@ -252,6 +252,12 @@ struct Gfx950 {
   }
   // the value that lane (lane ^ mask) of the wave passes
   __device__ static __forceinline__ uint32_t xor_lanes(uint32_t v, int mask) { return (uint32_t)__shfl_xor((int)v, mask); }
+  // bit l: whether lane l's v is true; the value that lane `lane` (the same for all) passes, in a scalar register
+  __device__ static __forceinline__ uint64_t ballot(bool v) { return __builtin_amdgcn_ballot_w64(v); }
+  __device__ static __forceinline__ uint32_t read_lane(uint32_t v, int lane)
+  {
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+  }
   __device__ static __forceinline__ void lds_write1(uint32_t addr, uint32_t v) { *(ALCOP_LDS uint32_t*)(uintptr_t)addr = v; }
   __device__ static __forceinline__ float sqrt(float v) { return sqrtf(v); }
   __device__ static __forceinline__ float fma(float a, float b, float c) { return __builtin_fmaf(a, b, c); }

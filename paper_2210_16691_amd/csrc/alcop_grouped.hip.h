@@ -1,0 +1,259 @@
+// Products grouped by expert: rows sorted by group, each group's rows times weights of its own, and the gradients.
+//
+//     rows offsets[g] .. offsets[g + 1] - 1:   Z = alpha sa sw A W_g + bias_g,  C = act(Z)
+//     dA = alpha dZ W_g^T,   dW_g = alpha A_g^T dZ_g,   dbias_g = sum over the group's rows of dZ
+//
+// How many rows a group has is known on the device only.  A launch has as many blocks as the rows could make tiles
+// (a partial tile for each group at most), and every wave finds its own tile: a lane per group reads two offsets, the groups' tiles are
+// summed up across the lanes, and the lane whose group holds the block's tile passes it on.  That costs some 0.4 us ahead of the
+// first load, less than a kernel that writes a table (a launch).  Blocks beyond the last tile leave at once.  Tiles of a
+// group are neighbours, and the eight XCDs get equal runs of them, so that a group's weights are read into one or two L2s.
+// From there on a tile is that of a product of its own: the loops and the epilogue are those of the linear layers.
+//
+// Offsets are clamped to 0 .. rows and to rising order where they are read: what they hold decides what is computed, never
+// whether an access is in bounds.
+#pragma once
+#include "alcop_rows.hip.h"
+
+namespace alcop {
+
+// Parameters of a product together with the tile that the block is to compute of it.
+template <class B>
+struct Placed : B {
+  int tile_m, tile_n;
+};
+template <class B>
+__device__ __forceinline__ void tile_of_block(const Placed<B>& p, int, int& tm, int& tn)
+{
+  tm = p.tile_m;
+  tn = p.tile_n;
+}
+
+struct GroupList {
+  const int* offsets;          // groups + 1 numbers
+  int groups, rows;
+};
+
+// ---- the tile of a block ---------------------------------------------------------------------------------
+// The rows of group 64 c + lane, its tiles of 2^shift rows times `width`, and those of the lanes before it; total: of all lanes.
+struct GroupLane {
+  int first, rows, tiles, before, total;
+};
+template <class HW>
+__device__ __forceinline__ GroupLane group_lane(const GroupList& l, int c, int shift, int width)
+{
+  const int lane = HW::lane_id(), g = c * 64 + lane;
+  GroupLane r = {0, 0, 0, 0, 0};
+  if (g < l.groups) {
+    const int a = (int)HW::global_load_u32(l.offsets + g), b = (int)HW::global_load_u32(l.offsets + g + 1);
+    r.first = a < 0 ? 0 : a > l.rows ? l.rows : a;
+    const int end = b > l.rows ? l.rows : b;
+    r.rows = end > r.first ? end - r.first : 0;
+    r.tiles = (int)(((uint32_t)r.rows + (1u << shift) - 1) >> shift) * width;
+  }
+  r.total = r.tiles;
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) {
+    const int o = (int)HW::xor_lanes((uint32_t)r.total, m);
+    if (lane & m) r.before += o;
+    r.total += o;
+  }
+  return r;
+}
+
+struct GroupTile {
+  int group, first, rows, tile;      // tile: among the group's own
+};
+// Tile `lid` of all groups' (SPREAD: dealt to the XCDs in runs).  False if there are not so many.
+template <bool SPREAD, class HW>
+__device__ __forceinline__ bool group_tile(const GroupList& l, int shift, int width, int lid, GroupTile& t)
+{
+  const int chunks = (l.groups + 63) / 64;
+  GroupLane g = group_lane<HW>(l, 0, shift, width);
+  if constexpr (SPREAD) {
+    int all = (int)HW::read_lane((uint32_t)g.total, 0);
+    for (int c = 1; c < chunks; c++) all += (int)HW::read_lane((uint32_t)group_lane<HW>(l, c, shift, width).total, 0);
+    if (lid >= all) return false;
+    const int x = lid & 7, rem8 = all & 7;
+    lid = x * (all >> 3) + (x < rem8 ? x : rem8) + (lid >> 3);
+  }
+  for (int c = 0;;) {
+    const int total = (int)HW::read_lane((uint32_t)g.total, 0);
+    const uint64_t mine = HW::ballot(lid >= g.before && lid - g.before < g.tiles);
+    if (mine) {
+      const int lane = __builtin_ctzll(mine);
+      t.group = c * 64 + lane;
+      t.first = (int)HW::read_lane((uint32_t)g.first, lane);
+      t.rows = (int)HW::read_lane((uint32_t)g.rows, lane);
+      t.tile = lid - (int)HW::read_lane((uint32_t)g.before, lane);
+      return true;
+    }
+    if (++c == chunks) return false;
+    lid -= total;
+    g = group_lane<HW>(l, c, shift, width);
+  }
+}
+// The rows of a group, its tiles and those ahead of it (in t.tile).
+template <class HW>
+__device__ __forceinline__ int group_tiles(const GroupList& l, int shift, int group, GroupTile& t)
+{
+  int ahead = 0, c = 0;
+  GroupLane g = group_lane<HW>(l, 0, shift, 1);
+  for (; c < group / 64; c++) {
+    ahead += (int)HW::read_lane((uint32_t)g.total, 0);
+    g = group_lane<HW>(l, c + 1, shift, 1);
+  }
+  const int lane = group - c * 64;
+  t.group = group;
+  t.first = (int)HW::read_lane((uint32_t)g.first, lane);
+  t.rows = (int)HW::read_lane((uint32_t)g.rows, lane);
+  t.tile = ahead + (int)HW::read_lane((uint32_t)g.before, lane);
+  return (int)HW::read_lane((uint32_t)g.tiles, lane);
+}
+
+constexpr int log2_of(int v)
+{
+  int s = 0;
+  while ((1 << s) < v) s++;
+  return s;
+}
+
+// ---- C = act(alpha sa sw A W_g + bias_g) ---------------------------------------------------------------------
+struct GroupedArgs {
+  LinearArgs l;                // M: all rows
+  const int* offsets;
+  int groups;
+  long strideW;                // between the weights of two groups, 16-bit units
+};
+
+template <class C, class HW>
+__device__ __forceinline__ bool place_group(const GroupedArgs& a, Placed<LinearParams>& p)
+{
+  (LinearParams&)p = expand_linear<C>(a.l);
+  GroupTile t;
+  if (!group_tile<true, HW>(GroupList{a.offsets, a.groups, a.l.M}, log2_of(C::BM), p.ntn, (int)HW::block_x(), t)) return false;
+  const int osz = p.out_dtype == 2 ? 4 : 2;
+  p.M = p.Mv = t.rows;
+  p.ntm = (t.rows + C::BM - 1) / C::BM;
+  p.group_m = p.ntm < 8 ? p.ntm : 8;
+  tile_in_bands(p, t.tile, p.tile_m, p.tile_n);
+  p.A = (const char*)p.A + (long)t.first * p.lda * 2;
+  p.B = (const char*)p.B + (long)t.group * a.strideW * 2;
+  p.C = (char*)p.C + (long)t.first * p.ldc * osz;
+  if (p.pre) p.pre = (char*)p.pre + (long)t.first * p.ldp * osz;
+  if (p.bias) p.bias += (long)t.group * p.N;
+  if (p.sw) p.sw += (long)t.group * p.N;
+  if (p.sa) p.sa += t.first;
+  return true;
+}
+
+template <class C, class HW>
+__global__ void __launch_bounds__(C::NT) alcop_grouped_tile(const GroupedArgs a)
+{
+  Placed<LinearParams> p;
+  if (place_group<C, HW>(a, p)) mainloop_body<C, HW>(p);
+}
+template <class C, class HW>
+__global__ void __launch_bounds__(C::NT) alcop_grouped_ksplit(const GroupedArgs a)
+{
+  Placed<LinearParams> p;
+  if (place_group<C, HW>(a, p)) ksplit_body<C, HW>(p);
+}
+
+// ---- dW_g = alpha P_g^T Q_g, P and Q stored with the rows' axis first ------------------------------------------
+struct GroupedGradArgs {
+  const void *P, *Q;
+  void* dW;
+  const int* offsets;
+  int groups, rows, M, N, ldp, ldq, ldw;
+  long strideW;                // elements of dW
+  float alpha;
+  int out;
+};
+
+template <class C, class HW>
+__global__ void __launch_bounds__(C::NT) alcop_grouped_grad(const GroupedGradArgs a)
+{
+  Placed<Params> p = {};
+  p.M = p.Mv = a.M;
+  p.N = p.Nv = a.N;
+  p.lda = a.ldp;
+  p.ldb = a.ldq;
+  p.ldc = a.ldw;
+  p.alpha = a.alpha;
+  p.out_dtype = a.out;
+  p.ntm = (p.M + C::BM - 1) / C::BM;
+  p.ntn = (p.N + C::BN - 1) / C::BN;
+  p.group_m = p.ntm < 8 ? p.ntm : 8;
+  // all groups have as many tiles: those of a group are neighbours, runs of them go to an XCD each
+  const int per = p.ntm * p.ntn, all = per * a.groups, x = (int)HW::block_x() & 7, rem8 = all & 7;
+  const int r = x * (all >> 3) + (x < rem8 ? x : rem8) + ((int)HW::block_x() >> 3);
+  const int group = r / per;
+  tile_in_bands(p, r - group * per, p.tile_m, p.tile_n);
+  GroupTile t;
+  t.first = (int)HW::read_lane(HW::global_load_u32(a.offsets + group), 0);
+  int end = (int)HW::read_lane(HW::global_load_u32(a.offsets + group + 1), 0);
+  t.first = t.first < 0 ? 0 : t.first > a.rows ? a.rows : t.first;
+  end = end > a.rows ? a.rows : end;
+  const int osz = a.out == 2 ? 4 : 2;
+  p.C = (char*)a.dW + (long)group * a.strideW * osz;
+  if (end <= t.first) {
+    // no rows: the gradient is 0
+    const int per_row = C::BN / 8, tid = HW::wave_id() * 64 + HW::lane_id();
+#pragma unroll 1
+    for (int i = tid; i < C::BM * per_row; i += C::NT) {
+      const int m = p.tile_m * C::BM + i / per_row, n = p.tile_n * C::BN + i % per_row * 8;
+      if (m < p.M && n < p.N) {
+        char* at = (char*)p.C + ((long)m * p.ldc + n) * osz;
+        HW::global_store16(at, u32x4{0, 0, 0, 0});
+        if (osz == 4) HW::global_store16(at + 16, u32x4{0, 0, 0, 0});
+      }
+    }
+    return;
+  }
+  p.K = end - t.first;                      // rows past it lie beyond both descriptors
+  p.A = (const char*)a.P + (long)t.first * p.lda * 2;
+  p.B = (const char*)a.Q + (long)t.first * p.ldb * 2;
+  mainloop_body<C, HW>(p);
+}
+
+// ---- dZ = dC act'(Z) and its sums by group -------------------------------------------------------------------
+// Blocks y have up to 2^shift rows of one group; the sums of a group's blocks are neighbours.
+struct GroupedActGradArgs {
+  ActGradArgs a;
+  GroupList l;
+  int shift;
+};
+template <int DT, class HW>
+__global__ void __launch_bounds__(256) alcop_grouped_act_grad(const GroupedActGradArgs p)
+{
+  GroupTile t;
+  if (!group_tile<false, HW>(p.l, p.shift, 1, (int)HW::block_y(), t)) return;
+  const long r0 = t.first + ((long)t.tile << p.shift), r1 = r0 + (1l << p.shift), end = (long)t.first + t.rows;
+  act_grad<DT, HW>(p.a, r0, r1 < end ? r1 : end, (long)HW::block_y());
+}
+// out[g][j]: the sum over the partial sums of group g
+struct GroupedSumArgs {
+  ColumnSumArgs s;
+  GroupList l;
+  int shift;
+};
+template <class HW>
+__global__ void __launch_bounds__(SUM_THREADS) alcop_grouped_sums(const GroupedSumArgs p)
+{
+  const int group = (int)HW::block_y();
+  GroupTile t;
+  ColumnSumArgs s = p.s;
+  const int count = group_tiles<HW>(p.l, p.shift, group, t);
+  // offsets that do not rise could count more blocks than there are
+  s.count = t.tile + count <= p.s.count ? count : t.tile < p.s.count ? p.s.count - t.tile : 0;
+  s.partial += (long)t.tile * s.cols;
+  s.out += (long)group * s.cols;
+  column_sums<HW>(s);
+}
+
+// the tiles of dW
+template <int DT, int BM, int BN, int BK, int WM, int WN, int S, int R, int F>
+using GradCfg = KCfg<DT, BM, BN, BK, WM, WN, S, R, F, 0, 0, 1>;
+
+}  // namespace alcop

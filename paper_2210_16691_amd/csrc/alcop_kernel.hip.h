@@ -664,6 +664,9 @@ template <class C, class HW, class P>
 __device__ __forceinline__ void linear_tile(const P& p, typename C::Ahead& ahead, f32x16 (&acc)[C::TN][C::TM], int m0, int n0,
                                             uint32_t ebase, int lane);
 
+// Rows of B that exist, where it is stored K x N: all K, unless the parameters know better (alcop_loss.hip.h).
+__device__ __forceinline__ int depth_of_b(const Params&, int K) { return K; }
+
 template <class C, class HW, class P = Params>
 __device__ __forceinline__ void mainloop_body(const P& p)
 {
@@ -775,7 +778,7 @@ __device__ __forceinline__ void mainloop_body(const P& p)
                            (C::AM == 2 ? 0 : c * 16));
     }
   }
-  lb = setup_loader<OB, HW>(Bbatch, tn, p.N, p.ldb, Kb, nko, q0);
+  lb = setup_loader<OB, HW>(Bbatch, tn, p.N, p.ldb, depth_of_b(p, Kb), nko, q0);
 
   // ---- HBM -> L2 touches (third pipeline level) --------------------------------------------
   // The blocks of one XCD that run side by side load the same A row-panel (those with equal tm)

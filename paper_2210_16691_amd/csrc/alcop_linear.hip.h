@@ -286,7 +286,7 @@ __device__ __forceinline__ void load_floats(const float* from, float none, float
   } else {
 #pragma unroll
     for (int i = 0; i < W / 4; i++) {
-      const f32x4 t = HW::global_load_f32x4(from + 4 * i);
+      const f32x4 t = __builtin_bit_cast(f32x4, HW::global_load16_any(from + 4 * i));
 #pragma unroll
       for (int e = 0; e < 4; e++) to[4 * i + e] = t[e];
     }

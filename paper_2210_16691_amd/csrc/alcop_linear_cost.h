@@ -71,15 +71,18 @@ inline const LinearCost kLinearCost[] = {
     {{256, 256, 64, 128, 64, 2, 2, 1, 1, 0, 0}, 3, 1, 1, 1, 5.552, 1.314, 2.420, 1.276, 0.000, 0.000},
 };
 
-// K in 16-bit units; bytes: of everything read and written.
-inline double linear_us(const LinearCost& m, int M, int N, int K, double bytes)
+// K in 16-bit units; bytes: of everything read and written.  tiles: of C; products: M N
+inline double linear_us(const LinearCost& m, double tiles, double products, int K, double bytes)
 {
   auto up = [](double x, double y) { return (double)(long)((x + y - 1) / y); };
-  const double tiles = up(M, m.s.bm) * up(N, m.s.bn);
   const double turns = up(tiles, 256), kt = up(up(K, m.s.bk), m.waves_k);
   const double turns2 = m.blocks == 2 ? 2.0 * up(tiles, 512) : 0.0;
-  return m.a + m.b * turns * kt + m.c * turns + m.d * bytes / 5.1e6 + m.e * 2.0 * M * N * (double)K / 1.4e9 +
+  return m.a + m.b * turns * kt + m.c * turns + m.d * bytes / 5.1e6 + m.e * 2.0 * products * (double)K / 1.4e9 +
          m.f * turns2 * kt;
+}
+inline double linear_us(const LinearCost& m, int M, int N, int K, double bytes)
+{
+  return linear_us(m, (double)(((long)M + m.s.bm - 1) / m.s.bm) * (((long)N + m.s.bn - 1) / m.s.bn), (double)M * N, K, bytes);
 }
 
 // The kernels whose waves split K are compared only while 64 x 64 tiles leave compute units idle, those of such tiles up to

@@ -473,15 +473,14 @@ __global__ void __launch_bounds__(SUM_THREADS) alcop_column_sums(const ColumnSum
 // 16 bits.  A block has 512 columns (or all, where there are fewer) and a run of rows; of 64 lanes `p.lanes` share a row,
 // so that a wave has 64 / lanes rows at a time; 16-byte chunks.
 constexpr int ACT_COLS = 512;
+// Rows r0 .. r1 - 1 of it, whose sums go to row `part` of the partial ones.
 template <int DT, class HW>
-__global__ void __launch_bounds__(256) alcop_act_grad(const ActGradArgs p)
+__device__ __forceinline__ void act_grad(const ActGradArgs& p, long r0, long r1, long part)
 {
   const uint32_t lds = HW::lds_base();
   const int tid = HW::wave_id() * 64 + HW::lane_id();
   const int mine = tid & (p.lanes - 1), rows = 256 / p.lanes;     // lanes: a power of two
   const int n = (int)HW::block_x() * ACT_COLS + mine * 8;
-  const long r0 = (long)HW::block_y() * p.rows_per_block;
-  const long r1 = r0 + p.rows_per_block < p.M ? r0 + p.rows_per_block : p.M;
   float sum[8];
 #pragma unroll
   for (int e = 0; e < 8; e++) sum[e] = 0.f;
@@ -514,8 +513,14 @@ __global__ void __launch_bounds__(256) alcop_act_grad(const ActGradArgs p)
     float t = 0.f;
 #pragma unroll 4
     for (int g = 0; g < rows; g++) t += __builtin_bit_cast(float, HW::lds_read4(lds + (uint32_t)(g * width + (c < width ? c : 0)) * 4));
-    if (c < width && j < p.N) HW::global_store_u32(p.partial + (long)HW::block_y() * p.N + j, __builtin_bit_cast(uint32_t, t));
+    if (c < width && j < p.N) HW::global_store_u32(p.partial + part * p.N + j, __builtin_bit_cast(uint32_t, t));
   }
+}
+template <int DT, class HW>
+__global__ void __launch_bounds__(256) alcop_act_grad(const ActGradArgs p)
+{
+  const long r0 = (long)HW::block_y() * p.rows_per_block;
+  act_grad<DT, HW>(p, r0, r0 + p.rows_per_block < p.M ? r0 + p.rows_per_block : p.M, (long)HW::block_y());
 }
 
 }  // namespace alcop

@@ -32,6 +32,10 @@ struct Api {
   decltype(&alcop_quantize_rows) quantize_rows = nullptr;
   decltype(&alcop_layernorm) layernorm = nullptr;
   decltype(&alcop_layernorm_backward) layernorm_backward = nullptr;
+  decltype(&alcop_grouped_linear) grouped_linear = nullptr;
+  decltype(&alcop_grouped_linear_backward) grouped_linear_backward = nullptr;
+  decltype(&alcop_linear_cross_entropy) cross_entropy = nullptr;
+  decltype(&alcop_linear_cross_entropy_backward) cross_entropy_backward = nullptr;
 } api;
 
 PyObject* sched_type = nullptr;   // the binding's ctypes mirror of alcop_sched
@@ -511,10 +515,151 @@ PyObject* layernorm_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
   });
 }
 
-// init_more(layernorm, layernorm_backward): addresses in the library
+// A matrix per group on the device of the call, or (None) none.
+struct Groups {
+  const at::Tensor* t = nullptr;
+  int groups = 0, rows = 0, cols = 0;
+  long ld = 0, stride = 0;
+  alcop_dtype type = ALCOP_F32;
+  Groups(PyObject* o, const Rows& like)
+  {
+    if (o == Py_None) return;
+    const at::Tensor& m = tensor(o);
+    need(m.dim() == 3 && m.device() == like.t->device());
+    for (int i = 0; i < 3; i++) need(m.size(i) >= 1 && m.size(i) < INT32_MAX);
+    need(m.size(2) == 1 || m.stride(2) == 1);
+    t = &m;
+    groups = (int)m.size(0);
+    rows = (int)m.size(1);
+    cols = (int)m.size(2);
+    ld = rows == 1 ? (long)cols : (long)m.stride(1);
+    stride = groups == 1 ? rows * ld : (long)m.stride(0);
+    type = m.scalar_type() == at::kFloat8_e4m3fn ? ALCOP_E4M3 : dtype(m);
+  }
+  void* out() const { return t ? t->data_ptr() : nullptr; }
+};
+const at::Tensor* floats_per_group(PyObject* o, int groups, int n, const Rows& like)
+{
+  if (o == Py_None) return nullptr;
+  const at::Tensor& v = tensor(o);
+  need(v.dim() == 2 && v.size(0) == groups && v.size(1) == n && v.is_contiguous() && v.scalar_type() == at::kFloat &&
+       v.device() == like.t->device());
+  return &v;
+}
+const at::Tensor& offsets_of(PyObject* o, int groups, const Rows& like)
+{
+  const at::Tensor& v = tensor(o);
+  need(v.dim() == 1 && v.size(0) == (int64_t)groups + 1 && v.is_contiguous() && v.scalar_type() == at::kInt &&
+       v.device() == like.t->device());
+  return v;
+}
+
+// grouped_linear(A, W, offsets, C, transB, alpha, bias, act, pre, scale_a, scale_w, stream)
+PyObject* grouped_linear(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+  return guarded([&] {
+    need(api.grouped_linear && n == 12 && a[1] != Py_None && a[3] != Py_None);
+    const Rows A(a[0]);
+    const Groups W(a[1], A);
+    const at::Tensor& offsets = offsets_of(a[2], W.groups, A);
+    const int tb = truth(a[4]), N = tb ? W.rows : W.cols;
+    need((tb ? W.cols : W.rows) == A.cols && W.type == A.type);
+    const Rows C(a[3], A.rows, N, A, false), pre(a[8], A.rows, N, C, true);
+    const at::Tensor *bias = floats_per_group(a[6], W.groups, N, A), *sw = floats_per_group(a[10], W.groups, N, A);
+    const at::Tensor* sa = floats(a[9], A.rows, A);
+    const alcop_linear_tail t{number(a[5]), in(bias), integer(a[7]), nullptr, 0, pre.out(), pre.ld, in(sa), in(sw)};
+    void* st = stream_on(A, a[11]);
+    const void *pa = A.in(), *pw = W.t->const_data_ptr(), *po = offsets.const_data_ptr();
+    void* pc = C.out();
+    return unlocked([&] {
+      return api.grouped_linear(pa, pw, po, pc, A.rows, W.groups, N, A.cols, A.ld, W.ld, W.stride, C.ld, tb, A.type, C.type, &t, st);
+    });
+  });
+}
+
+// grouped_linear_backward(dC, A, W, offsets, dA, dW, dbias, pre, act, alpha, transB, workspace, stream)
+PyObject* grouped_linear_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+  return guarded([&] {
+    need(api.grouped_linear_backward && n == 13 && a[2] != Py_None);
+    const Rows dC(a[0]), A(a[1]);
+    const Groups W(a[2], dC), dW(a[5], dC);
+    const at::Tensor& offsets = offsets_of(a[3], W.groups, dC);
+    const int tb = truth(a[10]), N = tb ? W.rows : W.cols, K = tb ? W.cols : W.rows, R = dC.rows;
+    need(A.rows == R && A.cols == K && dC.cols == N && A.type == dC.type && W.type == dC.type && A.t->device() == dC.t->device());
+    need(!dW.t || (dW.groups == W.groups && dW.rows == W.rows && dW.cols == W.cols));
+    const Rows dA(a[4], R, K, dC, false), pre(a[7], R, N, dC, true);
+    need(!dA.t || !dW.t || dA.type == dW.type);
+    const at::Tensor* db = floats_per_group(a[6], W.groups, N, dC);
+    const int act = integer(a[8]);
+    const float alpha = number(a[9]);
+    const Scratch ws(a[11], dC);
+    void* st = stream_on(dC, a[12]);
+    const void *pc = dC.in(), *pa = A.in(), *pw = W.t->const_data_ptr(), *pp = pre.in(), *po = offsets.const_data_ptr();
+    void *oa = dA.out(), *ow = dW.out(), *ob = out(db);
+    const alcop_dtype type = dA.t ? dA.type : dW.t ? dW.type : dC.type;
+    return unlocked([&] {
+      return api.grouped_linear_backward(pc, pa, pw, pp, po, oa, ow, ob, R, W.groups, N, K, dC.ld, A.ld, W.ld, W.stride, pre.ld,
+                                         dA.ld, dW.ld, dW.stride, tb, dC.type, type, alpha, act, ws.p, ws.bytes, st);
+    });
+  });
+}
+
+const at::Tensor& labels_of(PyObject* o, const Rows& X)
+{
+  const at::Tensor& v = tensor(o);
+  need(v.dim() == 1 && v.size(0) == X.rows && v.is_contiguous() && v.scalar_type() == at::kLong && v.device() == X.t->device());
+  return v;
+}
+
+// cross_entropy(X, W, labels, loss, lse, workspace, alpha, stream)
+PyObject* cross_entropy(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+  return guarded([&] {
+    need(api.cross_entropy && n == 8 && a[3] != Py_None);
+    const Rows X(a[0]), W(a[1]);
+    need(W.cols == X.cols && W.type == X.type && W.t->device() == X.t->device());
+    const at::Tensor& labels = labels_of(a[2], X);
+    const at::Tensor *loss = floats(a[3], X.rows, X), *lse = floats(a[4], X.rows, X);
+    const Scratch ws(a[5], X);
+    const float alpha = number(a[6]);
+    void* st = stream_on(X, a[7]);
+    const void *px = X.in(), *pw = W.in(), *pl = labels.const_data_ptr();
+    void *po = out(loss), *pe = out(lse);
+    return unlocked([&] {
+      return api.cross_entropy(px, pw, pl, po, pe, X.rows, W.rows, X.cols, X.ld, W.ld, alpha, X.type, ws.p, ws.bytes, st);
+    });
+  });
+}
+
+// cross_entropy_backward(X, W, labels, lse, workspace, dX, dW, dloss, alpha, stream)
+PyObject* cross_entropy_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+  return guarded([&] {
+    need(api.cross_entropy_backward && n == 10);
+    const Rows X(a[0]), W(a[1]);
+    need(W.cols == X.cols && W.type == X.type && W.t->device() == X.t->device());
+    const at::Tensor& labels = labels_of(a[2], X);
+    const at::Tensor *lse = floats(a[3], X.rows, X), *dloss = floats(a[7], X.rows, X);
+    const Scratch ws(a[4], X);
+    const Rows dX(a[5], X.rows, X.cols, X, false), dW(a[6], W.rows, W.cols, X, false);
+    need(!dX.t || !dW.t || dX.type == dW.type);
+    const float alpha = number(a[8]);
+    void* st = stream_on(X, a[9]);
+    const void *px = X.in(), *pw = W.in(), *pl = labels.const_data_ptr(), *pe = in(lse), *pd = in(dloss);
+    void *ox = dX.out(), *ow = dW.out();
+    const alcop_dtype type = dX.t ? dX.type : dW.t ? dW.type : X.type;
+    return unlocked([&] {
+      return api.cross_entropy_backward(px, pw, pl, pe, pd, ox, ow, X.rows, W.rows, X.cols, X.ld, W.ld, dX.ld, dW.ld, alpha, X.type,
+                                        type, ws.p, ws.bytes, st);
+    });
+  });
+}
+
+// init_more(layernorm, layernorm_backward, grouped_linear, grouped_linear_backward, cross_entropy, cross_entropy_backward): addresses in the library
 PyObject* init_more(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
-  constexpr int COUNT = 2;
+  constexpr int COUNT = 6;
   if (n != COUNT) {
     PyErr_Format(PyExc_TypeError, "init_more takes %d addresses", COUNT);
     return nullptr;
@@ -526,6 +671,10 @@ PyObject* init_more(PyObject*, PyObject* const* a, Py_ssize_t n)
   }
   api.layernorm = (decltype(api.layernorm))f[0];
   api.layernorm_backward = (decltype(api.layernorm_backward))f[1];
+  api.grouped_linear = (decltype(api.grouped_linear))f[2];
+  api.grouped_linear_backward = (decltype(api.grouped_linear_backward))f[3];
+  api.cross_entropy = (decltype(api.cross_entropy))f[4];
+  api.cross_entropy_backward = (decltype(api.cross_entropy_backward))f[5];
   Py_RETURN_NONE;
 }
 
@@ -587,6 +736,10 @@ PyMethodDef methods[] = {
     {"init_more", (PyCFunction)(void*)init_more, METH_FASTCALL, "set the entry points of layer norm, experts and losses"},
     {"layernorm", (PyCFunction)(void*)layernorm, METH_FASTCALL, "layer norm of rows"},
     {"layernorm_backward", (PyCFunction)(void*)layernorm_backward, METH_FASTCALL, "gradients of the layer norm"},
+    {"grouped_linear", (PyCFunction)(void*)grouped_linear, METH_FASTCALL, "products grouped by expert"},
+    {"grouped_linear_backward", (PyCFunction)(void*)grouped_linear_backward, METH_FASTCALL, "gradients of such products"},
+    {"cross_entropy", (PyCFunction)(void*)cross_entropy, METH_FASTCALL, "cross entropy of a vocabulary's product"},
+    {"cross_entropy_backward", (PyCFunction)(void*)cross_entropy_backward, METH_FASTCALL, "gradients of the cross entropy"},
     {"conv_any", (PyCFunction)(void*)conv_any, METH_FASTCALL, "convolution of unaligned operands"},
     {nullptr, nullptr, 0, nullptr}};
 

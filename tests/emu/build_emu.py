@@ -39,11 +39,14 @@ def build() -> str:
     emu = os.path.join(HERE, "emu_lib.cpp")
     jobs = [(emu, os.path.join(OUT, "emu_part%d.o" % p), ["-DEMU_PART=%d" % p]) for p in range(8)]
     jobs.append((emu, os.path.join(OUT, "emu_main.o"), ["-DEMU_PART=-1"]))
-    for name in ("alcop_api.cpp", "alcop_model.cpp", "alcop_linear.cpp", "alcop_layernorm.cpp"):
+    for name in ("alcop_api.cpp", "alcop_model.cpp", "alcop_linear.cpp", "alcop_layernorm.cpp", "alcop_grouped.cpp", "alcop_loss.cpp"):
         jobs.append((os.path.join(CSRC, name), os.path.join(OUT, name + ".o"), []))
     lin = os.path.join(HERE, "emu_linear.cpp")
     jobs += [(lin, os.path.join(OUT, "emu_linear%d.o" % p), ["-DEMU_PART=%d" % p]) for p in range(5)]
     jobs.append((os.path.join(HERE, "emu_layernorm.cpp"), os.path.join(OUT, "emu_layernorm.o"), []))
+    grouped = os.path.join(HERE, "emu_grouped.cpp")
+    jobs += [(grouped, os.path.join(OUT, "emu_grouped%d.o" % p), ["-DEMU_PART=%d" % p]) for p in range(5)]
+    jobs += [(os.path.join(HERE, "emu_loss.cpp"), os.path.join(OUT, "emu_loss%d.o" % p), ["-DEMU_PART=%d" % p]) for p in range(3)]
     with cf.ThreadPoolExecutor(max_workers=8) as ex:
         objs = list(ex.map(_compile, jobs))
     if not os.path.exists(LIB) or any(os.path.getmtime(o) > os.path.getmtime(LIB) for o in objs):

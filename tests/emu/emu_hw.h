@@ -733,6 +733,31 @@ struct Emu {
     wave_sync();
     return W.T[par][l ^ mask];
   }
+  static uint64_t ballot(bool v)
+  {
+    Block& b = *blk();
+    Lane& L = b.lanes[b.cur];
+    Wave& W = b.waves[b.cur >> 6];
+    const int par = L.tr_par;
+    L.tr_par ^= 1;
+    W.T[par][b.cur & 63] = v;
+    wave_sync();
+    uint64_t m = 0;
+    for (int l = 0; l < 64; l++) m |= (uint64_t)(W.T[par][l] != 0) << l;
+    return m;
+  }
+  static uint32_t read_lane(uint32_t v, int lane)
+  {
+    Block& b = *blk();
+    Lane& L = b.lanes[b.cur];
+    Wave& W = b.waves[b.cur >> 6];
+    const int par = L.tr_par;
+    L.tr_par ^= 1;
+    W.T[par][b.cur & 63] = v;
+    wave_sync();
+    if (lane < 0 || lane > 63) fail("read of lane %d (thread %d)", lane, b.cur);
+    return W.T[par][lane & 63];
+  }
   static void lds_write1(uint32_t addr, uint32_t v) { lds_write(addr, v); }
   static float sqrt(float v) { return __builtin_sqrtf(v); }
   static float fma(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
