@@ -588,8 +588,8 @@ int alcop_linear_cross_entropy(const void* X, const void* W, const void* labels,
  *   lse: as alcop_linear_cross_entropy left it.  dloss: rows fp32 values, NULL = 1.
  *   dX (rows x K), dW (vocab x K): type `out`, which is `in` or ALCOP_F32; one may be NULL.  16-byte aligned, pitches multiples of 8.
  *   workspace: DEVICE, 16-byte aligned, at least alcop_linear_cross_entropy_backward_workspace_bytes(rows, vocab, K) bytes,
- *     as above: G of a piece of the vocabulary (up to 256 MiB, or rows x 512 bytes if that is more) and, if there are several
- *     pieces, dX in fp32.
+ *     as above: G of a piece of the vocabulary (up to 128 MiB, or rows x 512 bytes if that is more) and sums of dX in fp32,
+ *     one for each of up to 16 slices of a piece where dX is small.
  * For dW, all rows of X and of a piece of G, 128 more counted, span less than 2 GiB each; else ALCOP_ERR_SIZE, before anything is
  * launched.  Up to three launches a piece and two more; sums have a fixed order, without atomics.
  */

@@ -43,19 +43,24 @@ const GroupedTable& grouped_table()
   return t;
 }
 
-// Tiles of bm rows that `rows` rows of `groups` groups make: at most, and where the groups are even.
+// Tiles of bm rows that `rows` rows of `groups` groups make at most.
 long most_tiles(long rows, long groups, long bm)
 {
   const long g = std::min(groups, rows);
   return (rows + g * (bm - 1)) / bm;
 }
-double even_tiles(long rows, long groups, long bm)
+// Microseconds by the costs of the linear layers (alcop_linear_cost.h) where the groups' sizes are not known: as many full tiles as
+// even groups have, a half more each for the one that is not full, and turns of the card that need not be whole.
+double grouped_us(const LinearCost& m, long rows, long groups, int N, int K, double bytes)
 {
-  const long g = std::min(groups, rows), per = (rows + g - 1) / g;
-  return (double)g * (double)((per + bm - 1) / bm);
+  const double live = (double)std::min(groups, rows), per = (double)rows / live;
+  const double tiles = live * std::max(1.0, per / m.s.bm + 0.5) * (double)((N + (long)m.s.bn - 1) / m.s.bn);
+  const double turns = std::max(1.0, tiles / 256), turns2 = m.blocks == 2 ? 2 * std::max(1.0, tiles / 512) : 0.0;
+  const double kt = (double)((K + m.s.bk - 1) / m.s.bk + m.waves_k - 1) / m.waves_k;
+  return m.a + m.b * turns * kt + m.c * turns + m.d * bytes / 5.1e6 + m.e * 2.0 * rows * N * (double)K / 1.4e9 + m.f * turns2 * kt;
 }
 
-// The kernel of the lowest cost, as alcop_linear has it, of groups that are even: what they are is not known here.
+// The kernel of the lowest cost.
 const GroupedKernel* pick(int cls, int dt, int bl, bool fine, int rows, int groups, int N, int K, double bytes)
 {
   const GroupedKernel* best = nullptr;
@@ -70,8 +75,7 @@ const GroupedKernel* pick(int cls, int dt, int bl, bool fine, int rows, int grou
       continue;
     }
     if (!k.cost) continue;
-    const double strips = (double)((N + (long)k.s.bn - 1) / k.s.bn);
-    const double us = linear_us(*k.cost, even_tiles(rows, groups, k.s.bm) * strips, (double)rows * N, K, bytes);
+    const double us = grouped_us(*k.cost, rows, groups, N, K, bytes);
     if (!best || us < best_us) {
       best = &k;
       best_us = us;
@@ -80,11 +84,16 @@ const GroupedKernel* pick(int cls, int dt, int bl, bool fine, int rows, int grou
   return best;
 }
 
-// Rows of a block of alcop_grouped_act_grad, as a power of two, and how many such blocks there may be.
-int act_shift(int rows, int groups)
+// Rows of a block of alcop_grouped_act_grad, as a power of two: enough blocks to fill the card (2048 with 512 columns each; 8192 rows of
+// 2048 in 16 groups, us of the whole backward pass: 234, 230, 232, 229, 245 and 275 with 4 to 128 rows), each with all its waves at
+// work, and at most 1024 sums to a column beside a group's last.
+int act_shift(int rows, int N)
 {
-  int shift = 6;
-  while (shift < 30 && most_tiles(rows, groups, 1l << shift) > 512 + groups) shift++;
+  const int strips = (N + ACT_COLS - 1) / ACT_COLS;
+  int lanes = 1, shift = 2;
+  while (lanes < 64 && lanes * 8 < N) lanes *= 2;
+  while ((1 << shift) < 256 / lanes) shift++;
+  while (shift < 30 && (((long)rows >> shift) * strips > 2048 || ((long)rows >> shift) > 1024)) shift++;
   return shift;
 }
 
@@ -96,7 +105,7 @@ struct GradPlan {
 GradPlan plan_of(int rows, int groups, int N)
 {
   GradPlan p;
-  p.shift = act_shift(rows, groups);
+  p.shift = act_shift(rows, N);
   p.runs = most_tiles(rows, groups, 1l << p.shift);
   p.dz = r256(2.0 * rows * N);
   p.sums = r256(4.0 * p.runs * N);
@@ -320,10 +329,15 @@ int alcop_grouped_linear_backward(const void* dC, const void* A, const void* W, 
     const double depth = std::max(8.0, (double)rows / std::min(groups, rows));
     const double bytes = 2.0 * rows * ((double)N + K) + (double)osz * groups * N * K;
     double best_us = 0;
+    const char* env = std::getenv("ALCOP_GRADIENT_KERNEL");       // a tuning and test knob: its number among those of the type
+    int nr = 0;
     for (const GroupedGradKernel& k : grouped_table().grad) {
+      if (k.dt != (in == ALCOP_BF16)) continue;
       const double tiles = (double)groups * ((w_rows + (long)k.s.bm - 1) / k.s.bm) * ((w_cols + (long)k.s.bn - 1) / k.s.bn);
-      if (k.dt != (in == ALCOP_BF16) || tiles >= 2147483648.0 || tiles * k.threads >= 4294967296.0) continue;
-      const double us = linear_us(*k.cost, tiles, (double)groups * N * K, (int)depth, bytes);
+      if (tiles >= 2147483648.0 || tiles * k.threads >= 4294967296.0) continue;
+      const bool named = env && *env;
+      if (named ? nr++ != std::atoi(env) : !k.cost) continue;
+      const double us = named ? 0.0 : linear_us(*k.cost, tiles, (double)groups * N * K, (int)depth, bytes);
       if (!wk || us < best_us) {
         wk = &k;
         best_us = us;

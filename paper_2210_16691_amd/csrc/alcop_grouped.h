@@ -43,7 +43,9 @@ hipError_t prepare_grouped();
   add_grouped_ksplit<CL, DT, 32, 32, 8, BL>(T);             \
   add_grouped_ksplit<CL, DT, 32, 64, 4, BL>(T);             \
   add_grouped<CL, DT, 64, 64, 64, 32, 32, 3, 2, 1, BL>(T);  \
+  add_grouped<CL, DT, 128, 64, 64, 64, 32, 3, 2, 1, BL>(T); \
   add_grouped<CL, DT, 128, 128, 64, 64, 64, 2, 2, 1, BL>(T); \
+  add_grouped<CL, DT, 256, 128, 64, 128, 64, 3, 2, 1, BL>(T); \
   add_grouped<CL, DT, 256, 256, 32, 128, 64, 3, 2, 1, BL>(T);
 #define ALCOP_GROUPED_KERNELS(T, DT, BL)        \
   ALCOP_GROUPED_CLASS(T, CLASS_PLAIN, DT, BL)   \
@@ -52,9 +54,13 @@ hipError_t prepare_grouped();
 // The kernels that multiply e4m3 as they are.
 #define ALCOP_GROUPED_F8(T, CL)                              \
   add_grouped<CL, 3, 64, 64, 64, 32, 32, 3, 2, 1, 1>(T);     \
+  add_grouped<CL, 3, 128, 64, 64, 64, 32, 3, 2, 1, 1>(T);    \
   add_grouped<CL, 3, 128, 128, 64, 64, 64, 2, 2, 1, 1>(T);   \
+  add_grouped<CL, 3, 256, 128, 64, 128, 64, 3, 2, 1, 1>(T);  \
   add_grouped<CL, 3, 256, 256, 64, 128, 64, 2, 2, 1, 1>(T);
 #define ALCOP_GROUPED_GRAD(T, DT)                              \
   add_grouped_grad<DT, 64, 64, 64, 32, 32, 3, 2, 1>(T);        \
+  add_grouped_grad<DT, 128, 64, 64, 64, 32, 3, 2, 1>(T);       \
   add_grouped_grad<DT, 128, 128, 64, 64, 64, 2, 2, 1>(T);      \
+  add_grouped_grad<DT, 256, 128, 64, 128, 64, 3, 2, 1>(T);     \
   add_grouped_grad<DT, 256, 256, 32, 128, 64, 3, 2, 1>(T);

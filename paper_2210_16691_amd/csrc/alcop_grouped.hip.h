@@ -6,7 +6,7 @@
 // How many rows a group has is known on the device only.  A launch has as many blocks as the rows could make tiles
 // (a partial tile for each group at most), and every wave finds its own tile: a lane per group reads two offsets, the groups' tiles are
 // summed up across the lanes, and the lane whose group holds the block's tile passes it on.  That costs some 0.4 us ahead of the
-// first load, less than a kernel that writes a table (a launch).  Blocks beyond the last tile leave at once.  Tiles of a
+// first load, less than a kernel that writes a table (a launch).  Blocks beyond the last tile leave at once.  Full tiles of a
 // group are neighbours, and the eight XCDs get equal runs of them, so that a group's weights are read into one or two L2s.
 // From there on a tile is that of a product of its own: the loops and the epilogue are those of the linear layers.
 //
@@ -17,7 +17,6 @@
 
 namespace alcop {
 
-// Parameters of a product together with the tile that the block is to compute of it.
 template <class B>
 struct Placed : B {
   int tile_m, tile_n;
@@ -35,11 +34,12 @@ struct GroupList {
 };
 
 // ---- the tile of a block ---------------------------------------------------------------------------------
-// The rows of group 64 c + lane, its tiles of 2^shift rows times `width`, and those of the lanes before it; total: of all lanes.
+// The rows of group 64 c + lane; its tiles of 2^shift rows, full ones (PARTS: all), times `width`; those of the lanes before it and of
+// all lanes.
 struct GroupLane {
   int first, rows, tiles, before, total;
 };
-template <class HW>
+template <bool PARTS, class HW>
 __device__ __forceinline__ GroupLane group_lane(const GroupList& l, int c, int shift, int width)
 {
   const int lane = HW::lane_id(), g = c * 64 + lane;
@@ -49,7 +49,7 @@ __device__ __forceinline__ GroupLane group_lane(const GroupList& l, int c, int s
     r.first = a < 0 ? 0 : a > l.rows ? l.rows : a;
     const int end = b > l.rows ? l.rows : b;
     r.rows = end > r.first ? end - r.first : 0;
-    r.tiles = (int)(((uint32_t)r.rows + (1u << shift) - 1) >> shift) * width;
+    r.tiles = (int)(((uint32_t)r.rows + (PARTS ? (1u << shift) - 1 : 0u)) >> shift) * width;
   }
   r.total = r.tiles;
 #pragma unroll
@@ -64,51 +64,94 @@ __device__ __forceinline__ GroupLane group_lane(const GroupList& l, int c, int s
 struct GroupTile {
   int group, first, rows, tile;      // tile: among the group's own
 };
-// Tile `lid` of all groups' (SPREAD: dealt to the XCDs in runs).  False if there are not so many.
-template <bool SPREAD, class HW>
-__device__ __forceinline__ bool group_tile(const GroupList& l, int shift, int width, int lid, GroupTile& t)
+template <class HW>
+__device__ __forceinline__ void take_lane(const GroupLane& g, int c, int lane, GroupTile& t)
+{
+  t.group = c * 64 + lane;
+  t.first = (int)HW::read_lane((uint32_t)g.first, lane);
+  t.rows = (int)HW::read_lane((uint32_t)g.rows, lane);
+}
+
+// Run `lid` of all groups' runs of 2^shift rows, the last of each shorter.  False if there are not so many.
+template <class HW>
+__device__ __forceinline__ bool group_run(const GroupList& l, int shift, int lid, GroupTile& t)
 {
   const int chunks = (l.groups + 63) / 64;
-  GroupLane g = group_lane<HW>(l, 0, shift, width);
-  if constexpr (SPREAD) {
-    int all = (int)HW::read_lane((uint32_t)g.total, 0);
-    for (int c = 1; c < chunks; c++) all += (int)HW::read_lane((uint32_t)group_lane<HW>(l, c, shift, width).total, 0);
-    if (lid >= all) return false;
-    const int x = lid & 7, rem8 = all & 7;
-    lid = x * (all >> 3) + (x < rem8 ? x : rem8) + (lid >> 3);
-  }
-  for (int c = 0;;) {
-    const int total = (int)HW::read_lane((uint32_t)g.total, 0);
+  for (int c = 0; c < chunks; c++) {
+    const GroupLane g = group_lane<true, HW>(l, c, shift, 1);
     const uint64_t mine = HW::ballot(lid >= g.before && lid - g.before < g.tiles);
     if (mine) {
       const int lane = __builtin_ctzll(mine);
-      t.group = c * 64 + lane;
-      t.first = (int)HW::read_lane((uint32_t)g.first, lane);
-      t.rows = (int)HW::read_lane((uint32_t)g.rows, lane);
+      take_lane<HW>(g, c, lane, t);
       t.tile = lid - (int)HW::read_lane((uint32_t)g.before, lane);
       return true;
     }
-    if (++c == chunks) return false;
-    lid -= total;
-    g = group_lane<HW>(l, c, shift, width);
+    lid -= (int)HW::read_lane((uint32_t)g.total, 0);
   }
+  return false;
 }
-// The rows of a group, its tiles and those ahead of it (in t.tile).
+// The rows of a group, its runs (returned) and those ahead of it (in t.tile).
 template <class HW>
-__device__ __forceinline__ int group_tiles(const GroupList& l, int shift, int group, GroupTile& t)
+__device__ __forceinline__ int group_runs(const GroupList& l, int shift, int group, GroupTile& t)
 {
   int ahead = 0, c = 0;
-  GroupLane g = group_lane<HW>(l, 0, shift, 1);
+  GroupLane g = group_lane<true, HW>(l, 0, shift, 1);
   for (; c < group / 64; c++) {
     ahead += (int)HW::read_lane((uint32_t)g.total, 0);
-    g = group_lane<HW>(l, c + 1, shift, 1);
+    g = group_lane<true, HW>(l, c + 1, shift, 1);
   }
   const int lane = group - c * 64;
-  t.group = group;
-  t.first = (int)HW::read_lane((uint32_t)g.first, lane);
-  t.rows = (int)HW::read_lane((uint32_t)g.rows, lane);
+  take_lane<HW>(g, c, lane, t);
   t.tile = ahead + (int)HW::read_lane((uint32_t)g.before, lane);
   return (int)HW::read_lane((uint32_t)g.tiles, lane);
+}
+
+// Item `lid` of `all` that are dealt to the XCDs in equal runs (blocks go to the XCDs in turn).
+__device__ __forceinline__ int spread_out(int lid, int all)
+{
+  const int x = lid & 7, rem8 = all & 7;
+  return x * (all >> 3) + (x < rem8 ? x : rem8) + (lid >> 3);
+}
+
+// The tile of block `lid` among those of `width` strips of columns: first the full tiles of all groups, then, as they take less time
+// (waves without rows do not multiply) and so even out the end, the groups' last tiles that are not full.  part: such a one,
+// t.tile its strip.  False if there are not so many.
+template <class HW>
+__device__ __forceinline__ bool group_tile(const GroupList& l, int shift, int width, int lid, GroupTile& t, bool& part)
+{
+  const int chunks = (l.groups + 63) / 64, lane = HW::lane_id(), rest = (1 << shift) - 1;
+  GroupLane g = group_lane<false, HW>(l, 0, shift, width);
+  uint64_t parts = HW::ballot((g.rows & rest) != 0);
+  int full = (int)HW::read_lane((uint32_t)g.total, 0), ends = __builtin_popcountll(parts);
+  for (int c = 1; c < chunks; c++) {
+    const GroupLane o = group_lane<false, HW>(l, c, shift, width);
+    full += (int)HW::read_lane((uint32_t)o.total, 0);
+    ends += __builtin_popcountll(HW::ballot((o.rows & rest) != 0));
+  }
+  part = lid >= full;
+  if (part && lid - full >= ends * width) return false;
+  lid = part ? spread_out(lid - full, ends * width) : spread_out(lid, full);
+  int q = 0;
+  if (part) {
+    q = lid / width;
+    t.tile = lid - q * width;
+  }
+  for (int c = 0;;) {
+    const int before = __builtin_popcountll(parts & ((1ull << lane) - 1));
+    const uint64_t mine = part ? HW::ballot((parts >> lane & 1) && before == q)
+                               : HW::ballot(lid >= g.before && lid - g.before < g.tiles);
+    if (mine) {
+      const int at = __builtin_ctzll(mine);
+      take_lane<HW>(g, c, at, t);
+      if (!part) t.tile = lid - (int)HW::read_lane((uint32_t)g.before, at);
+      return true;
+    }
+    if (++c == chunks) return false;
+    q -= __builtin_popcountll(parts);
+    lid -= (int)HW::read_lane((uint32_t)g.total, 0);
+    g = group_lane<false, HW>(l, c, shift, width);
+    parts = HW::ballot((g.rows & rest) != 0);
+  }
 }
 
 constexpr int log2_of(int v)
@@ -131,12 +174,18 @@ __device__ __forceinline__ bool place_group(const GroupedArgs& a, Placed<LinearP
 {
   (LinearParams&)p = expand_linear<C>(a.l);
   GroupTile t;
-  if (!group_tile<true, HW>(GroupList{a.offsets, a.groups, a.l.M}, log2_of(C::BM), p.ntn, (int)HW::block_x(), t)) return false;
+  bool part;
+  if (!group_tile<HW>(GroupList{a.offsets, a.groups, a.l.M}, log2_of(C::BM), p.ntn, (int)HW::block_x(), t, part)) return false;
   const int osz = p.out_dtype == 2 ? 4 : 2;
   p.M = p.Mv = t.rows;
-  p.ntm = (t.rows + C::BM - 1) / C::BM;
+  p.ntm = t.rows / C::BM;
   p.group_m = p.ntm < 8 ? p.ntm : 8;
-  tile_in_bands(p, t.tile, p.tile_m, p.tile_n);
+  if (part) {
+    p.tile_m = p.ntm;
+    p.tile_n = t.tile;
+  } else {
+    tile_in_bands(p, t.tile, p.tile_m, p.tile_n);
+  }
   p.A = (const char*)p.A + (long)t.first * p.lda * 2;
   p.B = (const char*)p.B + (long)t.group * a.strideW * 2;
   p.C = (char*)p.C + (long)t.first * p.ldc * osz;
@@ -186,9 +235,7 @@ __global__ void __launch_bounds__(C::NT) alcop_grouped_grad(const GroupedGradArg
   p.ntn = (p.N + C::BN - 1) / C::BN;
   p.group_m = p.ntm < 8 ? p.ntm : 8;
   // all groups have as many tiles: those of a group are neighbours, runs of them go to an XCD each
-  const int per = p.ntm * p.ntn, all = per * a.groups, x = (int)HW::block_x() & 7, rem8 = all & 7;
-  const int r = x * (all >> 3) + (x < rem8 ? x : rem8) + ((int)HW::block_x() >> 3);
-  const int group = r / per;
+  const int per = p.ntm * p.ntn, r = spread_out((int)HW::block_x(), per * a.groups), group = r / per;
   tile_in_bands(p, r - group * per, p.tile_m, p.tile_n);
   GroupTile t;
   t.first = (int)HW::read_lane(HW::global_load_u32(a.offsets + group), 0);
@@ -228,7 +275,7 @@ template <int DT, class HW>
 __global__ void __launch_bounds__(256) alcop_grouped_act_grad(const GroupedActGradArgs p)
 {
   GroupTile t;
-  if (!group_tile<false, HW>(p.l, p.shift, 1, (int)HW::block_y(), t)) return;
+  if (!group_run<HW>(p.l, p.shift, (int)HW::block_y(), t)) return;
   const long r0 = t.first + ((long)t.tile << p.shift), r1 = r0 + (1l << p.shift), end = (long)t.first + t.rows;
   act_grad<DT, HW>(p.a, r0, r1 < end ? r1 : end, (long)HW::block_y());
 }
@@ -244,7 +291,7 @@ __global__ void __launch_bounds__(SUM_THREADS) alcop_grouped_sums(const GroupedS
   const int group = (int)HW::block_y();
   GroupTile t;
   ColumnSumArgs s = p.s;
-  const int count = group_tiles<HW>(p.l, p.shift, group, t);
+  const int count = group_runs<HW>(p.l, p.shift, group, t);
   // offsets that do not rise could count more blocks than there are
   s.count = t.tile + count <= p.s.count ? count : t.tile < p.s.count ? p.s.count - t.tile : 0;
   s.partial += (long)t.tile * s.cols;

@@ -9,11 +9,12 @@ namespace alcop {
 namespace {
 
 // Blocks that walk the rows of the gradients, each leaving a row of sums for dgain and one for dshift; as for the
-// root-mean-square norm, a single block writes them itself.
+// root-mean-square norm, a single block writes them itself.  8192 x 4096 bf16 takes 54.5, 55.4, 60.7 and 70 us with 256, 512, 768 and 1024
+// blocks (their sums are read again: 33 MB with 1024), 1531 x 1111 fp16 20.8, 16.5, 15.9 and 16.6.
 int grad_blocks(int rows, int cols)
 {
   const long blocks = ((long)rows + rows_per_block(rows, cols) - 1) / rows_per_block(rows, cols);
-  return blocks <= 2 ? 1 : (int)std::min(blocks, 1024L);
+  return blocks <= 2 ? 1 : (int)std::min(blocks, 512L);
 }
 
 }  // namespace

@@ -7,10 +7,15 @@
 // As the root-mean-square norm (alcop_rows.hip.h), whose layout of a row this takes over: bound by memory, a row loaded once,
 // held in fp32 registers and stored once, past the caches.
 //
-// The mean is found in two steps.  m = sum(h) / n is off by some 2^-24 of |h|'s mean, which where rows lie far from 0 is not small
-// beside their spread; so the second turn sums d = h - m and d^2 together: mean = m + sum(d) / n, var = mean(d^2) - mean(d)^2, where
-// mean(d) is tiny.  No sum of squares of h itself is formed, and a row needs two turns of the block, as many as the plain
-// two-pass form.  The gradient's two means share a turn.
+// The mean is found in two steps.  sum(h) / n is off by some 2^-24 of |h|'s mean, which where rows lie far from 0 is not small
+// beside their spread; so it only gives a point m near the mean, and the second turn sums d = h - m and d^2 together: mean = m + sum(d) / n,
+// var = mean(d^2) - mean(d)^2.  m is a multiple of 2^-12 of |h|'s mean (down to its power of two): h - m is then exact but for
+// fp32 rows, where a rounding that all of a row's numbers share would not average out of their sum, and mean(d) is so small that its square
+// costs no digits.  No sum of squares of h itself is formed, and a row needs two turns of the block, as many as the plain two-pass form.
+// The gradient's two means share a turn.
+//
+// A block of the norm has one row (one of its waves, up to 1024 columns): 16384 x 4096 bf16 95.5 us, blocks that walk over several rows, the
+// next one loaded ahead of the sums, 97 to 107.  The gradient's blocks walk, for the sums over rows that they keep, and load ahead.
 #pragma once
 #include "alcop_rows.hip.h"
 
@@ -61,37 +66,43 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_rows(const LayerNormArg
   const int me = tid % C::TPR;
   const long row = (long)HW::block_x() * C::ROWS + tid / C::TPR;
   if (row >= p.rows) return;                       // a whole wave, where a wave has a row; else never
-
-  const Raw<C> x = load_raw<C, HW>(row_at<DT>(p.x, row, p.ldx), me, p.cols);
   // ahead of the sums that they do not depend on, where there are registers for them
   constexpr bool AHEAD = C::TPR < 1024 && NV < 4;
+  const float n = (float)p.cols;
   float g[NV][8], b[NV][8];
+
+  Raw<C> x = load_raw<C, HW>(row_at<DT>(p.x, row, p.ldx), me, p.cols), r = {};
+  if (p.residual != nullptr) r = load_raw<C, HW>(row_at<DT>(p.residual, row, p.ldr), me, p.cols);
   if (AHEAD) {
     load_columns<C, HW>(p.gain, 1.0f, me, p.cols, g);
     load_columns<C, HW>(p.shift, 0.0f, me, p.cols, b);
   }
+  finish<C>(x, me, p.cols);
+  if (p.residual != nullptr) finish<C>(r, me, p.cols);
   float h[NV][8];
-  if (p.residual != nullptr) {
-    const Raw<C> r = load_raw<C, HW>(row_at<DT>(p.residual, row, p.ldr), me, p.cols);
-#pragma unroll
-    for (int i = 0; i < NV; i++)
-#pragma unroll
-      for (int e = 0; e < 8; e++) h[i][e] = value<C, HW>(x, i, e) + value<C, HW>(r, i, e);
-  } else {
-#pragma unroll
-    for (int i = 0; i < NV; i++)
-#pragma unroll
-      for (int e = 0; e < 8; e++) h[i][e] = value<C, HW>(x, i, e);
-  }
-  if (p.total != nullptr) store_values<C, DT, HW>((void*)row_at<DT>(p.total, row, p.ldt), me, p.cols, h);
-
-  float s = 0.f;
+  float s = 0.f, size = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; i++)
 #pragma unroll
-    for (int e = 0; e < 8; e++) s += h[i][e];
-  const float n = (float)p.cols;
-  const float m = row_sum<C::TPR, HW>(s, lds) / n;
+    for (int e = 0; e < 8; e++) h[i][e] = value<C, HW>(x, i, e);
+  if (p.residual != nullptr) {
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) h[i][e] += value<C, HW>(r, i, e);
+  }
+  if (p.total != nullptr) store_values<C, DT, HW>((void*)row_at<DT>(p.total, row, p.ldt), me, p.cols, h);
+#pragma unroll
+  for (int i = 0; i < NV; i++)
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      s += h[i][e];
+      size += __builtin_fabsf(h[i][e]);
+    }
+  row_sums<C::TPR, HW>(s, size, lds);
+  // the nearest multiple of 2^-12 of a power of two: what is left when 3 / 2 of 2^23 of them are added and taken away
+  const float many = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, size / n) & 0x7f800000u) * 3072.0f;
+  const float m = (s / n + many) - many;
   float sd = 0.f, sdd = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; i++)
@@ -106,11 +117,11 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_rows(const LayerNormArg
   row_sums<C::TPR, HW>(sd, sdd, lds + 128);
   const float off = sd / n, var = sdd / n - off * off;
   const float rstd = 1.0f / HW::sqrt((var < 0.f ? 0.f : var) + p.eps);       // NaN stays
-  if (!AHEAD) load_columns<C, HW>(p.gain, 1.0f, me, p.cols, g);
   if (me == 0) {
     if (p.mean != nullptr) HW::global_store_u32(p.mean + row, __builtin_bit_cast(uint32_t, m + off));
     if (p.rstd != nullptr) HW::global_store_u32(p.rstd + row, __builtin_bit_cast(uint32_t, rstd));
   }
+  if (!AHEAD) load_columns<C, HW>(p.gain, 1.0f, me, p.cols, g);
   if (!AHEAD) load_columns<C, HW>(p.shift, 0.0f, me, p.cols, b);
 #pragma unroll
   for (int i = 0; i < NV; i++)
@@ -141,17 +152,33 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_grad(const LayerNormGra
   if (GAIN_HELD) load_columns<C, HW>(p.gain, 1.0f, me, p.cols, g);
   const float n = (float)p.cols;
   int turn = 0;
+  // the next row ahead of the sums of the one at hand, where there are registers for it
+  constexpr bool NEXT = HOLD && NV * C::TPR <= 1024;
+  Raw<C> dy2 = {}, h2 = {}, dt2 = {};
+  float mean2 = 0.f, rstd2 = 0.f;
+  auto load_next = [&](long row) __attribute__((always_inline)) {
+    dy2 = load_raw<C, HW>(row_at<DT>(p.dy, row, p.lddy), me, p.cols);
+    h2 = load_raw<C, HW>(row_at<DT>(p.total, row, p.ldt), me, p.cols);
+    if (p.dtotal != nullptr) dt2 = load_raw<C, HW>(row_at<DT>(p.dtotal, row, p.lddt), me, p.cols);
+    mean2 = __builtin_bit_cast(float, HW::global_load_u32(p.mean + row));
+    rstd2 = __builtin_bit_cast(float, HW::global_load_u32(p.rstd + row));
+  };
+  if (NEXT && group < p.rows) load_next(group);
   for (long row = group; row < p.rows; row += groups, turn ^= 1) {
-    const char *dy_row = row_at<DT>(p.dy, row, p.lddy), *h_row = row_at<DT>(p.total, row, p.ldt);
-    Raw<C> dy = load_raw<C, HW>(dy_row, me, p.cols);
-    Raw<C> h = load_raw<C, HW>(h_row, me, p.cols);
-    const char* dt_row = row_at<DT>(p.dtotal, row, p.lddt);
-    Raw<C> dt = {};
-    constexpr bool AHEAD = NV * C::TPR <= 1024;    // of the sums, where there are registers for it
-    if (AHEAD && p.dtotal != nullptr) dt = load_raw<C, HW>(dt_row, me, p.cols);
-    const float mean = __builtin_bit_cast(float, HW::global_load_u32(p.mean + row));
-    const float rstd = __builtin_bit_cast(float, HW::global_load_u32(p.rstd + row));
+    Raw<C> dy, h, dt = {};
+    float mean, rstd;
+    if constexpr (NEXT) {
+      dy = dy2, h = h2, dt = dt2, mean = mean2, rstd = rstd2;
+      if (row + groups < p.rows) load_next(row + groups);
+    } else {
+      dy = load_raw<C, HW>(row_at<DT>(p.dy, row, p.lddy), me, p.cols);
+      h = load_raw<C, HW>(row_at<DT>(p.total, row, p.ldt), me, p.cols);
+      mean = __builtin_bit_cast(float, HW::global_load_u32(p.mean + row));
+      rstd = __builtin_bit_cast(float, HW::global_load_u32(p.rstd + row));
+    }
     if (!GAIN_HELD) load_columns<C, HW>(p.gain, 1.0f, me, p.cols, g);
+    finish<C>(dy, me, p.cols);
+    finish<C>(h, me, p.cols);
     float st = 0.f, stx = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; i++)
@@ -169,9 +196,11 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_grad(const LayerNormGra
     st /= n;
     stx /= n;
     if constexpr (!HOLD) {
-      dy = load_raw<C, HW>(dy_row, me, p.cols);
-      h = load_raw<C, HW>(h_row, me, p.cols);
+      dy = load_raw<C, HW>(row_at<DT>(p.dy, row, p.lddy), me, p.cols);
+      h = load_raw<C, HW>(row_at<DT>(p.total, row, p.ldt), me, p.cols);
       load_columns<C, HW>(p.gain, 1.0f, me, p.cols, g);
+      finish<C>(dy, me, p.cols);
+      finish<C>(h, me, p.cols);
     }
     float dx[NV][8];
 #pragma unroll
@@ -180,7 +209,8 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_grad(const LayerNormGra
       for (int e = 0; e < 8; e++)
         dx[i][e] = rstd * (value<C, HW>(dy, i, e) * g[i][e] - st - (value<C, HW>(h, i, e) - mean) * rstd * stx);
     if (p.dtotal != nullptr) {
-      if (!AHEAD) dt = load_raw<C, HW>(dt_row, me, p.cols);
+      if (!NEXT) dt = load_raw<C, HW>(row_at<DT>(p.dtotal, row, p.lddt), me, p.cols);
+      finish<C>(dt, me, p.cols);
 #pragma unroll
       for (int i = 0; i < NV; i++)
 #pragma unroll
@@ -228,6 +258,18 @@ template <class HW>
 __global__ void __launch_bounds__(SUM_THREADS) alcop_two_column_sums(const TwoColumnSums p)
 {
   column_sums<HW>(HW::block_y() ? p.of[1] : p.of[0]);
+}
+
+// LDS that the norm asks for: more than it needs where fewer blocks on a compute unit are better, as 64 KB of rows (three blocks at least)
+// are enough on their way, and more are read in a worse order.  us with all blocks that the registers allow, and so: 16384 x 4096
+// with a residual, bf16 103 and 95.6, fp32 202 and 188; 8192 x 8192 bf16 95.3 and 93.6; 65536 x 1024 91.8 and 90.3; without
+// a residual 16384 x 4096, 8 KB a block, 64.0 either way.
+template <class C>
+int layernorm_lds(const LayerNormArgs& a)
+{
+  const long block = (long)C::ROWS * a.cols * (C::DT == 2 ? 4 : 2) * (a.residual != nullptr ? 2 : 1);
+  const long blocks = 65536 / block < 3 ? 3 : 65536 / block;
+  return blocks >= 8 || C::TPR == 1024 ? LAYERNORM_LDS_BYTES : (int)(163840 / blocks / 512 * 512);
 }
 
 template <class C>

@@ -29,8 +29,8 @@ const LossTable& loss_table()
   return t;
 }
 
-// The kernel of a step of the lowest cost, as alcop_linear has it.
-const LossKernel* pick(LossStep step, int dt, int M, int N, int K, double bytes)
+// The kernel of a step of the lowest cost, as alcop_linear has it; slices: as many such products in one launch.
+const LossKernel* pick(LossStep step, int dt, int M, int N, int K, double bytes, int slices = 1)
 {
   const LossKernel* best = nullptr;
   double best_us = 0;
@@ -43,7 +43,8 @@ const LossKernel* pick(LossStep step, int dt, int M, int N, int K, double bytes)
       continue;
     }
     if (!k.cost) continue;
-    const double us = linear_us(*k.cost, M, N, K, bytes);
+    const double tiles = (double)(((long)M + k.s.bm - 1) / k.s.bm) * (((long)N + k.s.bn - 1) / k.s.bn) * slices;
+    const double us = linear_us(*k.cost, tiles, (double)M * N * slices, K, bytes);
     if (!best || us < best_us) {
       best = &k;
       best_us = us;
@@ -71,13 +72,16 @@ struct Pieces {
   int width;                   // columns, a multiple of 256 where there are several pieces
   int pitch;                   // of G
   int count;
+  int slices, slice;           // of a piece's columns, for dX
+  bool sums;                   // whether dX is added up in the workspace
   size_t dx, scale, all;       // where they start, and the end
 };
 Pieces pieces_of(int rows, int vocab, int K)
 {
-  // G of a piece: 256 MiB, or 256 columns of so many rows that it is more
+  // G of a piece: 128 MiB, which with what the products read stays in the memory-side cache (4096 rows, 65536 x 2048 bf16, pieces of
+  // 64 to 512 MiB: 2878, 2762, 2896 and 2970 us, of 32 MiB 3200), or 256 columns of so many rows that it is more
   const char* env = std::getenv("ALCOP_LOSS_PIECE");          // a test knob: columns of a piece, a multiple of 256
-  const long most = env && std::atoi(env) > 0 ? (std::atoi(env) + 255) / 256 * 256 : std::max(256L, (1L << 27) / rows / 256 * 256);
+  const long most = env && std::atoi(env) > 0 ? (std::atoi(env) + 255) / 256 * 256 : std::max(256L, (1L << 26) / rows / 256 * 256);
   Pieces p;
   p.width = (int)std::min((long)vocab, most);
   p.count = (int)(((long)vocab + p.width - 1) / p.width);
@@ -88,8 +92,15 @@ Pieces pieces_of(int rows, int vocab, int K)
     p.count = (int)(((long)vocab + p.width - 1) / p.width);
   }
   p.pitch = (p.width + 7) & ~7;
+  // dX: slices of the piece while its largest tiles leave compute units idle, each 2048 columns or more
+  const double tiles = (double)((rows + 255L) / 256) * ((K + 255L) / 256);
+  p.slices = 1;
+  while (p.slices < 16 && tiles * p.slices * 2 <= 256 && p.pitch / (p.slices * 2) >= 2048) p.slices *= 2;
+  p.slice = p.slices > 1 ? (p.pitch / p.slices + 255) / 256 * 256 : p.pitch;
+  p.slices = (p.pitch + p.slice - 1) / p.slice;
+  p.sums = p.count > 1 || p.slices > 1;
   p.dx = r256(2.0 * rows * p.pitch);
-  p.scale = p.dx + (p.count > 1 ? r256(4.0 * rows * K) : 0);
+  p.scale = p.dx + (p.sums ? r256(4.0 * rows * K * p.slices) : 0);
   p.all = p.scale + 256;
   return p;
 }
@@ -230,9 +241,11 @@ int alcop_linear_cross_entropy_backward(const void* X, const void* W, const void
     rc = grid_of(kg[i], rows, n, ldx, ldw, &gg[i]);
     if (rc) return rc;
     if (dX) {
-      kx[i] = pick(LOSS_DX, dt, rows, K, n8, g_bytes + 2.0 * n * (double)K + 8.0 * rows * K);
+      const int slices = (n8 + pc.slice - 1) / pc.slice;
+      kx[i] = pick(LOSS_DX, dt, rows, K, std::min(n8, pc.slice), (g_bytes + 2.0 * n * (double)K) + 8.0 * rows * K * slices, slices);
       rc = grid_of(kx[i], rows, K, pc.pitch, 8, &gx[i]);
       if (rc) return rc;
+      gx[i].y = (unsigned)slices;
       if (2.0 * (n8 + 128.0) * ldw >= 2147483648.0 || 4.0 * 256 * lddx >= 2147483648.0) return ALCOP_ERR_SIZE;
     }
     if (dW) {
@@ -254,7 +267,7 @@ int alcop_linear_cross_entropy_backward(const void* X, const void* W, const void
   const float fixed = scaled && !dloss ? 16384.0f : 1.0f;        // S where |dloss| is 1
   const float* inverse = scaled && dloss ? scale + 1 : nullptr;
   // dX is added up in fp32: where it is to be, or in the workspace
-  const bool direct = pc.count == 1 || out == ALCOP_F32;
+  const bool direct = !pc.sums || (out == ALCOP_F32 && pc.slices == 1);
   for (int i = 0; i < pc.count; i++) {
     const int end = i == pc.count - 1, v0 = i * pc.width, n = end ? last : pc.width, n8 = (n + 7) & ~7;
     LossArgs a;
@@ -284,7 +297,7 @@ int alcop_linear_cross_entropy_backward(const void* X, const void* W, const void
       p.l.W = a.W;
       p.l.C = direct ? dX : sums;
       p.l.ldc = direct ? (int)lddx : K;
-      p.l.residual = i ? p.l.C : nullptr;
+      p.l.residual = i ? p.l.C : nullptr;          // the last piece may have fewer slices: theirs are the first
       p.l.ldr = p.l.ldc;
       p.l.M = rows;
       p.l.N = K;
@@ -295,6 +308,8 @@ int alcop_linear_cross_entropy_backward(const void* X, const void* W, const void
       p.l.flags = (int)(direct ? out : ALCOP_F32);
       p.inverse = inverse;
       p.depth = n;
+      p.slice = std::min(n8, pc.slice);
+      p.next = (long)rows * K;
       if (kx[end]->launch_product(p, gx[end], st) != hipSuccess) return ALCOP_ERR_LAUNCH;
     }
     if (dW) {
@@ -316,7 +331,7 @@ int alcop_linear_cross_entropy_backward(const void* X, const void* W, const void
     }
   }
   if (dX && !direct) {
-    const RoundArgs r{sums, dX, lddx, rows, K, (int)out};
+    const RoundArgs r{sums, dX, lddx, rows, K, (int)out, pc.slices};
     if (launch_round_rows(r, st) != hipSuccess) return ALCOP_ERR_LAUNCH;
   }
   return ALCOP_OK;

@@ -38,5 +38,7 @@ using DwCfg = KCfg<DT, BM, BN, BK, WM, WN, S, R, F, 0, 0, 1>;
 
 #define ALCOP_LOSS_KERNELS(T, DT)                     \
   add_loss<DT, 64, 64, 64, 32, 32, 3, 2, 1>(T);       \
+  add_loss<DT, 128, 64, 64, 64, 32, 3, 2, 1>(T);      \
   add_loss<DT, 128, 128, 64, 64, 64, 2, 2, 1>(T);     \
+  add_loss<DT, 256, 128, 64, 128, 64, 3, 2, 1>(T);    \
   add_loss<DT, 256, 256, 32, 128, 64, 3, 2, 1>(T);

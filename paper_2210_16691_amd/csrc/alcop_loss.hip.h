@@ -328,6 +328,8 @@ struct LossProductArgs {
   LinearArgs l;                // dX: A = G, W = the piece's vectors.  dW: A = G, W = X
   const float* inverse;        // 1 / S, or null = 1
   int depth;                   // dX: the piece's columns, of which K is the next multiple of 8.  dW: its rows, M likewise
+  int slice;                   // dX: columns that blocks y have each, a multiple of 64, or K
+  long next;                   // dX: elements from the sums of one slice to the next one's
 };
 struct DepthParams : LinearParams {
   int depth;
@@ -339,14 +341,23 @@ __device__ __forceinline__ float with_inverse(float alpha, const float* inverse)
 {
   return inverse != nullptr ? alpha * __builtin_bit_cast(float, HW::read_lane(HW::global_load_u32(inverse), 0)) : alpha;
 }
-// G's columns past the piece are 0, the vectors' rows there lie beyond the descriptor
+// G's columns past the piece are 0, the vectors' rows there lie beyond the descriptor.  The piece is a long axis: where dX has too few tiles
+// to fill the card, blocks y add up a slice of it each, in sums of their own.
 template <class C, class HW>
 __global__ void __launch_bounds__(C::NT) alcop_loss_dx(const LossProductArgs a)
 {
   DepthParams p = {};
   (LinearParams&)p = expand_linear<C>(a.l);
   p.alpha = with_inverse<HW>(p.alpha, a.inverse);
-  p.depth = a.depth;
+  const int y = (int)HW::block_y(), k0 = y * a.slice;
+  p.K = p.K - k0 < a.slice ? p.K - k0 : a.slice;
+  p.depth = a.depth - k0 < p.K ? a.depth - k0 : p.K;
+  p.A = (const char*)p.A + (long)k0 * 2;
+  p.B = (const char*)p.B + (long)k0 * p.ldb * 2;
+  if (y) {
+    p.C = (float*)p.C + y * a.next;
+    if (p.residual != nullptr) p.residual = (const float*)p.residual + y * a.next;
+  }
   mainloop_body<C, HW>(p);
 }
 template <class C, class HW>
@@ -359,12 +370,13 @@ __global__ void __launch_bounds__(C::NT) alcop_loss_dw(const LossProductArgs a)
   mainloop_body<C, HW>(p);
 }
 
-// ---- rows of fp32 to 16 bits: dX after the last piece ------------------------------------------------------------------
+// ---- dX after the last piece: the slices' sums, rounded ------------------------------------------------------------------
 struct RoundArgs {
   const float* from;
   void* to;
   long ld;                     // of `to`; `from` has none
   int rows, cols, out;         // cols: a multiple of 8
+  int slices;
 };
 template <class HW>
 __global__ void __launch_bounds__(256) alcop_round_rows(const RoundArgs p)
@@ -377,10 +389,14 @@ __global__ void __launch_bounds__(256) alcop_round_rows(const RoundArgs p)
   float v[8];
 #pragma unroll
   for (int e = 0; e < 8; e++) v[e] = element<8, 2, HW>(r, e);
-  if (p.out == 0)
-    store_row<8, 0, HW, false>(element_at<0>(p.to, row * p.ld + n), v);
-  else
-    store_row<8, 1, HW, false>(element_at<1>(p.to, row * p.ld + n), v);
+  for (int z = 1; z < p.slices; z++) {
+    const RawRow<8, 2> t = load_chunk<8, 2, HW, true>((const char*)(p.from + (z * (long)p.rows + row) * p.cols + n));
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] += element<8, 2, HW>(t, e);
+  }
+  by_type(p.out, [&](auto t) __attribute__((always_inline)) {
+    store_row<8, decltype(t)::value, HW, false>(element_at<decltype(t)::value>(p.to, row * p.ld + n), v);
+  });
 }
 
 }  // namespace alcop

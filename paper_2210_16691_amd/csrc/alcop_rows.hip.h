@@ -11,7 +11,7 @@
 //
 // A row belongs to TPR threads (a wave, or a whole block), each holding NV chunks of eight elements, moved sixteen bytes a load at
 // whatever address they lie (a global access may start at any element).  Where the length is no multiple of eight (!WHOLE)
-// the last chunk goes element by element.
+// the last chunk is loaded as the row's last eight elements and stored in parts.
 //
 // Measured: norm of 16384 x 4096 bf16 with residual and sum 90.6 us = 5.9 TB/s, 8192 x 4096 bf16 to 8 bits 17.2 us, the norm's
 // gradients of 8192 x 4096 51.4 us = 5.2 TB/s and 6 for the sums of the gain's, dZ of 4096 x 4096 20 us = 5.0 TB/s (a copy of
@@ -161,11 +161,34 @@ __device__ __forceinline__ void by_chunk(int me, int i, int cols, F&& whole, G&&
   }
 }
 
-// The chunks of a row as they lie in memory; columns past the end are 0.
+// The chunks of a row as they lie in memory; columns past the end are 0, but for what finish() below is there for.
 template <class C>
 struct Raw {
   RawRow<8, C::DT> c[C::NV];
 };
+// Where a row of cols elements, 8 or more, is not made of chunks, its last chunk is loaded as the eight elements that the row ends with,
+// and chunks past it alike, so that no load waits for a branch; finish() shifts out what is not theirs, once the loads of all
+// matrices are on their way.  end_of_row: the last 8 - k elements in front, zeros behind (1 <= k <= 8).  Element by element it took longer:
+// gradients of the layer norm of 1531 x 1111 fp16 16.5 us, ENDS_AFTER so, norm of 8000 x 1111 bf16 42 and TAIL_AFTER.
+template <int DT>
+__device__ __forceinline__ RawRow<8, DT> end_of_row(RawRow<8, DT> r, int k)
+{
+  constexpr int WORDS = DT == 2 ? 8 : 4;
+#pragma unroll
+  for (int step = WORDS / 2; step >= 1; step /= 2) {
+    const bool by = (k & (DT == 2 ? step : 2 * step)) != 0;
+#pragma unroll
+    for (int i = 0; i < WORDS; i++) r.w[i] = by ? (i + step < WORDS ? r.w[i + step < WORDS ? i + step : 0] : 0u) : r.w[i];
+  }
+  if constexpr (DT != 2) {
+#pragma unroll
+    for (int i = 0; i < WORDS; i++)
+      r.w[i] = k & 1 ? r.w[i] >> 16 | (i + 1 < WORDS ? r.w[i + 1 < WORDS ? i + 1 : 0] << 16 : 0u) : r.w[i];
+  }
+#pragma unroll
+  for (int i = 0; i < WORDS; i++) r.w[i] = k >= 8 ? 0u : r.w[i];
+  return r;
+}
 template <class C, class HW>
 __device__ __forceinline__ Raw<C> load_raw(const void* row, int me, int cols)
 {
@@ -174,17 +197,34 @@ __device__ __forceinline__ Raw<C> load_raw(const void* row, int me, int cols)
 #pragma unroll
   for (int i = 0; i < C::NV; i++) {
     r.c[i] = {};
-    by_chunk<C>(
-        me, i, cols, [&](int n) __attribute__((always_inline)) { r.c[i] = load_chunk<8, DT, HW>(element_at<DT>(row, n)); },
-        [&](int n, int e) __attribute__((always_inline)) {
-          const char* at = element_at<DT>(row, n + e);
-          if constexpr (DT == 2)
-            r.c[i].w[e] = HW::global_load_u32(at);
-          else
-            r.c[i].w[e / 2] |= (uint32_t)HW::global_load_u16(at) << (e & 1 ? 16 : 0);
-        });
+    if (!C::WHOLE && cols >= 8) {
+      const int n = chunk_at<C>(me, i);
+      r.c[i] = load_chunk<8, DT, HW>(element_at<DT>(row, n + 8 <= cols ? n : cols - 8));
+      continue;
+    }
+    if (C::WHOLE || i == 0)          // the others lie past a row shorter than a chunk
+      by_chunk<C>(
+          me, i, cols, [&](int n) __attribute__((always_inline)) { r.c[i] = load_chunk<8, DT, HW>(element_at<DT>(row, n)); },
+          [&](int n, int e) __attribute__((always_inline)) {
+            const char* at = element_at<DT>(row, n + e);
+            if constexpr (DT == 2)
+              r.c[i].w[e] = HW::global_load_u32(at);
+            else
+              r.c[i].w[e / 2] |= (uint32_t)HW::global_load_u16(at) << (e & 1 ? 16 : 0);
+          });
   }
   return r;
+}
+template <class C>
+__device__ __forceinline__ void finish(Raw<C>& r, int me, int cols)
+{
+  if constexpr (!C::WHOLE) {
+#pragma unroll
+    for (int i = 0; i < C::NV; i++) {
+      const int k = chunk_at<C>(me, i) + 8 - cols;
+      if (k > 0 && cols >= 8) r.c[i] = end_of_row<C::DT>(r.c[i], k < 8 ? k : 8);
+    }
+  }
 }
 template <class C, class HW>
 __device__ __forceinline__ float value(const Raw<C>& r, int i, int e)
@@ -192,29 +232,72 @@ __device__ __forceinline__ float value(const Raw<C>& r, int i, int e)
   return element<8, C::DT, HW>(r.c[i], e);
 }
 
-// v[NV][8] to a row of type DT (0, 1, 2; 3: e4m3)
+// v[NV][8] to a row of type DT (0, 1, 2; 3: e4m3).  The last chunk of a row that is not made of them is stored behind the
+// others, in parts: element by element for every chunk that might be the last, it takes more than twice the registers.
 template <class C, int DT, class HW>
 __device__ __forceinline__ void store_values(void* row, int me, int cols, const float (&v)[C::NV][8])
 {
+  constexpr int WORDS = DT == 2 ? 8 : DT == 3 ? 2 : 4;
+  uint32_t last[WORDS];
+  int n1 = cols;               // where the row's last chunk starts, if it is this thread's
 #pragma unroll
-  for (int i = 0; i < C::NV; i++)
-    by_chunk<C>(
-        me, i, cols,
-        [&](int n) __attribute__((always_inline)) {
-          if constexpr (DT == 3) {
-            const uint32_t lo = HW::cvt_e4m3(v[i][0], v[i][1]) | HW::cvt_e4m3(v[i][2], v[i][3]) << 16;
-            const uint32_t hi = HW::cvt_e4m3(v[i][4], v[i][5]) | HW::cvt_e4m3(v[i][6], v[i][7]) << 16;
-            HW::global_store8_byte((char*)row + n, u32x2{lo, hi});
-          } else {
-            store_row<8, DT, HW, false>(element_at<DT>(row, n), v[i]);
-          }
-        },
-        [&](int n, int e) __attribute__((always_inline)) {
-          if constexpr (DT == 3)
-            HW::global_store_u8((char*)row + n + e, (uint8_t)HW::cvt_e4m3(v[i][e], v[i][e]));
+  for (int i = 0; i < C::NV; i++) {
+    const int n = chunk_at<C>(me, i);
+    if (n + 8 <= cols) {
+      if constexpr (DT == 3) {
+        const uint32_t lo = HW::cvt_e4m3(v[i][0], v[i][1]) | HW::cvt_e4m3(v[i][2], v[i][3]) << 16;
+        const uint32_t hi = HW::cvt_e4m3(v[i][4], v[i][5]) | HW::cvt_e4m3(v[i][6], v[i][7]) << 16;
+        HW::global_store8_byte((char*)row + n, u32x2{lo, hi});
+      } else {
+        store_row<8, DT, HW, false>(element_at<DT>(row, n), v[i]);
+      }
+    } else if constexpr (!C::WHOLE) {
+      if (n < cols) {
+        n1 = n;
+#pragma unroll
+        for (int e = 0; e < WORDS; e++) {
+          if constexpr (DT == 2)
+            last[e] = __builtin_bit_cast(uint32_t, v[i][e]);
+          else if constexpr (DT == 3)
+            last[e] = HW::cvt_e4m3(v[i][4 * e], v[i][4 * e + 1]) | HW::cvt_e4m3(v[i][4 * e + 2], v[i][4 * e + 3]) << 16;
           else
-            store_element<DT, HW>(row, n + e, v[i][e]);
-        });
+            last[e] = float_to_half<DT, HW>(v[i][2 * e]) | float_to_half<DT, HW>(v[i][2 * e + 1]) << 16;
+        }
+      }
+    }
+  }
+  if constexpr (!C::WHOLE) {
+    const int k = cols - n1;         // 0 .. 7: fours, twos and ones, each from the low end of what is left
+    if (k & 4) {
+      char* at = const_cast<char*>(DT == 3 ? (const char*)row + n1 : element_at<DT == 3 ? 0 : DT>(row, n1));
+      if constexpr (DT == 2) {
+        HW::global_store16_any(at, u32x4{last[0], last[1], last[2], last[3]});
+      } else if constexpr (DT == 3) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) HW::global_store_u8(at + e, (uint8_t)(last[0] >> 8 * e));
+      } else {
+        HW::global_store8_any(at, u32x2{last[0], last[1]});
+      }
+#pragma unroll
+      for (int e = 0; e < WORDS / 2; e++) last[e] = last[WORDS / 2 + e];
+      n1 += 4;
+    }
+    auto one = [&](uint32_t bits) __attribute__((always_inline)) {
+      if constexpr (DT == 2)
+        HW::global_store_u32((float*)row + n1, bits);
+      else if constexpr (DT == 3)
+        HW::global_store_u8((char*)row + n1, (uint8_t)bits);
+      else
+        HW::global_store_u16((char*)row + 2 * (long)n1, (uint16_t)bits);
+      n1++;
+    };
+    if (k & 2) {
+      one(last[0]);
+      one(DT == 2 ? last[1] : DT == 3 ? last[0] >> 8 : last[0] >> 16);
+      last[0] = DT == 2 ? last[WORDS > 2 ? 2 : 0] : DT == 3 ? last[0] >> 16 : last[1];
+    }
+    if (k & 1) one(last[0]);
+  }
 }
 
 template <class C, class HW>
@@ -225,14 +308,23 @@ __device__ __forceinline__ void load_gain(const float* gain, int me, int cols, f
 #pragma unroll
     for (int e = 0; e < 8; e++) g[i][e] = 1.0f;
     if (gain == nullptr) continue;
-    by_chunk<C>(
-        me, i, cols,
-        [&](int n) __attribute__((always_inline)) {
-          const RawRow<8, 2> t = load_chunk<8, 2, HW>((const char*)(gain + n));
+    if (!C::WHOLE && cols >= 8) {
+      const int n = chunk_at<C>(me, i), k = n + 8 - cols;
+      RawRow<8, 2> t = load_chunk<8, 2, HW>((const char*)(gain + (k <= 0 ? n : cols - 8)));
+      if (k > 0) t = end_of_row<2>(t, k < 8 ? k : 8);
 #pragma unroll
-          for (int e = 0; e < 8; e++) g[i][e] = element<8, 2, HW>(t, e);
-        },
-        [&](int n, int e) __attribute__((always_inline)) { g[i][e] = load_element<2, HW>(gain, n + e); });
+      for (int e = 0; e < 8; e++) g[i][e] = element<8, 2, HW>(t, e);
+      continue;
+    }
+    if (C::WHOLE || i == 0)
+      by_chunk<C>(
+          me, i, cols,
+          [&](int n) __attribute__((always_inline)) {
+            const RawRow<8, 2> t = load_chunk<8, 2, HW>((const char*)(gain + n));
+#pragma unroll
+            for (int e = 0; e < 8; e++) g[i][e] = element<8, 2, HW>(t, e);
+          },
+          [&](int n, int e) __attribute__((always_inline)) { g[i][e] = load_element<2, HW>(gain, n + e); });
   }
 }
 
@@ -315,14 +407,16 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_rows(const NormArgs p)
   const bool norm = (p.flags & 4) != 0;
   const int out = p.flags & 3;
 
-  const Raw<C> x = load_raw<C, HW>(row_at<DT>(p.x, row, p.ldx), me, p.cols);
+  Raw<C> x = load_raw<C, HW>(row_at<DT>(p.x, row, p.ldx), me, p.cols), r = {};
+  if (p.residual != nullptr) r = load_raw<C, HW>(row_at<DT>(p.residual, row, p.ldr), me, p.cols);
   // ahead of the sum that it does not depend on, where there are registers for it
   constexpr bool GAIN_AHEAD = C::TPR < 1024 || NV < 4;
   float g[NV][8];
   if (GAIN_AHEAD && norm) load_gain<C, HW>(p.gain, me, p.cols, g);
   float h[NV][8];
+  finish<C>(x, me, p.cols);
   if (p.residual != nullptr) {
-    const Raw<C> r = load_raw<C, HW>(row_at<DT>(p.residual, row, p.ldr), me, p.cols);
+    finish<C>(r, me, p.cols);
 #pragma unroll
     for (int i = 0; i < NV; i++)
 #pragma unroll
@@ -385,6 +479,8 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_grad(const NormGradArgs p, i
     if (AHEAD && p.dtotal != nullptr) dt = load_raw<C, HW>(dt_row, me, p.cols);
     const float rstd = __builtin_bit_cast(float, HW::global_load_u32(p.rstd + row));
     if (!GAIN_HELD) load_gain<C, HW>(p.gain, me, p.cols, g);
+    finish<C>(dy, me, p.cols);
+    finish<C>(h, me, p.cols);
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; i++)
@@ -399,6 +495,8 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_grad(const NormGradArgs p, i
       dy = load_raw<C, HW>(dy_row, me, p.cols);
       h = load_raw<C, HW>(h_row, me, p.cols);
       load_gain<C, HW>(p.gain, me, p.cols, g);
+      finish<C>(dy, me, p.cols);
+      finish<C>(h, me, p.cols);
     }
     float dx[NV][8];
 #pragma unroll
@@ -408,6 +506,7 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_grad(const NormGradArgs p, i
         dx[i][e] = rstd * (value<C, HW>(dy, i, e) * g[i][e] - value<C, HW>(h, i, e) * rstd * mean);
     if (p.dtotal != nullptr) {
       if (!AHEAD) dt = load_raw<C, HW>(dt_row, me, p.cols);
+      finish<C>(dt, me, p.cols);
 #pragma unroll
       for (int i = 0; i < NV; i++)
 #pragma unroll

@@ -8,7 +8,7 @@ struct Norm {
   static hipError_t go(const LayerNormArgs& a, hipStream_t st)
   {
     alcop_layernorm_rows<C, Gfx950>
-        <<<dim3((unsigned)(((long)a.rows + C::ROWS - 1) / C::ROWS)), dim3(C::NT), LAYERNORM_LDS_BYTES, st>>>(a);
+        <<<dim3((unsigned)(((long)a.rows + C::ROWS - 1) / C::ROWS)), dim3(C::NT), layernorm_lds<C>(a), st>>>(a);
     return hipGetLastError();
   }
 };

@@ -13,7 +13,7 @@ struct Norm {
   static void entry(const void* p) { alcop_layernorm_rows<C, emu::Emu>(*(const LayerNormArgs*)p); }
   static hipError_t go(const LayerNormArgs& a, hipStream_t)
   {
-    emu::run_grid(&entry, &a, C::NT, LAYERNORM_LDS_BYTES, (unsigned)((a.rows + C::ROWS - 1) / C::ROWS), 1, 1);
+    emu::run_grid(&entry, &a, C::NT, LAYERNORM_LDS_BYTES, (unsigned)(((long)a.rows + C::ROWS - 1) / C::ROWS), 1, 1);
     return hipSuccess;
   }
 };

@@ -8,9 +8,9 @@ from layers_util import ULP, act64, act_error, slope64
 def layernorm64(x, residual=None, gain=None, shift=None, eps=1e-5):
     """(y, h, mean, rstd, bound of y's error before the rounding, of the mean's, of rstd's relative one).
 
-    The mean: m = sum / n is off by e <= (n + 2) ULP mean|h|, and mean(h - m) by (n + 2) ULP of the mean of |h - m|, itself at most
-    mean|h - mean| + e; what is left of e is its product with that, so E = (n + 4) ULP (mean|d| + e) + 2 ULP |mean|.
-    h is rounded once on the way in where a residual is added.  The variance: n + 6 roundings, halved by the root, and E^2."""
+    The mean: the point m is within e = (n + 2) ULP mean|h| + 2^-13 mean|h| of it (a sum, and half of a step of 2^-12), and
+    mean(h - m) is off by (n + 2) ULP of the mean of |h - m|, itself at most mean|h - mean| + e: E = (n + 4) ULP (mean|d| + e) + 2 ULP
+    |mean|.  h is rounded once on the way in where a residual is added.  The variance: n + 8 roundings of mean(d^2) = var + e^2 at most."""
     h = x.cpu().double()
     eh = 0.0
     if residual is not None:
@@ -22,7 +22,7 @@ def layernorm64(x, residual=None, gain=None, shift=None, eps=1e-5):
     d = h - mean
     var = d.square().mean(dim=1, keepdim=True)
     rstd = (var + eps).rsqrt()
-    first = (n + 2) * ULP * h.abs().mean(dim=1, keepdim=True)
+    first = ((n + 2) * ULP + 2.0 ** -13) * h.abs().mean(dim=1, keepdim=True)
     em = (n + 4) * ULP * (d.abs().mean(dim=1, keepdim=True) + first) + 2 * ULP * mean.abs()
     if residual is not None:
         em = em + eh.mean(dim=1, keepdim=True)

@@ -9,8 +9,8 @@ from layers_util import DT, check
 from more_util import grouped64, grouped_grad64
 from test_layers_emulated import matrix, some, vector
 
-KERNELS = 7             # per operand type, layout and class of activation (ALCOP_GROUPED_CLASS)
-F8_KERNELS = 3          # and on e4m3 operands with a 16-bit result (ALCOP_GROUPED_F8)
+KERNELS = 9             # per operand type, layout and class of activation (ALCOP_GROUPED_CLASS)
+F8_KERNELS = 5          # and on e4m3 operands with a 16-bit result (ALCOP_GROUPED_F8)
 
 
 def groups_of(m, G):
