@@ -133,3 +133,15 @@ def test_rows_that_do_not_count_have_no_gradient():
     errs = emu.call(al.alcop_linear_cross_entropy_backward, X, W, y, lse, ws, dX=dX, dW=dW, dloss=d, reads=[X, W, y, lse, d],
                     writes=[dX, dW, ws])
     assert not errs and not dX.any() and not dW.any()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_norms_experts_and_loss_together(dtype):
+    from block_util import run_block
+
+    def call(fn, *args, **kw):
+        ts = [t for t in list(args) + list(kw.values()) if isinstance(t, torch.Tensor)]
+        errs = emu.call(fn, *args, reads=ts, writes=ts, **kw)
+        assert not errs, errs[:3]
+
+    run_block(call, "cpu", dtype, 40, 40, 24, [0, 9, 21, 7], 131, behind=3)
