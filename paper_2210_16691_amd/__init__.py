@@ -33,6 +33,10 @@ EXPORTS = [
     "alcop_conv2d_igemm_unaligned", "alcop_init",
     "alcop_linear", "alcop_linear_backward", "alcop_linear_backward_workspace_bytes", "alcop_rmsnorm",
     "alcop_rmsnorm_backward", "alcop_rmsnorm_backward_workspace_bytes", "alcop_quantize_rows",
+    "alcop_layernorm", "alcop_layernorm_backward", "alcop_layernorm_backward_workspace_bytes", "alcop_grouped_linear",
+    "alcop_grouped_linear_backward", "alcop_grouped_linear_backward_workspace_bytes", "alcop_linear_cross_entropy",
+    "alcop_linear_cross_entropy_workspace_bytes", "alcop_linear_cross_entropy_backward",
+    "alcop_linear_cross_entropy_backward_workspace_bytes",
 ]
 
 

@@ -252,6 +252,35 @@ struct Gfx950 {
   }
   // the value that lane (lane ^ mask) of the wave passes
   __device__ static __forceinline__ uint32_t xor_lanes(uint32_t v, int mask) { return (uint32_t)__shfl_xor((int)v, mask); }
+  // The sum over a wave, the same in all lanes, and the sums of the lanes up to each, by moves within and between rows of 16 lanes
+  // (an exchange through __shfl_xor takes an LDS instruction and its wait, some 60 clocks, at each of six steps).
+  // what lane l is given by a move of kind CTRL, 0 where there is no source or ROWS leaves its row out
+  template <int CTRL, int ROWS = 0xf>
+  __device__ static __forceinline__ uint32_t moved(uint32_t v)
+  {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+  }
+  static constexpr int QUAD_XOR_1 = 0xb1, QUAD_XOR_2 = 0x4e, HALF_MIRROR = 0x141, MIRROR = 0x140, SHIFT = 0x110, NEXT_ROW = 0x142, UPPER_HALF = 0x143;
+  __device__ static __forceinline__ float sum_lanes(float v)
+  {
+    v += __builtin_bit_cast(float, moved<QUAD_XOR_1>(__builtin_bit_cast(uint32_t, v)));
+    v += __builtin_bit_cast(float, moved<QUAD_XOR_2>(__builtin_bit_cast(uint32_t, v)));
+    v += __builtin_bit_cast(float, moved<HALF_MIRROR>(__builtin_bit_cast(uint32_t, v)));
+    v += __builtin_bit_cast(float, moved<MIRROR>(__builtin_bit_cast(uint32_t, v)));
+    v += __builtin_bit_cast(float, moved<NEXT_ROW, 0xa>(__builtin_bit_cast(uint32_t, v)));        // lane 15 of rows 0, 2 to rows 1, 3
+    v += __builtin_bit_cast(float, moved<UPPER_HALF, 0xc>(__builtin_bit_cast(uint32_t, v)));      // lane 31 to rows 2, 3
+    return __builtin_bit_cast(float, read_lane(__builtin_bit_cast(uint32_t, v), 63));
+  }
+  __device__ static __forceinline__ uint32_t scan_lanes(uint32_t v)
+  {
+    v += moved<SHIFT + 1>(v);
+    v += moved<SHIFT + 2>(v);
+    v += moved<SHIFT + 4>(v);
+    v += moved<SHIFT + 8>(v);
+    v += moved<NEXT_ROW, 0xa>(v);
+    v += moved<UPPER_HALF, 0xc>(v);
+    return v;
+  }
   // bit l: whether lane l's v is true; the value that lane `lane` (the same for all) passes, in a scalar register
   __device__ static __forceinline__ uint64_t ballot(bool v) { return __builtin_amdgcn_ballot_w64(v); }
   __device__ static __forceinline__ uint32_t read_lane(uint32_t v, int lane)

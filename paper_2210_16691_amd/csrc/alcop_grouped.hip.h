@@ -51,13 +51,9 @@ __device__ __forceinline__ GroupLane group_lane(const GroupList& l, int c, int s
     r.rows = end > r.first ? end - r.first : 0;
     r.tiles = (int)(((uint32_t)r.rows + (PARTS ? (1u << shift) - 1 : 0u)) >> shift) * width;
   }
-  r.total = r.tiles;
-#pragma unroll
-  for (int m = 1; m < 64; m *= 2) {
-    const int o = (int)HW::xor_lanes((uint32_t)r.total, m);
-    if (lane & m) r.before += o;
-    r.total += o;
-  }
+  const int upto = (int)HW::scan_lanes((uint32_t)r.tiles);
+  r.before = upto - r.tiles;
+  r.total = (int)HW::read_lane((uint32_t)upto, 63);
   return r;
 }
 
@@ -86,7 +82,7 @@ __device__ __forceinline__ bool group_run(const GroupList& l, int shift, int lid
       t.tile = lid - (int)HW::read_lane((uint32_t)g.before, lane);
       return true;
     }
-    lid -= (int)HW::read_lane((uint32_t)g.total, 0);
+    lid -= g.total;
   }
   return false;
 }
@@ -97,7 +93,7 @@ __device__ __forceinline__ int group_runs(const GroupList& l, int shift, int gro
   int ahead = 0, c = 0;
   GroupLane g = group_lane<true, HW>(l, 0, shift, 1);
   for (; c < group / 64; c++) {
-    ahead += (int)HW::read_lane((uint32_t)g.total, 0);
+    ahead += g.total;
     g = group_lane<true, HW>(l, c + 1, shift, 1);
   }
   const int lane = group - c * 64;
@@ -122,10 +118,10 @@ __device__ __forceinline__ bool group_tile(const GroupList& l, int shift, int wi
   const int chunks = (l.groups + 63) / 64, lane = HW::lane_id(), rest = (1 << shift) - 1;
   GroupLane g = group_lane<false, HW>(l, 0, shift, width);
   uint64_t parts = HW::ballot((g.rows & rest) != 0);
-  int full = (int)HW::read_lane((uint32_t)g.total, 0), ends = __builtin_popcountll(parts);
+  int full = g.total, ends = __builtin_popcountll(parts);
   for (int c = 1; c < chunks; c++) {
     const GroupLane o = group_lane<false, HW>(l, c, shift, width);
-    full += (int)HW::read_lane((uint32_t)o.total, 0);
+    full += o.total;
     ends += __builtin_popcountll(HW::ballot((o.rows & rest) != 0));
   }
   part = lid >= full;
@@ -148,7 +144,7 @@ __device__ __forceinline__ bool group_tile(const GroupList& l, int shift, int wi
     }
     if (++c == chunks) return false;
     q -= __builtin_popcountll(parts);
-    lid -= (int)HW::read_lane((uint32_t)g.total, 0);
+    lid -= g.total;
     g = group_lane<false, HW>(l, c, shift, width);
     parts = HW::ballot((g.rows & rest) != 0);
   }
@@ -285,8 +281,9 @@ struct GroupedSumArgs {
   GroupList l;
   int shift;
 };
+constexpr int GROUP_SUM_THREADS = 256;      // a group has few of them
 template <class HW>
-__global__ void __launch_bounds__(SUM_THREADS) alcop_grouped_sums(const GroupedSumArgs p)
+__global__ void __launch_bounds__(GROUP_SUM_THREADS) alcop_grouped_sums(const GroupedSumArgs p)
 {
   const int group = (int)HW::block_y();
   GroupTile t;
@@ -296,7 +293,7 @@ __global__ void __launch_bounds__(SUM_THREADS) alcop_grouped_sums(const GroupedS
   s.count = t.tile + count <= p.s.count ? count : t.tile < p.s.count ? p.s.count - t.tile : 0;
   s.partial += (long)t.tile * s.cols;
   s.out += (long)group * s.cols;
-  column_sums<HW>(s);
+  column_sums<HW, GROUP_SUM_THREADS>(s);
 }
 
 // the tiles of dW

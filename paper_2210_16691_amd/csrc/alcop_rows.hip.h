@@ -11,7 +11,7 @@
 //
 // A row belongs to TPR threads (a wave, or a whole block), each holding NV chunks of eight elements, moved sixteen bytes a load at
 // whatever address they lie (a global access may start at any element).  Where the length is no multiple of eight (!WHOLE)
-// the last chunk is loaded as the row's last eight elements and stored in parts.
+// the last chunk is loaded as the row's last eight elements and stored element by element.
 //
 // Measured: norm of 16384 x 4096 bf16 with residual and sum 90.6 us = 5.9 TB/s, 8192 x 4096 bf16 to 8 bits 17.2 us, the norm's
 // gradients of 8192 x 4096 51.4 us = 5.2 TB/s and 6 for the sums of the gain's, dZ of 4096 x 4096 20 us = 5.0 TB/s (a copy of
@@ -95,8 +95,8 @@ __device__ __forceinline__ float row_sum(float v, uint32_t at)
 template <int TPR, class HW>
 __device__ __forceinline__ void row_sums(float& a, float& b, uint32_t at)
 {
-  a = wave_sum<HW>(a);
-  b = wave_sum<HW>(b);
+  a = HW::sum_lanes(a);
+  b = HW::sum_lanes(b);
   if constexpr (TPR > 64) {
     HW::lds_write(at + 8 * HW::wave_id(), u32x2{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)});
     HW::wait_lds();
@@ -232,18 +232,19 @@ __device__ __forceinline__ float value(const Raw<C>& r, int i, int e)
   return element<8, C::DT, HW>(r.c[i], e);
 }
 
-// v[NV][8] to a row of type DT (0, 1, 2; 3: e4m3).  The last chunk of a row that is not made of them is stored behind the
-// others, in parts: element by element for every chunk that might be the last, it takes more than twice the registers.
+// v[NV][8] to a row of type DT (0, 1, 2; 3: e4m3).  The last chunk of a row that is not made of them is picked out first and then stored
+// element by element: unrolled for every chunk that might be the last, that takes more than twice the registers.
 template <class C, int DT, class HW>
 __device__ __forceinline__ void store_values(void* row, int me, int cols, const float (&v)[C::NV][8])
 {
   constexpr int WORDS = DT == 2 ? 8 : DT == 3 ? 2 : 4;
-  uint32_t last[WORDS];
+  uint32_t last[WORDS] = {};
   int n1 = cols;               // where the row's last chunk starts, if it is this thread's
 #pragma unroll
   for (int i = 0; i < C::NV; i++) {
     const int n = chunk_at<C>(me, i);
-    if (n + 8 <= cols) {
+    const bool whole = n + 8 <= cols;
+    if (whole) {
       if constexpr (DT == 3) {
         const uint32_t lo = HW::cvt_e4m3(v[i][0], v[i][1]) | HW::cvt_e4m3(v[i][2], v[i][3]) << 16;
         const uint32_t hi = HW::cvt_e4m3(v[i][4], v[i][5]) | HW::cvt_e4m3(v[i][6], v[i][7]) << 16;
@@ -251,52 +252,37 @@ __device__ __forceinline__ void store_values(void* row, int me, int cols, const 
       } else {
         store_row<8, DT, HW, false>(element_at<DT>(row, n), v[i]);
       }
-    } else if constexpr (!C::WHOLE) {
-      if (n < cols) {
-        n1 = n;
+    }
+    if constexpr (!C::WHOLE) {
+      const bool mine = !whole && n < cols;
+      n1 = mine ? n : n1;
 #pragma unroll
-        for (int e = 0; e < WORDS; e++) {
-          if constexpr (DT == 2)
-            last[e] = __builtin_bit_cast(uint32_t, v[i][e]);
-          else if constexpr (DT == 3)
-            last[e] = HW::cvt_e4m3(v[i][4 * e], v[i][4 * e + 1]) | HW::cvt_e4m3(v[i][4 * e + 2], v[i][4 * e + 3]) << 16;
-          else
-            last[e] = float_to_half<DT, HW>(v[i][2 * e]) | float_to_half<DT, HW>(v[i][2 * e + 1]) << 16;
-        }
+      for (int e = 0; e < WORDS; e++) {
+        uint32_t w;
+        if constexpr (DT == 2)
+          w = __builtin_bit_cast(uint32_t, v[i][e]);
+        else if constexpr (DT == 3)
+          w = HW::cvt_e4m3(v[i][4 * e], v[i][4 * e + 1]) | HW::cvt_e4m3(v[i][4 * e + 2], v[i][4 * e + 3]) << 16;
+        else
+          w = float_to_half<DT, HW>(v[i][2 * e]) | float_to_half<DT, HW>(v[i][2 * e + 1]) << 16;
+        const uint32_t before = last[e];
+        last[e] = mine ? w : before;
       }
     }
   }
   if constexpr (!C::WHOLE) {
-    const int k = cols - n1;         // 0 .. 7: fours, twos and ones, each from the low end of what is left
-    if (k & 4) {
-      char* at = const_cast<char*>(DT == 3 ? (const char*)row + n1 : element_at<DT == 3 ? 0 : DT>(row, n1));
-      if constexpr (DT == 2) {
-        HW::global_store16_any(at, u32x4{last[0], last[1], last[2], last[3]});
-      } else if constexpr (DT == 3) {
+    char* at = (char*)row + (long)n1 * (DT == 2 ? 4 : DT == 3 ? 1 : 2);
 #pragma unroll
-        for (int e = 0; e < 4; e++) HW::global_store_u8(at + e, (uint8_t)(last[0] >> 8 * e));
-      } else {
-        HW::global_store8_any(at, u32x2{last[0], last[1]});
+    for (int e = 0; e < 7; e++) {
+      if (n1 + e < cols) {
+        if constexpr (DT == 2)
+          HW::global_store_u32(at + 4 * e, last[e]);
+        else if constexpr (DT == 3)
+          HW::global_store_u8(at + e, (uint8_t)(last[e / 4] >> 8 * (e % 4)));
+        else
+          HW::global_store_u16(at + 2 * e, (uint16_t)(last[e / 2] >> 16 * (e % 2)));
       }
-#pragma unroll
-      for (int e = 0; e < WORDS / 2; e++) last[e] = last[WORDS / 2 + e];
-      n1 += 4;
     }
-    auto one = [&](uint32_t bits) __attribute__((always_inline)) {
-      if constexpr (DT == 2)
-        HW::global_store_u32((float*)row + n1, bits);
-      else if constexpr (DT == 3)
-        HW::global_store_u8((char*)row + n1, (uint8_t)bits);
-      else
-        HW::global_store_u16((char*)row + 2 * (long)n1, (uint16_t)bits);
-      n1++;
-    };
-    if (k & 2) {
-      one(last[0]);
-      one(DT == 2 ? last[1] : DT == 3 ? last[0] >> 8 : last[0] >> 16);
-      last[0] = DT == 2 ? last[WORDS > 2 ? 2 : 0] : DT == 3 ? last[0] >> 16 : last[1];
-    }
-    if (k & 1) one(last[0]);
   }
 }
 
@@ -539,7 +525,7 @@ __global__ void __launch_bounds__(C::NT) alcop_norm_grad(const NormGradArgs p, i
 // ---- column sums ------------------------------------------------------------------------------------------------------
 // out[j] = sum over i of partial[i][j], in a fixed order: 32 columns a block, 32 runs of rows, then the runs.
 constexpr int SUM_THREADS = 1024, SUM_COLS = 32;
-template <class HW>
+template <class HW, int THREADS = SUM_THREADS>
 __device__ __forceinline__ void column_sums(const ColumnSumArgs& p)
 {
   const uint32_t lds = HW::lds_base();
@@ -549,7 +535,7 @@ __device__ __forceinline__ void column_sums(const ColumnSumArgs& p)
   float s = 0.f;
   if (j < p.cols) {
 #pragma unroll 8
-    for (int i = run; i < p.count; i += SUM_THREADS / SUM_COLS)
+    for (int i = run; i < p.count; i += THREADS / SUM_COLS)
       s += __builtin_bit_cast(float, HW::global_load_u32(p.partial + (long)i * p.cols + j));
   }
   HW::lds_write1(lds + 4 * (run * SUM_COLS + c), __builtin_bit_cast(uint32_t, s));
@@ -558,7 +544,7 @@ __device__ __forceinline__ void column_sums(const ColumnSumArgs& p)
   if (tid >= 64) return;
   float t = 0.f;
 #pragma unroll 4
-  for (int i = 0; i < SUM_THREADS / SUM_COLS; i++) t += __builtin_bit_cast(float, HW::lds_read4(lds + 4 * (i * SUM_COLS + c)));
+  for (int i = 0; i < THREADS / SUM_COLS; i++) t += __builtin_bit_cast(float, HW::lds_read4(lds + 4 * (i * SUM_COLS + c)));
   if (tid < SUM_COLS && j < p.cols) HW::global_store_u32(p.out + j, __builtin_bit_cast(uint32_t, t));
 }
 template <class HW>

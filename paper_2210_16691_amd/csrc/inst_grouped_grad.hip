@@ -20,7 +20,7 @@ hipError_t launch_grouped_act_grad(const GroupedActGradArgs& a, int dt, int runs
 hipError_t launch_grouped_sums(const GroupedSumArgs& a, hipStream_t st)
 {
   const dim3 grid((unsigned)((a.s.cols + SUM_COLS - 1) / SUM_COLS), (unsigned)a.l.groups);
-  alcop_grouped_sums<Gfx950><<<grid, dim3(SUM_THREADS), SUM_THREADS * 4, st>>>(a);
+  alcop_grouped_sums<Gfx950><<<grid, dim3(GROUP_SUM_THREADS), GROUP_SUM_THREADS * 4, st>>>(a);
   return hipGetLastError();
 }
 

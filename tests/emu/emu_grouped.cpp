@@ -80,7 +80,7 @@ hipError_t launch_grouped_act_grad(const GroupedActGradArgs& a, int dt, int runs
 }
 hipError_t launch_grouped_sums(const GroupedSumArgs& a, hipStream_t)
 {
-  emu::run_grid(&entry<&alcop_grouped_sums<emu::Emu>, GroupedSumArgs>, &a, SUM_THREADS, SUM_THREADS * 4,
+  emu::run_grid(&entry<&alcop_grouped_sums<emu::Emu>, GroupedSumArgs>, &a, GROUP_SUM_THREADS, GROUP_SUM_THREADS * 4,
                 (unsigned)((a.s.cols + SUM_COLS - 1) / SUM_COLS), (unsigned)a.l.groups, 1);
   return hipSuccess;
 }

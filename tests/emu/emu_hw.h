@@ -733,6 +733,24 @@ struct Emu {
     wave_sync();
     return W.T[par][l ^ mask];
   }
+  static float sum_lanes(float v)
+  {
+    for (int m = 1; m < 64; m *= 2) {
+      const uint32_t o = xor_lanes(__builtin_bit_cast(uint32_t, v), m);
+      v += __builtin_bit_cast(float, o);
+    }
+    return v;
+  }
+  static uint32_t scan_lanes(uint32_t v)
+  {
+    uint32_t all = v, before = 0;
+    for (int m = 1; m < 64; m *= 2) {
+      const uint32_t o = xor_lanes(all, m);
+      if (lane_id() & m) before += o;
+      all += o;
+    }
+    return before + v;
+  }
   static uint64_t ballot(bool v)
   {
     Block& b = *blk();
