@@ -57,7 +57,11 @@ double grouped_us(const LinearCost& m, long rows, long groups, int N, int K, dou
   const double tiles = live * std::max(1.0, per / m.s.bm + 0.5) * (double)((N + (long)m.s.bn - 1) / m.s.bn);
   const double turns = std::max(1.0, tiles / 256), turns2 = m.blocks == 2 ? 2 * std::max(1.0, tiles / 512) : 0.0;
   const double kt = (double)((K + m.s.bk - 1) / m.s.bk + m.waves_k - 1) / m.waves_k;
-  return m.a + m.b * turns * kt + m.c * turns + m.d * bytes / 5.1e6 + m.e * 2.0 * rows * N * (double)K / 1.4e9 + m.f * turns2 * kt;
+  const double us = m.a + m.b * turns * kt + m.c * turns + m.d * bytes / 5.1e6 + m.e * 2.0 * rows * N * (double)K / 1.4e9 + m.f * turns2 * kt;
+  // tiles of 256x128 are further below these costs than their neighbours: 16384 rows in 16 groups, 4096 x 2048, 354 us for 411 (256x256
+  // 344 for 373, 128x128 385 for 387), in one group 286 for 348; gradients of 8192 rows in 16 groups, 2048 x 2048, 237 with them,
+  // 242 and 250 with the others
+  return m.s.bm == 256 && m.s.bn == 128 ? 0.93 * us : us;
 }
 
 // The kernel of the lowest cost.

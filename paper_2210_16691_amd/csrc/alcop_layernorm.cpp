@@ -9,12 +9,14 @@ namespace alcop {
 namespace {
 
 // Blocks that walk the rows of the gradients, each leaving a row of sums for dgain and one for dshift; as for the
-// root-mean-square norm, a single block writes them itself.  8192 x 4096 bf16 takes 54.5, 55.4, 60.7 and 70 us with 256, 512, 768 and 1024
-// blocks (their sums are read again: 33 MB with 1024), 1531 x 1111 fp16 20.8, 16.5, 15.9 and 16.6.
-int grad_blocks(int rows, int cols)
+// root-mean-square norm, a single block writes them itself.  One block a compute unit, two where its rows are short: more of them leave
+// more sums, which are read again.  us with 256 and 512 blocks: 8192 x 4096 bf16 54.5 and 55.4 (1024: 70), 3000 x 16384 89 and 106, 2000 x
+// 2048 13.6 and 19.4, 20000 x 1024 34.3 and 35.7; 1531 x 1111 fp16 14.2 and 13.0, 4750 x 318 12.7 and 11.8.
+int grad_blocks(int rows, int cols, int size)
 {
   const long blocks = ((long)rows + rows_per_block(rows, cols) - 1) / rows_per_block(rows, cols);
-  return blocks <= 2 ? 1 : (int)std::min(blocks, 512L);
+  const long most = (long)rows_per_block(rows, cols) * cols * size >= 4096 ? 256 : 512;
+  return blocks <= 2 ? 1 : (int)std::min(blocks, most);
 }
 
 }  // namespace
@@ -83,7 +85,7 @@ int alcop_layernorm(const void* x, const void* residual, const void* gain, const
 size_t alcop_layernorm_backward_workspace_bytes(int rows, int cols)
 {
   if (rows <= 0 || cols <= 0 || cols > ROWS_MAX_COLS) return 0;
-  return 2 * r256(4.0 * grad_blocks(rows, cols) * cols);
+  return 2 * r256(4.0 * grad_blocks(rows, cols, 2) * cols);      // 32-bit rows need no more
 }
 
 int alcop_layernorm_backward(const void* dy, const void* total, const void* gain, const void* mean, const void* rstd,
@@ -130,7 +132,7 @@ int alcop_layernorm_backward(const void* dy, const void* total, const void* gain
   a.lddx = lddx;
   a.rows = rows;
   a.cols = cols;
-  const int blocks = grad_blocks(rows, cols);
+  const int blocks = grad_blocks(rows, cols, isz);
   float *sums_g = (float*)workspace, *sums_s = sums ? (float*)((char*)workspace + need / 2) : nullptr;
   a.dgain = !dgain ? nullptr : blocks == 1 ? (float*)dgain : sums_g;
   a.dshift = !dshift ? nullptr : blocks == 1 ? (float*)dshift : sums_s;
