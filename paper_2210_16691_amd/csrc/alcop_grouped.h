@@ -35,8 +35,8 @@ hipError_t prepare_grouped();
 
 }  // namespace alcop
 
-// The kernels of one operand type and layout, each per class of activation.  Fewer tiles than a linear layer has: its
-// 128x64 and 256x128 tiles and the four waves of 64x64 are within a few percent of a neighbour where groups are uneven.
+// The kernels of one operand type and layout, each per class of activation: those of a linear layer but for 64x64 tiles of four waves that
+// split K and the deeper 128x128, which are for few tiles.
 #define ALCOP_GROUPED_CLASS(T, CL, DT, BL)                  \
   add_grouped_ksplit<CL, DT, 16, 16, 8, BL>(T);             \
   add_grouped_ksplit<CL, DT, 16, 32, 8, BL>(T);             \

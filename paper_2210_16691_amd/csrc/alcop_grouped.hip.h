@@ -5,10 +5,15 @@
 //
 // How many rows a group has is known on the device only.  A launch has as many blocks as the rows could make tiles
 // (a partial tile for each group at most), and every wave finds its own tile: a lane per group reads two offsets, the groups' tiles are
-// summed up across the lanes, and the lane whose group holds the block's tile passes it on.  That costs some 0.4 us ahead of the
-// first load, less than a kernel that writes a table (a launch).  Blocks beyond the last tile leave at once.  Full tiles of a
-// group are neighbours, and the eight XCDs get equal runs of them, so that a group's weights are read into one or two L2s.
+// summed up across the lanes, and the lane whose group holds the block's tile passes it on, all ahead of the first load; a kernel that
+// writes a table would be a launch more.  Blocks beyond the last tile leave at once.  Tiles of a group are neighbours, and the eight
+// XCDs get equal runs of them, so that a group's weights are read into one or two L2s (tiles that their groups do not fill put last, to even
+// out the end, read the weights again: 54 groups of 300 rows, 4096 x 2048, 532 us in place of 436).
 // From there on a tile is that of a product of its own: the loops and the epilogue are those of the linear layers.
+//
+// What bounds them.  16384 rows in one group, 4096 x 2048 bf16 with SiLU and pre, take 264 us as the linear layer does (1.04
+// PFLOP/s); in 16 groups of 1024 rows 293, as 268 MB of weights come from memory in place of 17; in 16 uneven ones 340, whose 4.5 turns
+// of 256x256 tiles on the card are five.  32 rows over 32 groups, 2048 x 1024: the weights' bytes, 11 us.
 //
 // Offsets are clamped to 0 .. rows and to rising order where they are read: what they hold decides what is computed, never
 // whether an access is in bounds.
@@ -34,12 +39,12 @@ struct GroupList {
 };
 
 // ---- the tile of a block ---------------------------------------------------------------------------------
-// The rows of group 64 c + lane; its tiles of 2^shift rows, full ones (PARTS: all), times `width`; those of the lanes before it and of
-// all lanes.
+// The rows of group 64 c + lane; its tiles of 2^shift rows, the last one maybe not full, times `width`; those of the lanes before it and
+// of all lanes.
 struct GroupLane {
   int first, rows, tiles, before, total;
 };
-template <bool PARTS, class HW>
+template <class HW>
 __device__ __forceinline__ GroupLane group_lane(const GroupList& l, int c, int shift, int width)
 {
   const int lane = HW::lane_id(), g = c * 64 + lane;
@@ -49,7 +54,7 @@ __device__ __forceinline__ GroupLane group_lane(const GroupList& l, int c, int s
     r.first = a < 0 ? 0 : a > l.rows ? l.rows : a;
     const int end = b > l.rows ? l.rows : b;
     r.rows = end > r.first ? end - r.first : 0;
-    r.tiles = (int)(((uint32_t)r.rows + (PARTS ? (1u << shift) - 1 : 0u)) >> shift) * width;
+    r.tiles = (int)(((uint32_t)r.rows + (1u << shift) - 1) >> shift) * width;
   }
   const int upto = (int)HW::scan_lanes((uint32_t)r.tiles);
   r.before = upto - r.tiles;
@@ -74,7 +79,7 @@ __device__ __forceinline__ bool group_run(const GroupList& l, int shift, int lid
 {
   const int chunks = (l.groups + 63) / 64;
   for (int c = 0; c < chunks; c++) {
-    const GroupLane g = group_lane<true, HW>(l, c, shift, 1);
+    const GroupLane g = group_lane<HW>(l, c, shift, 1);
     const uint64_t mine = HW::ballot(lid >= g.before && lid - g.before < g.tiles);
     if (mine) {
       const int lane = __builtin_ctzll(mine);
@@ -91,10 +96,10 @@ template <class HW>
 __device__ __forceinline__ int group_runs(const GroupList& l, int shift, int group, GroupTile& t)
 {
   int ahead = 0, c = 0;
-  GroupLane g = group_lane<true, HW>(l, 0, shift, 1);
+  GroupLane g = group_lane<HW>(l, 0, shift, 1);
   for (; c < group / 64; c++) {
     ahead += g.total;
-    g = group_lane<true, HW>(l, c + 1, shift, 1);
+    g = group_lane<HW>(l, c + 1, shift, 1);
   }
   const int lane = group - c * 64;
   take_lane<HW>(g, c, lane, t);
@@ -109,45 +114,29 @@ __device__ __forceinline__ int spread_out(int lid, int all)
   return x * (all >> 3) + (x < rem8 ? x : rem8) + (lid >> 3);
 }
 
-// The tile of block `lid` among those of `width` strips of columns: first the full tiles of all groups, then, as they take less time
-// (waves without rows do not multiply) and so even out the end, the groups' last tiles that are not full.  part: such a one,
-// t.tile its strip.  False if there are not so many.
+// The tile of block `lid` among those of `width` strips of columns: the tiles of a group are neighbours, also the ones that it does not
+// fill, so that its weights are read once.  False if there are not so many.
 template <class HW>
-__device__ __forceinline__ bool group_tile(const GroupList& l, int shift, int width, int lid, GroupTile& t, bool& part)
+__device__ __forceinline__ bool group_tile(const GroupList& l, int shift, int width, int lid, GroupTile& t)
 {
-  const int chunks = (l.groups + 63) / 64, lane = HW::lane_id(), rest = (1 << shift) - 1;
-  GroupLane g = group_lane<false, HW>(l, 0, shift, width);
-  uint64_t parts = HW::ballot((g.rows & rest) != 0);
-  int full = g.total, ends = __builtin_popcountll(parts);
-  for (int c = 1; c < chunks; c++) {
-    const GroupLane o = group_lane<false, HW>(l, c, shift, width);
-    full += o.total;
-    ends += __builtin_popcountll(HW::ballot((o.rows & rest) != 0));
-  }
-  part = lid >= full;
-  if (part && lid - full >= ends * width) return false;
-  lid = part ? spread_out(lid - full, ends * width) : spread_out(lid, full);
-  int q = 0;
-  if (part) {
-    q = lid / width;
-    t.tile = lid - q * width;
-  }
-  for (int c = 0;;) {
-    const int before = __builtin_popcountll(parts & ((1ull << lane) - 1));
-    const uint64_t mine = part ? HW::ballot((parts >> lane & 1) && before == q)
-                               : HW::ballot(lid >= g.before && lid - g.before < g.tiles);
+  const int chunks = (l.groups + 63) / 64;
+  GroupLane g = group_lane<HW>(l, 0, shift, width);
+  int all = g.total;
+  for (int c = 1; c < chunks; c++) all += group_lane<HW>(l, c, shift, width).total;
+  if (lid >= all) return false;
+  lid = spread_out(lid, all);
+  for (int c = 0; c < chunks; c++) {
+    if (c) g = group_lane<HW>(l, c, shift, width);
+    const uint64_t mine = HW::ballot(lid >= g.before && lid - g.before < g.tiles);
     if (mine) {
-      const int at = __builtin_ctzll(mine);
-      take_lane<HW>(g, c, at, t);
-      if (!part) t.tile = lid - (int)HW::read_lane((uint32_t)g.before, at);
+      const int lane = __builtin_ctzll(mine);
+      take_lane<HW>(g, c, lane, t);
+      t.tile = lid - (int)HW::read_lane((uint32_t)g.before, lane);
       return true;
     }
-    if (++c == chunks) return false;
-    q -= __builtin_popcountll(parts);
     lid -= g.total;
-    g = group_lane<false, HW>(l, c, shift, width);
-    parts = HW::ballot((g.rows & rest) != 0);
   }
+  return false;
 }
 
 constexpr int log2_of(int v)
@@ -170,18 +159,12 @@ __device__ __forceinline__ bool place_group(const GroupedArgs& a, Placed<LinearP
 {
   (LinearParams&)p = expand_linear<C>(a.l);
   GroupTile t;
-  bool part;
-  if (!group_tile<HW>(GroupList{a.offsets, a.groups, a.l.M}, log2_of(C::BM), p.ntn, (int)HW::block_x(), t, part)) return false;
+  if (!group_tile<HW>(GroupList{a.offsets, a.groups, a.l.M}, log2_of(C::BM), p.ntn, (int)HW::block_x(), t)) return false;
   const int osz = p.out_dtype == 2 ? 4 : 2;
   p.M = p.Mv = t.rows;
-  p.ntm = t.rows / C::BM;
+  p.ntm = (t.rows + C::BM - 1) / C::BM;
   p.group_m = p.ntm < 8 ? p.ntm : 8;
-  if (part) {
-    p.tile_m = p.ntm;
-    p.tile_n = t.tile;
-  } else {
-    tile_in_bands(p, t.tile, p.tile_m, p.tile_n);
-  }
+  tile_in_bands(p, t.tile, p.tile_m, p.tile_n);
   p.A = (const char*)p.A + (long)t.first * p.lda * 2;
   p.B = (const char*)p.B + (long)t.group * a.strideW * 2;
   p.C = (char*)p.C + (long)t.first * p.ldc * osz;

@@ -10,7 +10,7 @@ from gpu_util import DEV
 from layers_util import DT, check
 from more_util import grouped64, grouped_grad64
 from test_gpu_z11_layers import matrix, padding, vector
-from test_grouped_emulated import F8_KERNELS, KERNELS, groups_of, offsets_of, rows_of
+from test_grouped_emulated import F8_KERNELS, GRADIENT_KERNELS, KERNELS, groups_of, offsets_of, rows_of
 
 pytestmark = pytest.mark.gpu
 
@@ -113,6 +113,15 @@ def run_backward(sizes, N, K, dtype, transB, out=None, act=0, pad=0, alpha=1.0, 
 @pytest.mark.parametrize("dtype,transB", [("f16", False), ("f16", True), ("bf16", False), ("bf16", True)])
 def test_gradients(act, dtype, transB):
     run_backward([3, 0, 41, 1, 70, 333], 200, 136, dtype, transB, act=act, pad=8, first=2, behind=3)
+
+
+@pytest.mark.parametrize("kernel", range(GRADIENT_KERNELS))
+@pytest.mark.parametrize("dtype,transB", [("f16", True), ("bf16", False)])
+def test_gradients_of_every_kernel(kernel, dtype, transB, monkeypatch):
+    # the weights' gradients by their own kernels, the rows' by those of the product
+    monkeypatch.setenv("ALCOP_GRADIENT_KERNEL", str(kernel))
+    monkeypatch.setenv("ALCOP_LINEAR_KERNEL", str(kernel + 4))
+    run_backward([3, 0, 41, 1, 270, 700], 328, 264, dtype, transB, act=4, pad=8, first=2, behind=3)
 
 
 def test_gradients_of_larger_products():

@@ -10,6 +10,7 @@ from more_util import grouped64, grouped_grad64
 from test_layers_emulated import matrix, some, vector
 
 KERNELS = 9             # per operand type, layout and class of activation (ALCOP_GROUPED_CLASS)
+GRADIENT_KERNELS = 5    # of the weights' gradients, per operand type (ALCOP_GROUPED_GRAD)
 F8_KERNELS = 5          # and on e4m3 operands with a 16-bit result (ALCOP_GROUPED_F8)
 
 
@@ -147,6 +148,15 @@ def run_backward(sizes, N, K, dtype, transB, out=None, act=0, bias=True, pad=0, 
 @pytest.mark.parametrize("dtype,transB", [("f16", False), ("bf16", True)])
 def test_gradients(act, dtype, transB):
     run_backward([3, 0, 41, 1, 70], 72, 40, dtype, transB, act=act, pad=8, first=2, behind=3, policy=emu.POLICIES[act % 4])
+
+
+@pytest.mark.parametrize("kernel", range(GRADIENT_KERNELS))
+@pytest.mark.parametrize("dtype,transB", [("f16", True), ("bf16", False)])
+def test_gradients_of_every_kernel(kernel, dtype, transB, monkeypatch):
+    # the weights' gradients by their own kernels, the rows' by those of the product
+    monkeypatch.setenv("ALCOP_GRADIENT_KERNEL", str(kernel))
+    monkeypatch.setenv("ALCOP_LINEAR_KERNEL", str(kernel + 4))
+    run_backward([3, 0, 41, 1, 70], 72, 136, dtype, transB, act=4, pad=8, first=2, behind=3, policy=emu.POLICIES[kernel % 4])
 
 
 def test_gradients_of_larger_tiles():
