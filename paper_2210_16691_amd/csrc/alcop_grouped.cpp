@@ -88,16 +88,16 @@ const GroupedKernel* pick(int cls, int dt, int bl, bool fine, int rows, int grou
   return best;
 }
 
-// Rows of a block of alcop_grouped_act_grad, as a power of two: enough blocks to fill the card (2048 with 512 columns each; 8192 rows of
-// 2048 in 16 groups, us of the whole backward pass: 234, 230, 232, 229, 245 and 275 with 4 to 128 rows), each with all its waves at
-// work, and at most 1024 sums to a column beside a group's last.
+// Rows of a block of alcop_grouped_act_grad, as a power of two: enough blocks to fill the card, which finds room for 2048 at a time (1024 with
+// 512 columns each; 8192 rows of 2048 in 16 groups, us of the whole backward pass: 234, 230, 232, 229, 245 and 275 with 4 to 128
+// rows), each with all its waves at work, and at most 1024 sums to a column beside a group's last.
 int act_shift(int rows, int N)
 {
   const int strips = (N + ACT_COLS - 1) / ACT_COLS;
   int lanes = 1, shift = 2;
   while (lanes < 64 && lanes * 8 < N) lanes *= 2;
   while ((1 << shift) < 256 / lanes) shift++;
-  while (shift < 30 && (((long)rows >> shift) * strips > 2048 || ((long)rows >> shift) > 1024)) shift++;
+  while (shift < 30 && (((long)rows >> shift) * strips > 1024 || ((long)rows >> shift) > 1024)) shift++;
   return shift;
 }
 

@@ -212,9 +212,11 @@ __global__ void __launch_bounds__(C::NT) alcop_grouped_grad(const GroupedGradArg
   p.out_dtype = a.out;
   p.ntm = (p.M + C::BM - 1) / C::BM;
   p.ntn = (p.N + C::BN - 1) / C::BN;
-  p.group_m = p.ntm < 8 ? p.ntm : 8;
-  // all groups have as many tiles: those of a group are neighbours, runs of them go to an XCD each
-  const int per = p.ntm * p.ntn, r = spread_out((int)HW::block_x(), per * a.groups), group = r / per;
+  p.group_m = p.ntm < 4 ? p.ntm : 4;
+  // all groups have as many tiles, which take as long as the group has rows: every XCD gets a run of each group's, not groups of its own
+  // (8192 rows in 16 uneven groups, 2048 x 2048, the whole backward pass: 227 us with two groups to an XCD, 218 so, 212 with bands of four
+  // rows of tiles, of which a run needs fewer panels; in 14 groups of 600 rows 202, 211 and 211)
+  const int per = p.ntm * p.ntn, group = (int)HW::block_x() / per, r = group * per + spread_out((int)HW::block_x() - group * per, per);
   tile_in_bands(p, r - group * per, p.tile_m, p.tile_n);
   GroupTile t;
   t.first = (int)HW::read_lane(HW::global_load_u32(a.offsets + group), 0);
