@@ -10,6 +10,7 @@ struct GroupedKernel {
   int cls, dt, bl;             // as in LCfg
   alcop_sched s;
   int threads;
+  bool quarters;               // alcop_grouped_quarters
   hipError_t (*launch)(const GroupedArgs&, dim3, hipStream_t);
   hipError_t (*prepare)();
   const LinearCost* cost = nullptr;
@@ -46,7 +47,7 @@ hipError_t prepare_grouped();
   add_grouped<CL, DT, 128, 64, 64, 64, 32, 3, 2, 1, BL>(T); \
   add_grouped<CL, DT, 128, 128, 64, 64, 64, 2, 2, 1, BL>(T); \
   add_grouped<CL, DT, 256, 128, 64, 128, 64, 3, 2, 1, BL>(T); \
-  add_grouped<CL, DT, 256, 256, 32, 128, 64, 3, 2, 1, BL>(T);
+  add_grouped_quarters<CL, DT, 32, 3, BL>(T);
 #define ALCOP_GROUPED_KERNELS(T, DT, BL)        \
   ALCOP_GROUPED_CLASS(T, CLASS_PLAIN, DT, BL)   \
   ALCOP_GROUPED_CLASS(T, CLASS_SIGMOID, DT, BL) \
@@ -57,7 +58,7 @@ hipError_t prepare_grouped();
   add_grouped<CL, 3, 128, 64, 64, 64, 32, 3, 2, 1, 1>(T);    \
   add_grouped<CL, 3, 128, 128, 64, 64, 64, 2, 2, 1, 1>(T);   \
   add_grouped<CL, 3, 256, 128, 64, 128, 64, 3, 2, 1, 1>(T);  \
-  add_grouped<CL, 3, 256, 256, 64, 128, 64, 2, 2, 1, 1>(T);
+  add_grouped_quarters<CL, 3, 64, 2, 1>(T);
 #define ALCOP_GROUPED_GRAD(T, DT)                              \
   add_grouped_grad<DT, 64, 64, 64, 32, 32, 3, 2, 1>(T);        \
   add_grouped_grad<DT, 128, 64, 64, 64, 32, 3, 2, 1>(T);       \

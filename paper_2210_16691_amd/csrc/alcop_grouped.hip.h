@@ -116,15 +116,25 @@ __device__ __forceinline__ int spread_out(int lid, int all)
 
 // The tile of block `lid` among those of `width` strips of columns: the tiles of a group are neighbours, also the ones that it does not
 // fill, so that its weights are read once.  False if there are not so many.
-template <class HW>
-__device__ __forceinline__ bool group_tile(const GroupList& l, int shift, int width, int lid, GroupTile& t)
+// quarter: what is left behind the last whole turn of the card is dealt out in quarters of a tile, 0 .. 3; -1: a whole one.
+constexpr int CARD = 256;            // compute units, of which each has one of the largest tiles at a time
+template <bool QUARTERS, class HW>
+__device__ __forceinline__ bool group_tile(const GroupList& l, int shift, int width, int lid, GroupTile& t, int& quarter)
 {
   const int chunks = (l.groups + 63) / 64;
   GroupLane g = group_lane<HW>(l, 0, shift, width);
   int all = g.total;
   for (int c = 1; c < chunks; c++) all += group_lane<HW>(l, c, shift, width).total;
-  if (lid >= all) return false;
-  lid = spread_out(lid, all);
+  quarter = -1;
+  const int whole = QUARTERS ? all / CARD * CARD : all;
+  if (lid < whole) {
+    lid = spread_out(lid, whole);
+  } else {
+    if (lid - whole >= 4 * (all - whole)) return false;
+    lid = spread_out(lid - whole, 4 * (all - whole));
+    quarter = lid & 3;
+    lid = whole + (lid >> 2);
+  }
   for (int c = 0; c < chunks; c++) {
     if (c) g = group_lane<HW>(l, c, shift, width);
     const uint64_t mine = HW::ballot(lid >= g.before && lid - g.before < g.tiles);
@@ -154,12 +164,12 @@ struct GroupedArgs {
   long strideW;                // between the weights of two groups, 16-bit units
 };
 
-template <class C, class HW>
-__device__ __forceinline__ bool place_group(const GroupedArgs& a, Placed<LinearParams>& p)
+template <class C, bool QUARTERS, class HW>
+__device__ __forceinline__ bool place_group(const GroupedArgs& a, Placed<LinearParams>& p, int& quarter)
 {
   (LinearParams&)p = expand_linear<C>(a.l);
   GroupTile t;
-  if (!group_tile<HW>(GroupList{a.offsets, a.groups, a.l.M}, log2_of(C::BM), p.ntn, (int)HW::block_x(), t)) return false;
+  if (!group_tile<QUARTERS, HW>(GroupList{a.offsets, a.groups, a.l.M}, log2_of(C::BM), p.ntn, (int)HW::block_x(), t, quarter)) return false;
   const int osz = p.out_dtype == 2 ? 4 : 2;
   p.M = p.Mv = t.rows;
   p.ntm = (t.rows + C::BM - 1) / C::BM;
@@ -179,13 +189,34 @@ template <class C, class HW>
 __global__ void __launch_bounds__(C::NT) alcop_grouped_tile(const GroupedArgs a)
 {
   Placed<LinearParams> p;
-  if (place_group<C, HW>(a, p)) mainloop_body<C, HW>(p);
+  int quarter;
+  if (place_group<C, false, HW>(a, p, quarter)) mainloop_body<C, HW>(p);
 }
 template <class C, class HW>
 __global__ void __launch_bounds__(C::NT) alcop_grouped_ksplit(const GroupedArgs a)
 {
   Placed<LinearParams> p;
-  if (place_group<C, HW>(a, p)) ksplit_body<C, HW>(p);
+  int quarter;
+  if (place_group<C, false, HW>(a, p, quarter)) ksplit_body<C, HW>(p);
+}
+// The largest tiles C, of which a compute unit has one at a time, and quarters Q of them behind the last whole turn of the card: how many
+// tiles uneven groups make is as good as never a multiple of its units, and a turn that a few tiles begin takes as long as one of all.
+// In us with and without quarters, bf16: 16384 x 4096 x 2048 in 16 groups with ends anywhere 337 and 344, with ends at multiples of
+// 32 394 and 422, in 54 groups 420 and 458, in 2 .. 8 groups no difference; 8192 x 2048 x 2048 in 16 groups, gradients, 202 and 209.
+template <class C, class Q, class HW>
+__global__ void __launch_bounds__(C::NT) alcop_grouped_quarters(const GroupedArgs a)
+{
+  static_assert(C::NT == Q::NT && 2 * Q::BM == C::BM && 2 * Q::BN == C::BN, "a quarter of the tile, as many waves");
+  Placed<LinearParams> p;
+  int quarter;
+  if (!place_group<C, true, HW>(a, p, quarter)) return;
+  if (quarter < 0) {
+    mainloop_body<C, HW>(p);
+    return;
+  }
+  p.tile_m = 2 * p.tile_m + (quarter & 1);
+  p.tile_n = 2 * p.tile_n + (quarter >> 1);
+  if (p.tile_m * Q::BM < p.M && p.tile_n * Q::BN < p.N) mainloop_body<Q, HW>(p);
 }
 
 // ---- dW_g = alpha P_g^T Q_g, P and Q stored with the rows' axis first ------------------------------------------

@@ -51,6 +51,16 @@ def test_every_kernel(kernel, dtype, transB, monkeypatch):
     run_grouped([513, 0, 65], 776, 1040, dtype, transB, out=("f16", "bf16", "f32")[(i + 1) % 3], act=(i + 2) % 5)
 
 
+@pytest.mark.parametrize("kernel,dtype,transB", [(KERNELS - 1, "f16", False), (KERNELS - 1, "bf16", True), (KERNELS - 1, "e4m3", True),
+                                                 (KERNELS + F8_KERNELS - 1, "e4m3", True)])
+def test_whole_turns_of_the_largest_tiles_and_quarters_behind_them(kernel, dtype, transB, monkeypatch):
+    monkeypatch.setenv("ALCOP_LINEAR_KERNEL", str(kernel))
+    run_grouped([(3, 130, 0, 257, 1)[g % 5] for g in range(256)] + [5, 300, 129], 264, 208, dtype, transB, act=2, pad=16, first=2,
+                behind=5)
+    run_grouped([1] * 256, 256, 80, dtype, transB, pre=False)
+    run_grouped([2] * 257, 200, 80, dtype, transB, pre=False)
+
+
 @pytest.mark.parametrize("kernel", range(KERNELS, KERNELS + F8_KERNELS))
 @pytest.mark.parametrize("act", [0, 2, 4])
 def test_every_kernel_that_multiplies_8_bits_as_they_are(kernel, act, monkeypatch):
