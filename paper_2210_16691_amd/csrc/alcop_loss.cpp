@@ -261,7 +261,7 @@ int alcop_linear_cross_entropy_backward(const void* X, const void* W, const void
   float *sums = (float*)((char*)workspace + pc.dx), *scale = (float*)((char*)workspace + pc.scale);
   const bool scaled = in == ALCOP_F16;
   if (scaled && dloss) {
-    const LossScaleArgs s{(const float*)dloss, scale, rows};
+    const LossScaleArgs s{(const float*)dloss, labels, scale, rows, vocab};
     if (launch_loss_scale(s, st) != hipSuccess) return ALCOP_ERR_LAUNCH;
   }
   const float fixed = scaled && !dloss ? 16384.0f : 1.0f;        // S where |dloss| is 1

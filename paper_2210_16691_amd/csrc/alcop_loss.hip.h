@@ -13,7 +13,7 @@
 // which none reads or writes rows x vocabulary numbers beyond one piece.
 //
 // G in fp16: its numbers are as small as dloss / vocabulary, which fp16 does not reach.  They are multiplied by a power of two S
-// that takes the largest |dloss| to 2^14 .. 2^15 (G is at most that), and the products by 1 / S.  bf16 has fp32's range, S = 1.
+// that takes the largest |dloss| of the rows that count to 2^14 .. 2^15 (G is at most that), and the products by 1 / S.  bf16 has fp32's range, S = 1.
 //
 // Exponents are of 2: u = z log2 e, exp2(u - shift) with u - shift in one fma from the accumulator.
 #pragma once
@@ -298,10 +298,12 @@ __global__ void __launch_bounds__(1024) alcop_loss_rows(const LossRowsArgs p)
 }
 
 // ---- S: the power of two that takes the largest |dloss| to 2^14 .. 2^15, and 1 / S ---------------------------------
+// Of the rows that count, and of finite ones: what a masked row holds there, or a row that is lost anyway, must not shrink the others.
 struct LossScaleArgs {
   const float* dloss;
+  const void* labels;
   float* scale;
-  int rows;
+  int rows, vocab;
 };
 template <class HW>
 __global__ void __launch_bounds__(1024) alcop_loss_scale(const LossScaleArgs p)
@@ -312,7 +314,9 @@ __global__ void __launch_bounds__(1024) alcop_loss_scale(const LossScaleArgs p)
 #pragma unroll 4
   for (int i = tid; i < p.rows; i += 1024) {
     const uint32_t b = HW::global_load_u32(p.dloss + i) & 0x7fffffffu;
-    top = b > top ? b : top;
+    const char* label = (const char*)p.labels + (long)i * 8;
+    const bool counts = HW::global_load_u32(label + 4) == 0 && HW::global_load_u32(label) < (uint32_t)p.vocab;
+    top = counts && b < 0x7f800000u && b > top ? b : top;
   }
   top = row_max<1024, HW>(top, lds);
   int e = 14 - ((int)(top >> 23) - 127);

@@ -90,6 +90,24 @@ def test_gradients_left_out_and_small():
     run_gradients(70, 5003, 24, "f16", parts="W", out="f32")
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_what_rows_that_do_not_count_hold_does_not_reach_the_others(dtype):
+    rows, vocab, K = 1100, 3001, 136
+    X, W, d = matrix(rows, K, dtype, 1), matrix(vocab, K, dtype, 2, scale=0.2), vector(rows, 4) / rows
+    y, lse = labels_of(rows, vocab, 3).to(DEV), torch.logsumexp(X.float() @ W.float().t(), dim=1)
+    wb = workspace(al.alcop_linear_cross_entropy_backward_workspace_bytes(rows, vocab, K))
+    out = []
+    for masked in (0.0, float("nan"), float("inf"), 1e30):
+        for r in (5, 900, 1099):
+            y[r], d[r], lse[r] = -100, masked, masked
+        dX, dW = torch.zeros_like(X), torch.zeros_like(W)
+        al.alcop_linear_cross_entropy_backward(X, W, y, lse, wb, dX=dX, dW=dW, dloss=d)
+        out.append((dX, dW))
+    assert out[0][0].isfinite().all() and out[0][1].isfinite().all() and out[0][1].any()
+    for dX, dW in out[1:]:
+        assert torch.equal(dX, out[0][0]) and torch.equal(dW, out[0][1])
+
+
 def test_gradients_against_differences():
     # loss in fp32 of logits below 8: off by 2^-20; the third derivative of a log-sum of 40 logits along one weight is below 2 |x|^3
     g = torch.Generator().manual_seed(7)

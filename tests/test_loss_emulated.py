@@ -135,6 +135,34 @@ def test_rows_that_do_not_count_have_no_gradient():
     assert not errs and not dX.any() and not dW.any()
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_what_rows_that_do_not_count_or_are_lost_hold_does_not_reach_the_others(dtype):
+    X, W, d = matrix(6, 16, dtype, 1), matrix(40, 16, dtype, 2), torch.tensor([1e-6, 0.0, 0.0, -1e-3, 0.0, 1e-4])
+    y = torch.tensor([3, -100, 40, 0, 2 ** 33, 39])
+    lse = torch.logsumexp(X.double() @ W.double().t(), dim=1).float()
+    with emu._swapped():
+        ws = torch.empty(al.alcop_linear_cross_entropy_backward_workspace_bytes(6, 40, 16), dtype=torch.uint8).fill_(255)
+
+    def gradients(d, lse):
+        dX, dW = matrix(6, 16, dtype, 3), matrix(40, 16, dtype, 4)
+        errs = emu.call(al.alcop_linear_cross_entropy_backward, X, W, y, lse, ws, dX=dX, dW=dW, dloss=d, reads=[X, W, y, lse, d],
+                        writes=[dX, dW, ws])
+        assert not errs, errs[:3]
+        return dX, dW
+
+    clean, rest = gradients(d, lse), [0, 3, 5]
+    assert clean[0][rest].any(dim=1).all()
+    masked, their = d.clone(), lse.clone()
+    masked[[1, 2, 4]], their[1] = torch.tensor([float("nan"), float("inf"), 1e30]), float("nan")
+    for a, b in zip(clean, gradients(masked, their)):
+        assert torch.equal(a, b)
+    for lost in (float("inf"), float("nan")):
+        bad = d.clone()
+        bad[5] = lost
+        dX = gradients(bad, lse)[0]
+        assert torch.equal(dX[[0, 1, 2, 3, 4]], clean[0][[0, 1, 2, 3, 4]]) and not dX[5].isfinite().any()
+
+
 @pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
 def test_norms_experts_and_loss_together(dtype):
     from block_util import run_block
