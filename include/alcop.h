@@ -548,7 +548,7 @@ int alcop_grouped_linear(const void* A, const void* W, const void* offsets, void
  *     dA = alpha * dZ . W_g^T,   dW_g = alpha * A_g^T . dZ_g  (stored as W_g is),   dbias[g][j] = sum of dZ over the group's rows
  * before the rounding; dW_g and dbias[g] of a group without rows are 0, rows of no group are left as they are in dA.
  *   dA, dW, dbias may be NULL (not all).  Types, alignment and pitches as for alcop_linear_backward; dW_g at dW + g * stridedW,
- *     which do not overlap; dbias: groups x N fp32 values.  groups <= 65535.
+ *     which do not overlap; dbias: groups x N fp32 values.  groups <= 64000.
  *   workspace: DEVICE, 16-byte aligned, at least alcop_grouped_linear_backward_workspace_bytes(rows, groups, N, K) bytes,
  *     needed if act != 0 or dbias is given; as for alcop_linear_backward.
  * For dW, all rows of A and of dZ (dC without an activation), 128 more counted, span less than 2 GiB each; else ALCOP_ERR_SIZE,
@@ -584,7 +584,7 @@ int alcop_linear_cross_entropy(const void* X, const void* W, const void* labels,
  * Its gradients: with G[t][v] = dloss[t] * (exp(z[t][v] - lse[t]) - (v == labels[t])), 0 in rows that do not count,
  *     dX = alpha * G . W,   dW = alpha * G^T . X
  * where G is rounded to the type `in` (the products take 16-bit operands), in fp16 times a power of two that takes the largest
- * |dloss| to 2^14 and more, so that the small numbers of a large vocabulary and a mean over many rows are not lost.
+ * finite |dloss| of the rows that count to 2^14 and more, so that the small numbers of a large vocabulary and a mean over many rows are not lost.
  *   lse: as alcop_linear_cross_entropy left it.  dloss: rows fp32 values, NULL = 1.
  *   dX (rows x K), dW (vocab x K): type `out`, which is `in` or ALCOP_F32; one may be NULL.  16-byte aligned, pitches multiples of 8.
  *   workspace: DEVICE, 16-byte aligned, at least alcop_linear_cross_entropy_backward_workspace_bytes(rows, vocab, K) bytes,

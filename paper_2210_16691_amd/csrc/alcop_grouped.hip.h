@@ -124,7 +124,11 @@ __device__ __forceinline__ bool group_tile(const GroupList& l, int shift, int wi
   const int chunks = (l.groups + 63) / 64;
   GroupLane g = group_lane<HW>(l, 0, shift, width);
   int all = g.total;
-  for (int c = 1; c < chunks; c++) all += group_lane<HW>(l, c, shift, width).total;
+  for (int c = 1; c < chunks; c++) {
+    // a launch has fewer than 2^24 blocks, 64 groups so fewer than 2^30 tiles; all could be more where offsets do not rise
+    const int more = group_lane<HW>(l, c, shift, width).total, most = 1 << 30;
+    all = all > most - more ? most : all + more;
+  }
   quarter = -1;
   const int whole = QUARTERS ? all / CARD * CARD : all;
   if (lid < whole) {

@@ -214,3 +214,25 @@ def test_two_streams_and_the_same_bits_again():
         al.alcop_grouped_linear(A, W, offs, o, transB=True, act=3, stream=s)
     torch.cuda.synchronize()
     assert all(torch.equal(first, o) for o in outs)
+
+
+def test_as_many_groups_as_gradients_take():
+    # rows of 8 against 8 x 8 weights, a few of every eight groups without any
+    G, sizes = 64000, torch.tensor([(0, 1, 3, 0, 2, 1, 1, 1)[g % 8] for g in range(64000)])
+    offs = torch.cat([torch.zeros(1, dtype=torch.int64), sizes.cumsum(0)])
+    rows = int(offs[-1])
+    A, dC, W = matrix(rows, 8, "f16", 1), matrix(rows, 8, "f16", 2), matrix(G * 8, 8, "f16", 3, scale=0.3).view(G, 8, 8)
+    dA, dW, db = torch.full_like(A, float("nan")), torch.full_like(W, float("nan")), torch.full((G, 8), float("nan"), device=DEV)
+    ws = torch.empty(al.alcop_grouped_linear_backward_workspace_bytes(rows, G, 8, 8), dtype=torch.uint8, device=DEV)
+    al.alcop_grouped_linear_backward(dC, A, W, offs.to(DEV, torch.int32), dA=dA, dW=dW, dbias=db, transB=True, workspace=ws)
+    torch.cuda.synchronize()
+    of = torch.repeat_interleave(torch.arange(G), sizes)
+    a, c, w = A.cpu().double(), dC.cpu().double(), W.cpu().double()
+    # half a step of fp16 beside fp32 sums of 8 products, or of 3 rows
+    for got, exact, size in (
+            (dA, (c[:, :, None] * w[of]).sum(1), (c.abs()[:, :, None] * w[of].abs()).sum(1)),
+            (dW, torch.zeros(G, 8, 8, dtype=torch.float64).index_add_(0, of, c[:, :, None] * a[:, None, :]),
+             torch.zeros(G, 8, 8, dtype=torch.float64).index_add_(0, of, (c[:, :, None] * a[:, None, :]).abs())),
+            (db, torch.zeros(G, 8, dtype=torch.float64).index_add_(0, of, c), torch.zeros(G, 8, dtype=torch.float64).index_add_(0, of, c.abs()))):
+        bound = exact.abs() * (2.0 ** -11 if got.dtype == torch.float16 else 2.0 ** -24) + size * 16 * 2.0 ** -24 + 2.0 ** -25
+        assert ((got.cpu().double() - exact).abs() <= bound).all()

@@ -92,7 +92,7 @@ def grouped_backward(dC=P[0], A=P[1], W=P[2], pre=P[3], off=P[4], dA=P[5], dW=P[
     (dict(sdw=4088), SHAPE), (dict(sw=-8), SHAPE), (dict(dC=EIGHT), ALIGN), (dict(A=EIGHT), ALIGN), (dict(W=EIGHT), ALIGN), (dict(pre=EIGHT), ALIGN),
     (dict(dA=EIGHT), ALIGN), (dict(dW=EIGHT), ALIGN), (dict(ws=EIGHT), ALIGN), (dict(db=TWO), ALIGN), (dict(off=TWO), ALIGN),
     (dict(lddc=68), ALIGN), (dict(ldda=68), ALIGN), (dict(sw=4100), ALIGN), (dict(sdw=4100), ALIGN), (dict(lddc=1 << 30), SIZE),
-    (dict(bytes=64), SIZE), (dict(groups=65536), SIZE),
+    (dict(bytes=64), SIZE), (dict(groups=65536), SIZE), (dict(groups=64001), SIZE),
     (dict(dA=P[0]), UNSUPPORTED), (dict(dW=P[1]), UNSUPPORTED), (dict(dA=P[6]), UNSUPPORTED), (dict(db=P[3]), UNSUPPORTED),
     (dict(ws=P[3]), UNSUPPORTED), (dict(ws=P[5]), UNSUPPORTED), (dict(dA=V((3 << 32) + 3 * 8192)), UNSUPPORTED), (dict(db=P[4]), UNSUPPORTED),
 ])
