@@ -58,13 +58,13 @@ double grouped_us(const LinearCost& m, long rows, long groups, int N, int K, dou
   const double turns = std::max(1.0, tiles / 256), turns2 = m.blocks == 2 ? 2 * std::max(1.0, tiles / 512) : 0.0;
   const double kt = (double)((K + m.s.bk - 1) / m.s.bk + m.waves_k - 1) / m.waves_k;
   const double us = m.a + m.b * turns * kt + m.c * turns + m.d * bytes / 5.1e6 + m.e * 2.0 * rows * N * (double)K / 1.4e9 + m.f * turns2 * kt;
-  // The costs are those of one product; groups' tiles end at other rows than its. What three tiles take beside their costs, with the other
-  // tiles of the same products (us, bf16, measured for the cost):
-  //   256x128  16384 x 4096 x 2048 in 16 groups 339 for 411, in one 286 for 348 (128x128 382 for 387, 295 for 331)
-  //   256x256  16384 x 4096 x 2048 in 16 groups 337 for 373, in one 262 for 282; 8192 x 2048 x 2048 in 16 groups, gradients, 202
-  //            (256x128 205, 128x128 224)
+  // The costs are those of one product; groups' tiles end at other rows than its, and the two large ones are quartered.  What three tiles
+  // take beside their costs, with the other tiles of the same products (us, bf16, measured for the cost):
+  //   256x256  16384 x 4096 x 2048 in 16 groups 336 for 373, in one 267 for 282; 2500 rows in 5 66 (256x128 71); 8192 x 2048 x 2048 in
+  //            16 groups, gradients, 202 (256x128 206, 128x128 224)
+  //   256x128  the first in 16 groups 343 for 411, in one 286 for 348 (128x128 382 for 387, 295 for 331)
   //   128x64   1531 x 1048 x 520 in 12 groups, fp16, 12.3 for 9.2 (64x64 11.0 for 9.3); 1150 x 2048 x 1024 in 4 14.2 (64x64 13.7)
-  const double side = m.s.bm == 256 ? (m.s.bn == 128 ? 0.86 : 0.92) : m.s.bm == 128 && m.s.bn == 64 ? 1.08 : 1.0;
+  const double side = m.s.bm == 256 ? (m.s.bn == 128 ? 0.86 : 0.88) : m.s.bm == 128 && m.s.bn == 64 ? 1.08 : 1.0;
   return side * us;
 }
 
@@ -141,7 +141,7 @@ int plan_product(const GroupedArgs& a, int cls, int dt, int bl, bool fine, int o
   if (2.0 * rows * l.lda >= 2147483648.0 || (bl ? 2.0 * cols * l.ldw : 2.0 * kceil * l.ldw) >= 2147483648.0) return ALCOP_ERR_SIZE;
   if (osz * rows * (double)std::max(l.ldc, l.ldp) >= 2147483648.0) return ALCOP_ERR_SIZE;
   const long strips = ((long)l.N + k->s.bn - 1) / k->s.bn, tiles = most_tiles(l.M, a.groups, k->s.bm);
-  const long blocks = tiles * strips + (k->quarters ? 3L * (CARD - 1) : 0);      // tiles and strips are below 2^32
+  const long blocks = tiles * strips + (k->quarters ? 3L * (CARD / 2) : 0);      // tiles and strips are below 2^32
   if (blocks >= (1L << 32) / k->threads) return ALCOP_ERR_SHAPE;                 // threads are counted in 32 bits
   if (std::getenv("ALCOP_LOG"))
     std::fprintf(stderr, "alcop: grouped linear rows %d groups %d N %d K %d in %d -> tile %dx%dx%d waves %dx%d S%d R%d F%d variant %d grid %ld\n",

@@ -46,8 +46,8 @@ hipError_t prepare_grouped();
   add_grouped<CL, DT, 64, 64, 64, 32, 32, 3, 2, 1, BL>(T);  \
   add_grouped<CL, DT, 128, 64, 64, 64, 32, 3, 2, 1, BL>(T); \
   add_grouped<CL, DT, 128, 128, 64, 64, 64, 2, 2, 1, BL>(T); \
-  add_grouped<CL, DT, 256, 128, 64, 128, 64, 3, 2, 1, BL>(T); \
-  add_grouped_quarters<CL, DT, 32, 3, BL>(T);
+  add_grouped_quarters<CL, DT, 256, 128, 64, 128, 64, 3, BL>(T); \
+  add_grouped_quarters<CL, DT, 256, 256, 32, 128, 64, 3, BL>(T);
 #define ALCOP_GROUPED_KERNELS(T, DT, BL)        \
   ALCOP_GROUPED_CLASS(T, CLASS_PLAIN, DT, BL)   \
   ALCOP_GROUPED_CLASS(T, CLASS_SIGMOID, DT, BL) \
@@ -57,8 +57,8 @@ hipError_t prepare_grouped();
   add_grouped<CL, 3, 64, 64, 64, 32, 32, 3, 2, 1, 1>(T);     \
   add_grouped<CL, 3, 128, 64, 64, 64, 32, 3, 2, 1, 1>(T);    \
   add_grouped<CL, 3, 128, 128, 64, 64, 64, 2, 2, 1, 1>(T);   \
-  add_grouped<CL, 3, 256, 128, 64, 128, 64, 3, 2, 1, 1>(T);  \
-  add_grouped_quarters<CL, 3, 64, 2, 1>(T);
+  add_grouped_quarters<CL, 3, 256, 128, 64, 128, 64, 3, 1>(T);  \
+  add_grouped_quarters<CL, 3, 256, 256, 64, 128, 64, 2, 1>(T);
 #define ALCOP_GROUPED_GRAD(T, DT)                              \
   add_grouped_grad<DT, 64, 64, 64, 32, 32, 3, 2, 1>(T);        \
   add_grouped_grad<DT, 128, 64, 64, 64, 32, 3, 2, 1>(T);       \

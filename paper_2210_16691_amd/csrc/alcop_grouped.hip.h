@@ -11,9 +11,9 @@
 // out the end, read the weights again: 54 groups of 300 rows, 4096 x 2048, 532 us in place of 436).
 // From there on a tile is that of a product of its own: the loops and the epilogue are those of the linear layers.
 //
-// What bounds them.  16384 rows in one group, 4096 x 2048 bf16 with SiLU and pre, take 264 us as the linear layer does (1.04
-// PFLOP/s); in 16 groups of 1024 rows 293, as 268 MB of weights come from memory in place of 17; in 16 uneven ones 340, whose 4.5 turns
-// of 256x256 tiles on the card are five.  32 rows over 32 groups, 2048 x 1024: the weights' bytes, 11 us.
+// What bounds them.  16384 rows in one group, 4096 x 2048 bf16 with SiLU and pre, take 267 us as the linear layer does (1.03
+// PFLOP/s); in 16 even groups 293, as 268 MB of weights come from memory in place of 17; in 16 uneven ones 336: tiles that their groups
+// do not fill, and the turn of the card that the last ones begin.  32 rows over 32 groups, 2048 x 1024: the weights' bytes, 11 us.
 //
 // Offsets are clamped to 0 .. rows and to rising order where they are read: what they hold decides what is computed, never
 // whether an access is in bounds.
@@ -116,9 +116,10 @@ __device__ __forceinline__ int spread_out(int lid, int all)
 
 // The tile of block `lid` among those of `width` strips of columns: the tiles of a group are neighbours, also the ones that it does not
 // fill, so that its weights are read once.  False if there are not so many.
-// quarter: what is left behind the last whole turn of the card is dealt out in quarters of a tile, 0 .. 3; -1: a whole one.
-constexpr int CARD = 256;            // compute units, of which each has one of the largest tiles at a time
-template <bool QUARTERS, class HW>
+// quarter: what is left behind the last whole turn of the card, up to QUARTERED tiles, is dealt out in quarters of a tile, 0 .. 3; -1: a
+// whole one.
+constexpr int CARD = 256;            // compute units, of which each has one of the large tiles at a time
+template <int QUARTERED, class HW>
 __device__ __forceinline__ bool group_tile(const GroupList& l, int shift, int width, int lid, GroupTile& t, int& quarter)
 {
   const int chunks = (l.groups + 63) / 64;
@@ -130,7 +131,7 @@ __device__ __forceinline__ bool group_tile(const GroupList& l, int shift, int wi
     all = all > most - more ? most : all + more;
   }
   quarter = -1;
-  const int whole = QUARTERS ? all / CARD * CARD : all;
+  const int whole = all % CARD <= QUARTERED ? all / CARD * CARD : all;
   if (lid < whole) {
     lid = spread_out(lid, whole);
   } else {
@@ -168,12 +169,12 @@ struct GroupedArgs {
   long strideW;                // between the weights of two groups, 16-bit units
 };
 
-template <class C, bool QUARTERS, class HW>
+template <class C, int QUARTERED, class HW>
 __device__ __forceinline__ bool place_group(const GroupedArgs& a, Placed<LinearParams>& p, int& quarter)
 {
   (LinearParams&)p = expand_linear<C>(a.l);
   GroupTile t;
-  if (!group_tile<QUARTERS, HW>(GroupList{a.offsets, a.groups, a.l.M}, log2_of(C::BM), p.ntn, (int)HW::block_x(), t, quarter)) return false;
+  if (!group_tile<QUARTERED, HW>(GroupList{a.offsets, a.groups, a.l.M}, log2_of(C::BM), p.ntn, (int)HW::block_x(), t, quarter)) return false;
   const int osz = p.out_dtype == 2 ? 4 : 2;
   p.M = p.Mv = t.rows;
   p.ntm = (t.rows + C::BM - 1) / C::BM;
@@ -194,26 +195,35 @@ __global__ void __launch_bounds__(C::NT) alcop_grouped_tile(const GroupedArgs a)
 {
   Placed<LinearParams> p;
   int quarter;
-  if (place_group<C, false, HW>(a, p, quarter)) mainloop_body<C, HW>(p);
+  if (place_group<C, 0, HW>(a, p, quarter)) mainloop_body<C, HW>(p);
 }
 template <class C, class HW>
 __global__ void __launch_bounds__(C::NT) alcop_grouped_ksplit(const GroupedArgs a)
 {
   Placed<LinearParams> p;
   int quarter;
-  if (place_group<C, false, HW>(a, p, quarter)) ksplit_body<C, HW>(p);
+  if (place_group<C, 0, HW>(a, p, quarter)) ksplit_body<C, HW>(p);
 }
-// The largest tiles C, of which a compute unit has one at a time, and quarters Q of them behind the last whole turn of the card: how many
+// Large tiles C, of which a compute unit has one at a time, and quarters Q of them behind the last whole turn of the card: how many
 // tiles uneven groups make is as good as never a multiple of its units, and a turn that a few tiles begin takes as long as one of all.
-// In us with and without quarters, bf16: 16384 x 4096 x 2048 in 16 groups with ends anywhere 337 and 344, with ends at multiples of
-// 32 394 and 422, in 54 groups 420 and 458, in 2 .. 8 groups no difference; 8192 x 2048 x 2048 in 16 groups, gradients, 202 and 209.
+// Of 256x256 tiles up to 128 are quartered (two turns of quarters), of 256x128, whose quarters load more for each product, up to 64 (one turn).
+// us, bf16, with none, 64, 128, 192 and all quartered:
+//   256x256  16384 x 4096 x 2048 in 16 groups 344, 345, 336, 336, 336; 4000 rows in 2 96.8, 78.7, 77.6, 78.4, 78.1; 2500 in 5 66.1,
+//            65.7, 65.7, 72.9, 80.3; 8192 x 2048 x 2048 in 16 groups, gradients, 223, 213, 208, 207, 207, of 5000 in 7 137, 138, 137, 145, 145
+//   256x128  the first 344, 343, 341, 342, 341; 4000 rows in 2 91.9, 82.8, 83.2, 83.1, 82.9; 2500 in 5 70.5, 71.0, 73.9, 81.6, 82.0;
+//            the gradients 210, 210, 212, 226, 224
+template <class C>
+constexpr int quartered()
+{
+  return C::BN >= 256 ? CARD / 2 : CARD / 4;
+}
 template <class C, class Q, class HW>
 __global__ void __launch_bounds__(C::NT) alcop_grouped_quarters(const GroupedArgs a)
 {
   static_assert(C::NT == Q::NT && 2 * Q::BM == C::BM && 2 * Q::BN == C::BN, "a quarter of the tile, as many waves");
   Placed<LinearParams> p;
   int quarter;
-  if (!place_group<C, true, HW>(a, p, quarter)) return;
+  if (!place_group<C, quartered<C>(), HW>(a, p, quarter)) return;
   if (quarter < 0) {
     mainloop_body<C, HW>(p);
     return;

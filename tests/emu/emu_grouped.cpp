@@ -35,13 +35,13 @@ template <int CL, int DT, int BM, int BN, int NW, int BL>
   t.push_back(GroupedKernel{CL, DT, BL, alcop_sched{BM, BN, 64, BM, BN, 2, 1, 0, 1, 0, 3}, C::NT, false,
                             &launch_kernel<C, &alcop_grouped_ksplit<C, emu::Emu>, GroupedArgs>, &prepare_none});
 }
-template <int CL, int DT, int BK, int S, int BL>
+template <int CL, int DT, int BM, int BN, int BK, int WM, int WN, int S, int BL>
 [[maybe_unused]] void add_grouped_quarters(std::vector<GroupedKernel>& t)
 {
-  using C = LCfg<CL, DT, 256, 256, BK, 128, 64, S, 2, 1, BL>;
-  using Q = LCfg<CL, DT, 128, 128, 64, 64, 32, 3, 2, 1, BL>;
+  using C = LCfg<CL, DT, BM, BN, BK, WM, WN, S, 2, 1, BL>;
+  using Q = LCfg<CL, DT, BM / 2, BN / 2, 64, WM / 2, WN / 2, 3, 2, 1, BL>;
   static_assert(C::LDS_BYTES >= Q::LDS_BYTES, "what is asked for is what the whole tiles need");
-  t.push_back(GroupedKernel{CL, DT, BL, alcop_sched{256, 256, BK, 128, 64, S, 2, 1, 1, 0, 0}, C::NT, true,
+  t.push_back(GroupedKernel{CL, DT, BL, alcop_sched{BM, BN, BK, WM, WN, S, 2, 1, 1, 0, 0}, C::NT, true,
                             &launch_kernel<C, &alcop_grouped_quarters<C, Q, emu::Emu>, GroupedArgs>, &prepare_none});
 }
 template <int DT, int BM, int BN, int BK, int WM, int WN, int S, int R, int F>

@@ -52,8 +52,9 @@ def test_every_kernel(kernel, dtype, transB, monkeypatch):
 
 
 @pytest.mark.parametrize("kernel,dtype,transB", [(KERNELS - 1, "f16", False), (KERNELS - 1, "bf16", True), (KERNELS - 1, "e4m3", True),
-                                                 (KERNELS + F8_KERNELS - 1, "e4m3", True)])
-def test_whole_turns_of_the_largest_tiles_and_quarters_behind_them(kernel, dtype, transB, monkeypatch):
+                                                 (KERNELS - 2, "f16", True), (KERNELS - 2, "bf16", False), (KERNELS - 2, "e4m3", True),
+                                                 (KERNELS + F8_KERNELS - 1, "e4m3", True), (KERNELS + F8_KERNELS - 2, "e4m3", True)])
+def test_whole_turns_of_the_large_tiles_and_quarters_behind_them(kernel, dtype, transB, monkeypatch):
     monkeypatch.setenv("ALCOP_LINEAR_KERNEL", str(kernel))
     run_grouped([(3, 130, 0, 257, 1)[g % 5] for g in range(256)] + [5, 300, 129], 264, 208, dtype, transB, act=2, pad=16, first=2,
                 behind=5)

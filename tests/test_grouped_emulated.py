@@ -73,7 +73,7 @@ def test_every_kernel_that_multiplies_8_bits_as_they_are(kernel, act, monkeypatc
         run_grouped([4], 16, 16, "e4m3", True, out="f32")
 
 
-def test_whole_turns_of_the_largest_tiles_and_quarters_behind_them(monkeypatch):
+def test_whole_turns_of_the_large_tiles_and_quarters_behind_them(monkeypatch):
     monkeypatch.setenv("ALCOP_LINEAR_KERNEL", str(KERNELS - 1))
     run_grouped([1] * 255 + [0, 130, 2], 16, 16, "f16", True, pre=False, first=2, behind=3)
 
