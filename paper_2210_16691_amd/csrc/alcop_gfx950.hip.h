@@ -263,13 +263,18 @@ struct Gfx950 {
   static constexpr int QUAD_XOR_1 = 0xb1, QUAD_XOR_2 = 0x4e, HALF_MIRROR = 0x141, MIRROR = 0x140, SHIFT = 0x110, NEXT_ROW = 0x142, UPPER_HALF = 0x143;
   __device__ static __forceinline__ float sum_lanes(float v)
   {
-    v += __builtin_bit_cast(float, moved<QUAD_XOR_1>(__builtin_bit_cast(uint32_t, v)));
-    v += __builtin_bit_cast(float, moved<QUAD_XOR_2>(__builtin_bit_cast(uint32_t, v)));
-    v += __builtin_bit_cast(float, moved<HALF_MIRROR>(__builtin_bit_cast(uint32_t, v)));
-    v += __builtin_bit_cast(float, moved<MIRROR>(__builtin_bit_cast(uint32_t, v)));
+    v = sum_sixteen(v);
     v += __builtin_bit_cast(float, moved<NEXT_ROW, 0xa>(__builtin_bit_cast(uint32_t, v)));        // lane 15 of rows 0, 2 to rows 1, 3
     v += __builtin_bit_cast(float, moved<UPPER_HALF, 0xc>(__builtin_bit_cast(uint32_t, v)));      // lane 31 to rows 2, 3
     return __builtin_bit_cast(float, read_lane(__builtin_bit_cast(uint32_t, v), 63));
+  }
+  // the sum over a row of 16 lanes, the same in all of them
+  __device__ static __forceinline__ float sum_sixteen(float v)
+  {
+    v += __builtin_bit_cast(float, moved<QUAD_XOR_1>(__builtin_bit_cast(uint32_t, v)));
+    v += __builtin_bit_cast(float, moved<QUAD_XOR_2>(__builtin_bit_cast(uint32_t, v)));
+    v += __builtin_bit_cast(float, moved<HALF_MIRROR>(__builtin_bit_cast(uint32_t, v)));
+    return v + __builtin_bit_cast(float, moved<MIRROR>(__builtin_bit_cast(uint32_t, v)));
   }
   __device__ static __forceinline__ uint32_t scan_lanes(uint32_t v)
   {

@@ -14,8 +14,8 @@ namespace {
 // 2048 13.6 and 19.4, 20000 x 1024 34.3 and 35.7; 1531 x 1111 fp16 14.2 and 13.0, 4750 x 318 12.7 and 11.8.
 int grad_blocks(int rows, int cols, int size)
 {
-  const long blocks = ((long)rows + rows_per_block(rows, cols) - 1) / rows_per_block(rows, cols);
-  const long most = (long)rows_per_block(rows, cols) * cols * size >= 4096 ? 256 : 512;
+  const long blocks = ((long)rows + layernorm_rows_per_block(rows, cols) - 1) / layernorm_rows_per_block(rows, cols);
+  const long most = (long)layernorm_rows_per_block(rows, cols) * cols * size >= 4096 ? 256 : 512;
   return blocks <= 2 ? 1 : (int)std::min(blocks, most);
 }
 
@@ -36,7 +36,7 @@ int alcop_layernorm(const void* x, const void* residual, const void* gain, const
   if (rows <= 0 || cols <= 0) return ALCOP_ERR_SHAPE;
   if (ldx < cols || ldy < cols || (residual && ldr < cols) || (total && ldt < cols)) return ALCOP_ERR_SHAPE;
   if (cols > ROWS_MAX_COLS) return ALCOP_ERR_SIZE;
-  if (rows / rows_per_block(rows, cols) >= (1 << 22) - 1) return ALCOP_ERR_SIZE;    // threads of a launch: 32 bits, 1024 a block
+  if (rows / layernorm_rows_per_block(rows, cols) >= (1 << 22) - 1) return ALCOP_ERR_SIZE;    // threads of a launch: 32 bits, 1024 a block
   const int isz = size_of(in), osz = size_of(out);
   if (!aligned(x, isz) || !aligned(residual, isz) || !aligned(total, isz) || !aligned(y, osz)) return ALCOP_ERR_ALIGN;
   for (const void* p : {gain, shift, (const void*)scale, (const void*)mean, (const void*)rstd})
@@ -137,7 +137,7 @@ int alcop_layernorm_backward(const void* dy, const void* total, const void* gain
   a.dgain = !dgain ? nullptr : blocks == 1 ? (float*)dgain : sums_g;
   a.dshift = !dshift ? nullptr : blocks == 1 ? (float*)dshift : sums_s;
   hipStream_t st = (hipStream_t)hip_stream;
-  if (launch_layernorm_grad(a, blocks * rows_per_block(rows, cols), (int)in, cols % 8 == 0, st) != hipSuccess)
+  if (launch_layernorm_grad(a, blocks * layernorm_rows_per_block(rows, cols), (int)in, cols % 8 == 0, st) != hipSuccess)
     return ALCOP_ERR_LAUNCH;
   if (sums && blocks > 1) {
     TwoColumnSums s;

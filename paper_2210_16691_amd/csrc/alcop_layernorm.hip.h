@@ -14,8 +14,8 @@
 // costs no digits.  No sum of squares of h itself is formed, and a row needs two turns of the block, as many as the plain two-pass form.
 // The gradient's two means share a turn.
 //
-// A block of the norm has one row (one of its waves, up to 1024 columns): 16384 x 4096 bf16 95.5 us, blocks that walk over several rows, the
-// next one loaded ahead of the sums, 97 to 107.  The gradient's blocks walk, for the sums over rows that they keep, and load ahead.
+// A block of the norm has one row (one of its waves up to 1024 columns, sixteen of its lanes up to 256): 16384 x 4096 bf16 94 us, blocks that walk over several rows, the
+// next one loaded ahead of the sums, 97 to 107 where this took 95.5.  The gradient's blocks walk, for the sums over rows that they keep, and load ahead.
 #pragma once
 #include "alcop_rows.hip.h"
 
@@ -64,8 +64,11 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_rows(const LayerNormArg
   const uint32_t lds = HW::lds_base();
   const int tid = HW::wave_id() * 64 + HW::lane_id();
   const int me = tid % C::TPR;
-  const long row = (long)HW::block_x() * C::ROWS + tid / C::TPR;
-  if (row >= p.rows) return;                       // a whole wave, where a wave has a row; else never
+  const long first = (long)HW::block_x() * C::ROWS + HW::wave_id() * 64 / C::TPR;
+  if (first >= p.rows) return;                     // a whole wave, where a wave has rows; else never
+  // where a wave has four rows, lanes past the last row have the last one once more, and store nothing
+  const long mine = first + HW::lane_id() / C::TPR, row = C::TPR < 64 && mine >= p.rows ? p.rows - 1 : mine;
+  const int cols = row == mine ? p.cols : 0;       // to be stored
   // ahead of the sums that they do not depend on, where there are registers for them
   constexpr bool AHEAD = C::TPR < 1024 && NV < 4;
   const float n = (float)p.cols;
@@ -91,7 +94,7 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_rows(const LayerNormArg
 #pragma unroll
       for (int e = 0; e < 8; e++) h[i][e] += value<C, HW>(r, i, e);
   }
-  if (p.total != nullptr) store_values<C, DT, HW>((void*)row_at<DT>(p.total, row, p.ldt), me, p.cols, h);
+  if (p.total != nullptr) store_values<C, DT, HW>((void*)row_at<DT>(p.total, row, p.ldt), me, cols, h);
 #pragma unroll
   for (int i = 0; i < NV; i++)
 #pragma unroll
@@ -117,7 +120,7 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_rows(const LayerNormArg
   row_sums<C::TPR, HW>(sd, sdd, lds + 128);
   const float off = sd / n, var = sdd / n - off * off;
   const float rstd = 1.0f / HW::sqrt((var < 0.f ? 0.f : var) + p.eps);       // NaN stays
-  if (me == 0) {
+  if (me == 0 && cols) {
     if (p.mean != nullptr) HW::global_store_u32(p.mean + row, __builtin_bit_cast(uint32_t, m + off));
     if (p.rstd != nullptr) HW::global_store_u32(p.rstd + row, __builtin_bit_cast(uint32_t, rstd));
   }
@@ -127,11 +130,12 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_rows(const LayerNormArg
   for (int i = 0; i < NV; i++)
 #pragma unroll
     for (int e = 0; e < 8; e++) h[i][e] = HW::fma((h[i][e] - off) * rstd, g[i][e], b[i][e]);
-  store_result<C, HW>(h, p.y, p.ldy, p.out, p.scale, row, me, p.cols, lds + 256);
+  store_result<C, HW>(h, p.y, p.ldy, p.out, p.scale, row, me, cols, lds + 256);
 }
 
 // A group of TPR threads takes rows g, g + groups, ... and keeps the sums of dgain and dshift for its columns in registers; the
-// waves of a block add theirs where each has a row, alcop_column_sums adds the blocks'.
+// groups of a block add theirs, alcop_column_sums adds the blocks'.  Where a wave has four rows, its lanes walk as long as the first of them, and
+// past the last row do the last row once more without adding or storing it.
 template <class C, class HW>
 __global__ void __launch_bounds__(C::NT) alcop_layernorm_grad(const LayerNormGradArgs p, int groups)
 {
@@ -141,7 +145,13 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_grad(const LayerNormGra
   const uint32_t lds = HW::lds_base();
   const int tid = HW::wave_id() * 64 + HW::lane_id();
   const int me = tid % C::TPR;
-  const int group = (int)HW::block_x() * C::ROWS + tid / C::TPR;
+  const int group = (int)HW::block_x() * C::ROWS + HW::wave_id() * 64 / C::TPR, part = HW::lane_id() / C::TPR;
+  auto clamped = [&](long row) __attribute__((always_inline)) {
+    if constexpr (C::TPR >= 64)
+      return row;
+    else
+      return row + part < p.rows ? row + part : (long)p.rows - 1;
+  };
   float dg[NV][8], ds[NV][8];
 #pragma unroll
   for (int i = 0; i < NV; i++)
@@ -163,13 +173,15 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_grad(const LayerNormGra
     mean2 = __builtin_bit_cast(float, HW::global_load_u32(p.mean + row));
     rstd2 = __builtin_bit_cast(float, HW::global_load_u32(p.rstd + row));
   };
-  if (NEXT && group < p.rows) load_next(group);
-  for (long row = group; row < p.rows; row += groups, turn ^= 1) {
+  if (NEXT && group < p.rows) load_next(clamped(group));
+  for (long first = group; first < p.rows; first += groups, turn ^= 1) {
+    const long row = clamped(first);
+    const int cols = C::TPR >= 64 || first + part < p.rows ? p.cols : 0;
     Raw<C> dy, h, dt = {};
     float mean, rstd;
     if constexpr (NEXT) {
       dy = dy2, h = h2, dt = dt2, mean = mean2, rstd = rstd2;
-      if (row + groups < p.rows) load_next(row + groups);
+      if (first + groups < p.rows) load_next(clamped(first + groups));
     } else {
       dy = load_raw<C, HW>(row_at<DT>(p.dy, row, p.lddy), me, p.cols);
       h = load_raw<C, HW>(row_at<DT>(p.total, row, p.ldt), me, p.cols);
@@ -185,8 +197,8 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_grad(const LayerNormGra
 #pragma unroll
       for (int e = 0; e < 8; e++) {
         // past the end dy is 0 (the mean may be infinite, which 0 times is not 0)
-        const bool there = C::WHOLE ? chunk_at<C>(me, i) < p.cols : chunk_at<C>(me, i) + e < p.cols;
-        const float d = value<C, HW>(dy, i, e), xh = there ? (value<C, HW>(h, i, e) - mean) * rstd : 0.f;
+        const bool there = C::WHOLE ? chunk_at<C>(me, i) < cols : chunk_at<C>(me, i) + e < cols;
+        const float d = C::TPR >= 64 || there ? value<C, HW>(dy, i, e) : 0.f, xh = there ? (value<C, HW>(h, i, e) - mean) * rstd : 0.f;
         st += d * g[i][e];
         stx += d * g[i][e] * xh;
         dg[i][e] += d * xh;
@@ -216,12 +228,23 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_grad(const LayerNormGra
 #pragma unroll
         for (int e = 0; e < 8; e++) dx[i][e] += value<C, HW>(dt, i, e);
     }
-    store_values<C, DT, HW>((void*)row_at<DT>(p.dx, row, p.lddx), me, p.cols, dx);
+    store_values<C, DT, HW>((void*)row_at<DT>(p.dx, row, p.lddx), me, cols, dx);
   }
   // the sums of a block: of dgain, then in the same LDS of dshift
   auto leave = [&](float(&v)[NV][8], float* to, bool again) __attribute__((always_inline)) {
     if (to == nullptr) return;
+    if constexpr (C::TPR < 64) {
+      // the four parts of a wave, which from here on add and store the same
+#pragma unroll
+      for (int i = 0; i < NV; i++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          v[i][e] += __builtin_bit_cast(float, HW::xor_lanes(__builtin_bit_cast(uint32_t, v[i][e]), 16));
+          v[i][e] += __builtin_bit_cast(float, HW::xor_lanes(__builtin_bit_cast(uint32_t, v[i][e]), 32));
+        }
+    }
     if constexpr (C::ROWS > 1) {
+      constexpr uint32_t ROW = C::TPR * 4;
       const uint32_t at = lds + LAYERNORM_LDS_BYTES + (uint32_t)me * 4;
       const int wave = HW::wave_id();
       if (again) HW::block_barrier();
@@ -229,17 +252,17 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_grad(const LayerNormGra
       for (int i = 0; i < NV; i++)
 #pragma unroll
         for (int e = 0; e < 8; e++)
-          HW::lds_write1(at + (uint32_t)((wave * NV + i) * 8 + e) * 256, __builtin_bit_cast(uint32_t, v[i][e]));
+          HW::lds_write1(at + (uint32_t)((wave * NV + i) * 8 + e) * ROW, __builtin_bit_cast(uint32_t, v[i][e]));
       HW::wait_lds();
       HW::block_barrier();
       if (wave == 0) {
 #pragma unroll
-        for (int w = 1; w < C::ROWS; w++)
+        for (int w = 1; w < C::NT / 64; w++)
 #pragma unroll
           for (int i = 0; i < NV; i++)
 #pragma unroll
             for (int e = 0; e < 8; e++)
-              v[i][e] += __builtin_bit_cast(float, HW::lds_read4(at + (uint32_t)((w * NV + i) * 8 + e) * 256));
+              v[i][e] += __builtin_bit_cast(float, HW::lds_read4(at + (uint32_t)((w * NV + i) * 8 + e) * ROW));
       }
       HW::wait_lds();
       if (wave > 0) return;
@@ -275,7 +298,7 @@ int layernorm_lds(const LayerNormArgs& a)
 template <class C>
 constexpr int layernorm_grad_lds()
 {
-  return LAYERNORM_LDS_BYTES + (C::ROWS > 1 ? C::ROWS * C::NV * 8 * 64 * 4 : 0);
+  return LAYERNORM_LDS_BYTES + (C::ROWS > 1 ? C::NT / 64 * C::NV * 8 * C::TPR * 4 : 0);
 }
 
 }  // namespace alcop

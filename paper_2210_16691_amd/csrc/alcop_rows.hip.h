@@ -9,7 +9,7 @@
 // found, and stored once, past the caches (kept in the memory-side cache, a norm and the layer that reads it take 3 to 11 % less with
 // 256 rows, 0 to 7 with 1024, but 3 to 4 % more with one to sixteen rows of 768 and up to 3 with 256 of 4096).  Sums are fp32 in a fixed order; nothing is atomic, so results do not change between runs.
 //
-// A row belongs to TPR threads (a wave, or a whole block), each holding NV chunks of eight elements, moved sixteen bytes a load at
+// A row belongs to TPR threads (a wave, a whole block, or sixteen lanes of a wave), each holding NV chunks of eight elements, moved sixteen bytes a load at
 // whatever address they lie (a global access may start at any element).  Where the length is no multiple of eight (!WHOLE)
 // the last chunk is loaded as the row's last eight elements and stored element by element.
 //
@@ -66,11 +66,11 @@ __device__ __forceinline__ float wave_sum(float v)
   return v;
 }
 // of magnitudes, as bit patterns: those of NaN are above all others, so that one NaN makes the result NaN
-template <class HW>
+template <int LANES, class HW>
 __device__ __forceinline__ uint32_t wave_max(uint32_t v)
 {
 #pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) {
+  for (int m = LANES / 2; m >= 1; m >>= 1) {
     const uint32_t o = HW::xor_lanes(v, m);
     v = o > v ? o : v;
   }
@@ -95,6 +95,11 @@ __device__ __forceinline__ float row_sum(float v, uint32_t at)
 template <int TPR, class HW>
 __device__ __forceinline__ void row_sums(float& a, float& b, uint32_t at)
 {
+  if constexpr (TPR == 16) {
+    a = HW::sum_sixteen(a);
+    b = HW::sum_sixteen(b);
+    return;
+  }
   a = HW::sum_lanes(a);
   b = HW::sum_lanes(b);
   if constexpr (TPR > 64) {
@@ -114,7 +119,7 @@ __device__ __forceinline__ void row_sums(float& a, float& b, uint32_t at)
 template <int TPR, class HW>
 __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t at)
 {
-  v = wave_max<HW>(v);
+  v = wave_max<(TPR < 64 ? TPR : 64), HW>(v);
   if constexpr (TPR > 64) {
     HW::lds_write1(at + 4 * HW::wave_id(), v);
     HW::wait_lds();
@@ -169,7 +174,7 @@ struct Raw {
 // Where a row of cols elements, 8 or more, is not made of chunks, its last chunk is loaded as the eight elements that the row ends with,
 // and chunks past it alike, so that no load waits for a branch; finish() shifts out what is not theirs, once the loads of all
 // matrices are on their way.  end_of_row: the last 8 - k elements in front, zeros behind (1 <= k <= 8).  Element by element it took longer:
-// gradients of the layer norm of 1531 x 1111 fp16 16.5 us, ENDS_AFTER so, norm of 8000 x 1111 bf16 42 and TAIL_AFTER.
+// gradients of the layer norm of 1531 x 1111 fp16 16.5 us, 12.8 so, norm of 8000 x 1111 bf16 42 and 27.8.
 template <int DT>
 __device__ __forceinline__ RawRow<8, DT> end_of_row(RawRow<8, DT> r, int k)
 {
@@ -352,7 +357,7 @@ __device__ __forceinline__ void divide_row(float (&v)[NV][8], float scale)
 }
 
 // ---- norm, 8 bits ------------------------------------------------------------------------------------------------
-// A row h of the result, in type `out` (3: e4m3, whose scale goes to scale[row]); `at`: LDS of the row's maximum.
+// A row h of the result, in type `out` (3: e4m3, whose scale goes to scale[row]); `at`: LDS of the row's maximum; no cols: nothing is stored.
 template <class C, class HW>
 __device__ __forceinline__ void store_result(float (&h)[C::NV][8], void* base, long ld, int out, float* scale_of, long row, int me,
                                              int cols, uint32_t at)
@@ -371,7 +376,7 @@ __device__ __forceinline__ void store_result(float (&h)[C::NV][8], void* base, l
     top = row_max<C::TPR, HW>(top, at);
     const float peak = __builtin_bit_cast(float, top) / 448.0f;
     const float scale = peak < 1.17549435e-38f ? 1.17549435e-38f : peak;     // NaN stays
-    if (me == 0) HW::global_store_u32(scale_of + row, __builtin_bit_cast(uint32_t, scale));
+    if (me == 0 && cols > 0) HW::global_store_u32(scale_of + row, __builtin_bit_cast(uint32_t, scale));
     divide_row<HW>(h, scale);
   }
   char* y = (char*)base + row * ld * (out == 3 ? 1 : out == 2 ? 4 : 2);

@@ -33,12 +33,12 @@ struct Load {
 
 hipError_t launch_layernorm_rows(const LayerNormArgs& a, int dt, bool whole, hipStream_t st)
 {
-  return dispatch_rows_of<Norm>(dt, whole, a.rows, a.cols, a, st);
+  return dispatch_layernorm<Norm>(dt, whole, a.rows, a.cols, a, st);
 }
 
 hipError_t launch_layernorm_grad(const LayerNormGradArgs& a, int groups, int dt, bool whole, hipStream_t st)
 {
-  return dispatch_rows_of<Grad>(dt, whole, a.rows, a.cols, a, groups, st);
+  return dispatch_layernorm<Grad>(dt, whole, a.rows, a.cols, a, groups, st);
 }
 
 hipError_t launch_two_column_sums(const TwoColumnSums& a, int arrays, hipStream_t st)
@@ -52,7 +52,7 @@ hipError_t prepare_layernorm()
 {
   hipFuncAttributes at;
   const hipError_t rc = hipFuncGetAttributes(&at, (const void*)alcop_two_column_sums<Gfx950>);
-  return rc != hipSuccess ? rc : each_rows_kernel<Load>();
+  return rc != hipSuccess ? rc : each_layernorm_kernel<Load>();
 }
 
 }  // namespace alcop

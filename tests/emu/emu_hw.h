@@ -741,6 +741,14 @@ struct Emu {
     }
     return v;
   }
+  static float sum_sixteen(float v)
+  {
+    for (int m = 1; m < 16; m *= 2) {
+      const uint32_t o = xor_lanes(__builtin_bit_cast(uint32_t, v), m);
+      v += __builtin_bit_cast(float, o);
+    }
+    return v;
+  }
   static uint32_t scan_lanes(uint32_t v)
   {
     uint32_t all = v, before = 0;

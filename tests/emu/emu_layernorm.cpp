@@ -34,11 +34,11 @@ struct Grad {
 }  // namespace
 hipError_t launch_layernorm_rows(const LayerNormArgs& a, int dt, bool whole, hipStream_t st)
 {
-  return dispatch_rows_of<Norm>(dt, whole, a.rows, a.cols, a, st);
+  return dispatch_layernorm<Norm>(dt, whole, a.rows, a.cols, a, st);
 }
 hipError_t launch_layernorm_grad(const LayerNormGradArgs& a, int groups, int dt, bool whole, hipStream_t st)
 {
-  return dispatch_rows_of<Grad>(dt, whole, a.rows, a.cols, a, groups, st);
+  return dispatch_layernorm<Grad>(dt, whole, a.rows, a.cols, a, groups, st);
 }
 static void sums_entry(const void* p) { alcop_two_column_sums<emu::Emu>(*(const TwoColumnSums*)p); }
 hipError_t launch_two_column_sums(const TwoColumnSums& a, int arrays, hipStream_t)

@@ -54,6 +54,19 @@ def test_norms_of_many_rows():
     run_norm(20000, 72, "bf16", "e4m3")
 
 
+@pytest.mark.parametrize("cols", [64, 100, 128, 129, 250, 256])
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("f16", "e4m3"), ("f32", "f32")])
+def test_short_rows(cols, dtype, out):
+    for rows in (1, 4, 5, 15, 17, 3001):
+        run_norm(rows, cols, dtype, out, pad=3 * (rows % 2), offset=rows % 2)
+        x, g, r, b = matrix(rows, cols, dtype, 1), vector(cols, 2), matrix(rows, cols, dtype, 3), vector(cols, 4)
+        y, h = torch.empty_like(x), torch.empty_like(x)
+        al.alcop_layernorm(x, g, b, y, residual=r, total=h)
+        al.alcop_layernorm(x, g, b, r, residual=r, total=x)
+        torch.cuda.synchronize()
+        assert torch.equal(x, h) and torch.equal(r, y)
+
+
 def test_rows_far_from_zero():
     for cols in (1000, 4096, 16384):
         run_norm(9, cols, "f32", "f32", residual=False, far=3000.0)
@@ -84,6 +97,15 @@ def run_grad(rows, cols, dtype, dtotal=True, gain=True, dgain=True, dshift=True,
 def test_gradients(cols, dtype):
     run_grad(37, cols, dtype, pad=3, offset=1)
     run_grad(1, cols, dtype, dtotal=False, gain=False)
+
+
+@pytest.mark.parametrize("cols", [64, 100, 128, 129, 250, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_gradients_of_short_rows(cols, dtype):
+    for rows in (1, 4, 5, 35, 3001, 9001):
+        run_grad(rows, cols, dtype, pad=3 * (rows % 2), offset=rows % 2)
+        run_grad(rows, cols, dtype, in_place=True)
+        run_grad(rows, cols, dtype, dtotal=False, dgain=False)
 
 
 def test_gradients_of_many_rows():

@@ -41,6 +41,20 @@ def test_norms(rows, cols, dtype, out):
     run_norm(rows, cols, dtype, out, pad=3, offset=1)
 
 
+@pytest.mark.parametrize("rows,cols", [(1, 64), (4, 100), (5, 128), (15, 129), (17, 256), (35, 250)])
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("f16", "e4m3"), ("f32", "f32")])
+def test_short_rows(rows, cols, dtype, out):
+    run_norm(rows, cols, dtype, out)
+    run_norm(rows, cols, dtype, out, pad=3, offset=1)
+    x, g = matrix(rows, cols, dtype, 1), vector(cols, 2)
+    r, b = matrix(rows, cols, dtype, 3), vector(cols, 4)
+    y = torch.empty(rows, cols, dtype=DT[dtype])
+    h = torch.empty_like(y)
+    assert not emu.call(al.alcop_layernorm, x, g, b, y, residual=r, total=h, reads=[x, g, b, r], writes=[y, h])
+    assert not emu.call(al.alcop_layernorm, x, g, b, r, residual=r, total=x, reads=[x, g, b, r], writes=[x, r])
+    assert torch.equal(x, h) and torch.equal(r, y)
+
+
 def test_norms_of_long_rows():
     run_norm(2, 9000, "bf16", "bf16")
     run_norm(1, 20001, "f16", "e4m3", pad=5)
@@ -103,6 +117,14 @@ def run_grad(rows, cols, dtype, dtotal=True, gain=True, dgain=True, dshift=True,
 @pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
 def test_gradients(rows, cols, dtype):
     run_grad(rows, cols, dtype, pad=3, offset=1)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 64), (4, 100), (50, 128), (15, 129), (35, 256), (33, 250)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_gradients_of_short_rows(rows, cols, dtype):
+    run_grad(rows, cols, dtype)
+    run_grad(rows, cols, dtype, pad=3, offset=1, in_place=True)
+    run_grad(rows, cols, dtype, dgain=False, dtotal=False)
 
 
 def test_gradients_of_long_rows_and_many():
