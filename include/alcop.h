@@ -536,7 +536,8 @@ int alcop_layernorm_backward(const void* dy, const void* total, const void* gain
  *     are out of range are taken as the nearest in range: which rows are then computed is not defined, no access is out of bounds.)
  *   tail: bias and scale_w are groups x N fp32 values without gaps; residual is NULL.  ALCOP_E4M3 operands, ALCOP_FP32_SUMS, act,
  *     types, alignment and pitches as for alcop_linear, but that bias and scale_w may start at any 4 bytes; strideW a multiple of 8
- *     (ALCOP_E4M3: 16) elements, 0 if all groups have the same.  ALCOP_LINEAR_KERNEL names a kernel here too.
+ *     (ALCOP_E4M3: 16) elements, 0 if all groups have the same.  ALCOP_LINEAR_KERNEL names a kernel here and in the
+ *     gradients' dA too, ALCOP_GRADIENT_KERNEL one of dW's (tuning and test knobs).
  * One launch.  1 <= groups < 2^24.  The same call gives the same bits.
  */
 int alcop_grouped_linear(const void* A, const void* W, const void* offsets, void* C, int rows, int groups, int N, int K,
@@ -591,7 +592,8 @@ int alcop_linear_cross_entropy(const void* X, const void* W, const void* labels,
  *     as above: G of a piece of the vocabulary (up to 128 MiB, or rows x 512 bytes if that is more) and sums of dX in fp32,
  *     one for each of up to 16 slices of a piece where dX is small.
  * For dW, all rows of X and of a piece of G, 128 more counted, span less than 2 GiB each; else ALCOP_ERR_SIZE, before anything is
- * launched.  Up to three launches a piece and two more; sums have a fixed order, without atomics.
+ * launched.  ALCOP_LINEAR_KERNEL names a kernel of each step, ALCOP_LOSS_PIECE the columns of a piece, the same for the size of the
+ * workspace and the call (tuning and test knobs).  Up to three launches a piece and two more; sums have a fixed order, without atomics.
  */
 size_t alcop_linear_cross_entropy_backward_workspace_bytes(int rows, int vocab, int K);
 int alcop_linear_cross_entropy_backward(const void* X, const void* W, const void* labels, const void* lse, const void* dloss,

@@ -1,5 +1,5 @@
 """MI355X-native load-compute-pipelined GEMM / BMM / implicit-GEMM conv2d (ALCOP, arXiv 2210.16691), and the linear
-layers, norms and 8-bit rows of a transformer's block around them.
+layers, norms, 8-bit rows, experts' products and loss of a transformer around them.
 
 Thin binding over ``libalcop.so`` (C ABI declared in ``include/alcop.h``).  Argument marshalling
 only (the hot entry points' in C++, the rest with ctypes): every step of the hot path runs in the
