@@ -36,7 +36,7 @@ int alcop_layernorm(const void* x, const void* residual, const void* gain, const
   if (rows <= 0 || cols <= 0) return ALCOP_ERR_SHAPE;
   if (ldx < cols || ldy < cols || (residual && ldr < cols) || (total && ldt < cols)) return ALCOP_ERR_SHAPE;
   if (cols > ROWS_MAX_COLS) return ALCOP_ERR_SIZE;
-  if (rows / layernorm_rows_per_block(rows, cols) >= (1 << 22) - 1) return ALCOP_ERR_SIZE;    // threads of a launch: 32 bits, 1024 a block
+  if (rows / rows_per_block(rows, cols) >= (1 << 22) - 1) return ALCOP_ERR_SIZE;    // threads of a launch: 32 bits, 1024 a block; as alcop_rmsnorm
   const int isz = size_of(in), osz = size_of(out);
   if (!aligned(x, isz) || !aligned(residual, isz) || !aligned(total, isz) || !aligned(y, osz)) return ALCOP_ERR_ALIGN;
   for (const void* p : {gain, shift, (const void*)scale, (const void*)mean, (const void*)rstd})
