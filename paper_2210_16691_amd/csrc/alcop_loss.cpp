@@ -33,7 +33,14 @@ const LossTable& loss_table()
 // of 64x64, 128x64, 128x128, 256x128 and 256x256 tiles, and (in brackets) what the costs alone would have picked of them, bf16:
 //   128 x 65536 x 2048  92.7 [79.1] 73.2 78.2 75.8     256 rows  143 121 97.1 [84.8] 79.5     100 x 50257 x 1600  59.1 [55.7] 45.1 54.8 51.4
 //   200 x 128256 x 1024 135 118 [96.7] 93.4 80.7       64 rows   [69.1] 73.8 72.8 76.3 79.6   400 x 10007 x 128  11.6 12.4 [11.5] 13.4 13.8
-double strips_side(const alcop_sched& s) { return s.bm == 256 ? (s.bn == 256 ? 0.70 : 0.75) : s.bm == 128 && s.bn == 128 ? 0.86 : 1.0; }
+// dX in slices of a long vocabulary in 256x256 tiles, us of the whole backward pass and [what the costs alone would have picked]:
+//   700 x 50257 x 768  303 [311] 309 307 280     2000 x 100000 x 512  976 940 927 [911] 844     300 x 30000 x 1024  118 [125] 125 129 145
+double side(LossStep step, const alcop_sched& s)
+{
+  if (step == LOSS_DX) return s.bn == 256 ? 0.85 : 1.0;
+  if (step != LOSS_STRIPS) return 1.0;
+  return s.bm == 256 ? (s.bn == 256 ? 0.70 : 0.75) : s.bm == 128 && s.bn == 128 ? 0.86 : 1.0;
+}
 
 // The kernel of a step of the lowest cost, as alcop_linear has it; slices: as many such products in one launch.
 const LossKernel* pick(LossStep step, int dt, int M, int N, int K, double bytes, int slices = 1)
@@ -50,7 +57,7 @@ const LossKernel* pick(LossStep step, int dt, int M, int N, int K, double bytes,
     }
     if (!k.cost) continue;
     const double tiles = (double)(((long)M + k.s.bm - 1) / k.s.bm) * (((long)N + k.s.bn - 1) / k.s.bn) * slices;
-    const double us = linear_us(*k.cost, tiles, (double)M * N * slices, K, bytes) * (step == LOSS_STRIPS ? strips_side(k.s) : 1.0);
+    const double us = linear_us(*k.cost, tiles, (double)M * N * slices, K, bytes) * side(step, k.s);
     if (!best || us < best_us) {
       best = &k;
       best_us = us;
