@@ -257,7 +257,8 @@ int alcop_grouped_linear_backward(const void* dC, const void* A, const void* W, 
   if (act && !pre) return ALCOP_ERR_NULL;
   if ((act || dbias) && !workspace) return ALCOP_ERR_NULL;
   if (rows <= 0 || groups <= 0 || N <= 0 || K <= 0 || N % 8 || K % 8) return ALCOP_ERR_SHAPE;
-  if (std::max(rows, std::max(N, K)) > 0x7ffff000 || groups > 64000) return ALCOP_ERR_SIZE;   // with the runs of alcop_grouped_act_grad fewer than 65536
+  if (std::max(rows, std::max(N, K)) > 0x7ffff000 || groups > 64000) return ALCOP_ERR_SIZE;
+  // (64000 groups and the full runs of alcop_grouped_act_grad are fewer than 65536 blocks)
   const int w_rows = transB ? N : K, w_cols = transB ? K : N;
   if (lddc < N || (dW && lda < K) || (dA && (ldw < w_cols || strideW < 0)) || (act && ldp < N) || (dA && ldda < K)) return ALCOP_ERR_SHAPE;
   if (dW && (lddw < w_cols || (groups > 1 && stridedW < (long)(w_rows - 1) * lddw + w_cols))) return ALCOP_ERR_SHAPE;

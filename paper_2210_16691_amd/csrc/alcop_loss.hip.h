@@ -13,7 +13,8 @@
 // which none reads or writes rows x vocabulary numbers beyond one piece.
 //
 // G in fp16: its numbers are as small as dloss / vocabulary, which fp16 does not reach.  They are multiplied by a power of two S
-// that takes the largest |dloss| of the rows that count to 2^14 .. 2^15 (G is at most that), and the products by 1 / S.  bf16 has fp32's range, S = 1.
+// that takes the largest |dloss| of the rows that count to 2^14 .. 2^15 (G is at most that), and the products by 1 / S.  bf16 has
+// fp32's range, S = 1.
 //
 // What bounds them: the matrix cores.  8192 rows, 65536 x 2048 bf16: 1.83 ms = 1.20 PFLOP/s (the cores 67 % busy at the 1.7 GHz that
 // power leaves), 6 us for the strips.  Gradients of 4096 rows: four pieces of 248 us for the logits and G (1.11 PFLOP/s), 220 for dX and 207
