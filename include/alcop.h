@@ -590,10 +590,11 @@ int alcop_linear_cross_entropy(const void* X, const void* W, const void* labels,
  *   dX (rows x K), dW (vocab x K): type `out`, which is `in` or ALCOP_F32; one may be NULL.  16-byte aligned, pitches multiples of 8.
  *   workspace: DEVICE, 16-byte aligned, at least alcop_linear_cross_entropy_backward_workspace_bytes(rows, vocab, K) bytes,
  *     as above: G of a piece of the vocabulary (up to 128 MiB, or rows x 512 bytes if that is more) and sums of dX in fp32,
- *     one for each of up to 16 slices of a piece where dX is small.
- * For dW, all rows of X and of a piece of G, 128 more counted, span less than 2 GiB each; else ALCOP_ERR_SIZE, before anything is
- * launched.  ALCOP_LINEAR_KERNEL names a kernel of each step, ALCOP_LOSS_PIECE the columns of a piece, the same for the size of the
- * workspace and the call (tuning and test knobs).  Up to three launches a piece and two more; sums have a fixed order, without atomics.
+ *     one for each of up to 17 slices of a piece where dX is small.
+ * For dW, all rows of X and of a piece of G, 128 more counted, span less than 2 GiB each; for dX, the vectors of a slice, 128 more
+ * counted, which with ldw <= 2 K (and K up to 10^6) they always do.  Else ALCOP_ERR_SIZE, before anything is launched.
+ * ALCOP_LINEAR_KERNEL names a kernel of each step, ALCOP_LOSS_PIECE the columns of a piece, the same for the size of the workspace
+ * and the call (tuning and test knobs).  Up to three launches a piece and two more; sums have a fixed order, without atomics.
  */
 size_t alcop_linear_cross_entropy_backward_workspace_bytes(int rows, int vocab, int K);
 int alcop_linear_cross_entropy_backward(const void* X, const void* W, const void* labels, const void* lse, const void* dloss,

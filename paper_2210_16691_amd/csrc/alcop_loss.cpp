@@ -94,23 +94,28 @@ Pieces pieces_of(int rows, int vocab, int K)
   // G of a piece: 128 MiB, which with what the products read stays in the memory-side cache (4096 rows, 65536 x 2048 bf16, pieces of
   // 64 to 512 MiB: 2878, 2762, 2896 and 2970 us, of 32 MiB 3200), or 256 columns of so many rows that it is more
   const char* env = std::getenv("ALCOP_LOSS_PIECE");          // a test knob: columns of a piece, a multiple of 256
-  const long most = env && std::atoi(env) > 0 ? (std::atoi(env) + 255) / 256 * 256 : std::max(256L, (1L << 26) / rows / 256 * 256);
-  Pieces p;
-  p.width = (int)std::min((long)vocab, most);
-  p.count = (int)(((long)vocab + p.width - 1) / p.width);
-  if (p.count > 1) {
-    // equal pieces
-    const long even = ((long)vocab + p.count - 1) / p.count;
-    p.width = (int)((even + 255) / 256 * 256);
-    p.count = (int)(((long)vocab + p.width - 1) / p.width);
-  }
-  p.pitch = (p.width + 7) & ~7;
-  // dX: slices of the piece while its largest tiles leave compute units idle, each 2048 columns or more
+  long most = env && std::atoi(env) > 0 ? (std::atoi(env) + 255) / 256 * 256 : std::max(256L, (1L << 26) / rows / 256 * 256);
+  // dX walks the vectors of a slice by 32-bit offsets, up to 128 past the last: 1 GiB of them at most, so that pitches of up to 2 K reach
+  const long reach = std::max(256L, ((1L << 29) / K - 128) / 256 * 256);
   const double tiles = (double)((rows + 255L) / 256) * ((K + 255L) / 256);
-  p.slices = 1;
-  while (p.slices < 16 && tiles * p.slices * 2 <= 256 && p.pitch / (p.slices * 2) >= 2048) p.slices *= 2;
-  p.slice = p.slices > 1 ? (p.pitch / p.slices + 255) / 256 * 256 : p.pitch;
-  p.slices = (p.pitch + p.slice - 1) / p.slice;
+  Pieces p;
+  for (;; most = std::min(most - 256, reach * p.slices)) {
+    p.width = (int)std::min((long)vocab, most);
+    p.count = (int)(((long)vocab + p.width - 1) / p.width);
+    if (p.count > 1) {
+      // equal pieces
+      const long even = ((long)vocab + p.count - 1) / p.count;
+      p.width = (int)((even + 255) / 256 * 256);
+      p.count = (int)(((long)vocab + p.width - 1) / p.width);
+    }
+    p.pitch = (p.width + 7) & ~7;
+    // dX: slices of the piece while its largest tiles leave compute units idle, each 2048 columns or more
+    p.slices = 1;
+    while (p.slices < 16 && tiles * p.slices * 2 <= 256 && p.pitch / (p.slices * 2) >= 2048) p.slices *= 2;
+    p.slice = p.slices > 1 ? (p.pitch / p.slices + 255) / 256 * 256 : p.pitch;
+    p.slices = (p.pitch + p.slice - 1) / p.slice;
+    if (p.slice <= reach) break;          // at 256 columns at the latest
+  }
   p.sums = p.count > 1 || p.slices > 1;
   p.dx = r256(2.0 * rows * p.pitch);
   p.scale = p.dx + (p.sums ? r256(4.0 * rows * K * p.slices) : 0);
@@ -259,7 +264,7 @@ int alcop_linear_cross_entropy_backward(const void* X, const void* W, const void
       rc = grid_of(kx[i], rows, K, pc.pitch, 8, &gx[i]);
       if (rc) return rc;
       gx[i].y = (unsigned)slices;
-      if (2.0 * (n8 + 128.0) * ldw >= 2147483648.0 || 4.0 * 256 * lddx >= 2147483648.0) return ALCOP_ERR_SIZE;
+      if (2.0 * (std::min(n8, pc.slice) + 128.0) * ldw >= 2147483648.0 || 4.0 * 256 * lddx >= 2147483648.0) return ALCOP_ERR_SIZE;
     }
     if (dW) {
       kw[i] = pick(LOSS_DW, dt, n8, K, rows, g_bytes + 2.0 * rows * (double)K + (double)osz * n * K);

@@ -16,7 +16,7 @@ void entry(const void* p)
 template <class C, auto KERNEL, class A>
 hipError_t launch_kernel(const A& a, dim3 grid, hipStream_t)
 {
-  emu::run_grid(&entry<KERNEL, A>, &a, C::NT, C::LDS_BYTES, grid.x, 1, 1);
+  emu::run_grid(&entry<KERNEL, A>, &a, C::NT, C::LDS_BYTES, grid.x, grid.y, 1);
   return hipSuccess;
 }
 [[maybe_unused]] hipError_t prepare_none() { return hipSuccess; }
