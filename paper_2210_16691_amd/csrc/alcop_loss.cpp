@@ -211,6 +211,7 @@ int alcop_linear_cross_entropy(const void* X, const void* W, const void* labels,
   r.rows = rows;
   r.count = (int)(((long)vocab + k->s.bn - 1) / k->s.bn);
   r.vocab = vocab;
+  r.alpha = alpha;
   return launch_loss_rows(r, st) == hipSuccess ? ALCOP_OK : ALCOP_ERR_LAUNCH;
 }
 
