@@ -29,13 +29,19 @@ namespace alcop {
 constexpr float LOG2_E = 1.44269504089f, LN_2 = 0.69314718056f;
 
 // (shift, sum) stands for sum 2^shift; (-infinity, 0) for nothing.  A strip's shift is finite; one whose logits are all -infinity
-// has the sum 0 and must not move the shift.
+// has the sum 0 and must not move the shift.  The factor is 2^-126 at least: beside the larger shift's sum of some 1 that is nothing,
+// and a sum that an infinite logit made infinite (its strip has the shift 0) stays so, where 0 would make it NaN.
+template <class HW>
+__device__ __forceinline__ float strip_factor(float d)
+{
+  return HW::exp2(d < -126.f ? -126.f : d);
+}
 template <class HW>
 __device__ __forceinline__ void add_strip(float& shift, float& sum, float shift2, float sum2)
 {
   if (sum2 == 0.f) return;
   const float top = shift2 > shift ? shift2 : shift;
-  sum = sum * HW::exp2(shift - top) + sum2 * HW::exp2(shift2 - top);
+  sum = sum * strip_factor<HW>(shift - top) + sum2 * strip_factor<HW>(shift2 - top);
   shift = top;
 }
 
