@@ -573,7 +573,7 @@ int alcop_grouped_linear_backward(const void* dC, const void* A, const void* W, 
  *   workspace: DEVICE, 16-byte aligned, at least alcop_linear_cross_entropy_workspace_bytes(rows, vocab, K) bytes (which
  *     returns 0 for arguments no call accepts): 8 bytes for each row and 64 columns at most.  Overwritten; calls that share it,
  *     captured ones too, must be ordered on one stream.
- * rows and vocab are free, K is a multiple of 8; X, W: 16-byte aligned, pitches multiples of 8 elements; labels 8-byte aligned.
+ * rows (below 2^27) and vocab are free, K is a multiple of 8; X, W: 16-byte aligned, pitches multiples of 8 elements; labels 8-byte aligned.
  * Outputs and workspace overlap nothing else.  Two launches; sums have a fixed order.
  */
 size_t alcop_linear_cross_entropy_workspace_bytes(int rows, int vocab, int K);
@@ -592,7 +592,8 @@ int alcop_linear_cross_entropy(const void* X, const void* W, const void* labels,
  *     as above: G of a piece of the vocabulary (up to 128 MiB, or rows x 512 bytes if that is more) and sums of dX in fp32,
  *     one for each of up to 17 slices of a piece where dX is small.
  * For dW, all rows of X and of a piece of G, 128 more counted, span less than 2 GiB each; for dX, the vectors of a slice, 128 more
- * counted, which with ldw <= 2 K (and K up to 10^6) they always do.  Else ALCOP_ERR_SIZE, before anything is launched.
+ * counted, which with ldw <= 2 K (and K up to 10^6) they always do, and rows K is below 2^35.  Else ALCOP_ERR_SIZE, before anything is
+ * launched.
  * ALCOP_LINEAR_KERNEL names a kernel of each step, ALCOP_LOSS_PIECE the columns of a piece, the same for the size of the workspace
  * and the call (tuning and test knobs).  Up to three launches a piece and two more; sums have a fixed order, without atomics.
  */

@@ -168,7 +168,7 @@ int alcop_linear_cross_entropy(const void* X, const void* W, const void* labels,
   if (rc) return rc;
   if (!aligned(loss, 4) || !aligned(lse, 4) || !aligned(workspace, 16)) return ALCOP_ERR_ALIGN;
   const size_t need = alcop_linear_cross_entropy_workspace_bytes(rows, vocab, K);
-  if (workspace_bytes < need) return ALCOP_ERR_SIZE;
+  if (workspace_bytes < need || (rows + 31L) / 32 * 1024 >= 1L << 32) return ALCOP_ERR_SIZE;      // threads of the second launch
   Span sw(workspace, 1, 1, 1, 1);
   sw.row = sw.pitch = (double)need;
   const Span outs[] = {Span(loss, 1, rows, rows, 4), Span(lse, 1, rows, rows, 4), sw};
@@ -249,6 +249,9 @@ int alcop_linear_cross_entropy_backward(const void* X, const void* W, const void
       if (meet(outs[i], outs[j])) return ALCOP_ERR_UNSUPPORTED;
   }
 
+  // dX is added up in fp32: where it is to be, or in the workspace
+  const bool direct = !pc.sums || (out == ALCOP_F32 && pc.slices == 1);
+  if (dX && !direct && (long)rows * (K / 8) > (1L << 32) - 256) return ALCOP_ERR_SIZE;             // threads of the last launch
   // every piece's products, the widest and the last, before anything is launched
   const int last = vocab - (pc.count - 1) * pc.width;
   const LossKernel *kg[2], *kx[2] = {nullptr, nullptr}, *kw[2] = {nullptr, nullptr};
@@ -285,8 +288,6 @@ int alcop_linear_cross_entropy_backward(const void* X, const void* W, const void
   }
   const float fixed = scaled && !dloss ? 16384.0f : 1.0f;        // S where |dloss| is 1
   const float* inverse = scaled && dloss ? scale + 1 : nullptr;
-  // dX is added up in fp32: where it is to be, or in the workspace
-  const bool direct = !pc.sums || (out == ALCOP_F32 && pc.slices == 1);
   for (int i = 0; i < pc.count; i++) {
     const int end = i == pc.count - 1, v0 = i * pc.width, n = end ? last : pc.width, n8 = (n + 7) & ~7;
     LossArgs a;
