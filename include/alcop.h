@@ -566,7 +566,7 @@ int alcop_grouped_linear_backward(const void* dC, const void* A, const void* W, 
  * Cross entropy of rows against their product with a vocabulary's vectors, logits not kept:
  *     z[t][v] = alpha * sum_k X(t,k) W(v,k);   lse[t] = log sum_v exp(z[t][v]);   loss[t] = lse[t] - z[t][labels[t]]
  * in fp32 from the accumulators on; the loss, which is 0 or more, as the sum of exp(z - z[labels[t]]), not as a difference of rounded numbers.
- *   X: row-major rows x K, W: vocab x K (a layer's weights: out x in), both ALCOP_F16 or ALCOP_BF16; alpha > 0.
+ *   X: row-major rows x K, W: vocab x K (a layer's weights: out x in), both ALCOP_F16 or ALCOP_BF16; 0 < alpha <= 2e38.
  *   labels: DEVICE, 64-bit numbers.  A row whose label is no column of the vocabulary (below 0, or vocab and more) does not count:
  *     its loss is 0, and so is its gradient; its lse is that of its logits.
  *   loss, lse (may be NULL): rows fp32 values.  An infinite logit makes them infinite or NaN as the formulas do.

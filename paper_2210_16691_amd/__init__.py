@@ -785,7 +785,7 @@ def alcop_linear_cross_entropy(X, W, labels, loss, lse=None, workspace=None, alp
 
     X is [rows,K], W [vocab,K] (a layer's weights), both fp16 or bf16; labels int64; loss and lse fp32 vectors of rows values,
     lse may be None.  A row whose label is no column of the vocabulary does not count: its loss is 0.  workspace: at least
-    alcop_linear_cross_entropy_workspace_bytes(rows, vocab, K) bytes.  alpha > 0."""
+    alcop_linear_cross_entropy_workspace_bytes(rows, vocab, K) bytes.  0 < alpha <= 2e38."""
     if _marshal_lib is _lib is not None:
         rc = _marshal.cross_entropy(X, W, labels, loss, lse, workspace, alpha, stream)
         if rc is not None:

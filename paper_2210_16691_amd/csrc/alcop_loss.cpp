@@ -131,7 +131,7 @@ int check_operands(const void* X, const void* W, const void* labels, int rows, i
   if (rows <= 0 || vocab <= 0 || K <= 0 || K % 8) return ALCOP_ERR_SHAPE;
   if (ldx < K || ldw < K) return ALCOP_ERR_SHAPE;
   if (!aligned(X, 16) || !aligned(W, 16) || ldx % 8 || ldw % 8 || !aligned(labels, 8)) return ALCOP_ERR_ALIGN;
-  if (!(alpha > 0.f) || alpha > 3e38f) return ALCOP_ERR_UNSUPPORTED;
+  if (!(alpha > 0.f) || alpha > 2e38f) return ALCOP_ERR_UNSUPPORTED;       // alpha log2(e) is finite
   if (ldx >= (1L << 30) || ldw >= (1L << 30) || std::max(rows, std::max(vocab, K)) > 0x7ffff000) return ALCOP_ERR_SIZE;
   return ALCOP_OK;
 }
