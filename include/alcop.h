@@ -549,7 +549,7 @@ int alcop_grouped_linear(const void* A, const void* W, const void* offsets, void
  *     dA = alpha * dZ . W_g^T,   dW_g = alpha * A_g^T . dZ_g  (stored as W_g is),   dbias[g][j] = sum of dZ over the group's rows
  * before the rounding; dW_g and dbias[g] of a group without rows are 0, rows of no group are left as they are in dA.
  *   dA, dW, dbias may be NULL (not all).  Types, alignment and pitches as for alcop_linear_backward; dW_g at dW + g * stridedW,
- *     which do not overlap; dbias: groups x N fp32 values.  groups <= 64000.
+ *     which do not overlap; dbias: groups x N fp32 values, N below 2^29.  groups <= 64000.
  *   workspace: DEVICE, 16-byte aligned, at least alcop_grouped_linear_backward_workspace_bytes(rows, groups, N, K) bytes,
  *     needed if act != 0 or dbias is given; as for alcop_linear_backward.
  * For dW, all rows of A and of dZ (dC without an activation), 128 more counted, span less than 2 GiB each; else ALCOP_ERR_SIZE,

@@ -271,6 +271,7 @@ int alcop_grouped_linear_backward(const void* dC, const void* A, const void* W, 
     return ALCOP_ERR_SIZE;
   const GradPlan plan = plan_of(rows, groups, N);
   if ((act || dbias) && workspace_bytes < plan.all) return ALCOP_ERR_SIZE;
+  if (dbias && ((long)N + SUM_COLS - 1) / SUM_COLS * GROUP_SUM_THREADS >= 1L << 32) return ALCOP_ERR_SIZE;      // threads of a launch
 
   const int osz = size_of(out);
   const Span outs[] = {Span(dA, rows, K, ldda, osz), group_span(dW, groups, w_rows, w_cols, lddw, stridedW, osz),
