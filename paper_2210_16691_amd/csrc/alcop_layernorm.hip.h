@@ -10,8 +10,9 @@
 // The mean is found in two steps.  sum(h) / n is off by some 2^-24 of |h|'s mean, which where rows lie far from 0 is not small
 // beside their spread; so it only gives a point m near the mean, and the second turn sums d = h - m and d^2 together: mean = m + sum(d) / n,
 // var = mean(d^2) - mean(d)^2.  m is a multiple of 2^-12 of |h|'s mean (down to its power of two): h - m is then exact but for
-// fp32 rows, where a rounding that all of a row's numbers share would not average out of their sum, and mean(d) is so small that its square
-// costs no digits.  No sum of squares of h itself is formed, and a row needs two turns of the block, as many as the plain two-pass form.
+// fp32 rows, where a rounding that all of a row's numbers share would not average out of their sum.  mean(d) is up to 2^-13 of |h|'s mean:
+// its square costs no digits while that is below the spread, and where it is not (a spread of 1 about 10^4 and more) a third turn sums
+// about m + mean(d).  No sum of squares of h itself is formed, and any other row needs two turns of the block, as many as the plain two-pass form.
 // The gradient's two means share a turn.
 //
 // A block of the norm has one row (one of its waves up to 1024 columns, sixteen of its lanes up to 256): 16384 x 4096 bf16 94 us; blocks
@@ -106,7 +107,7 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_rows(const LayerNormArg
   row_sums<C::TPR, HW>(s, size, lds);
   // the nearest multiple of 2^-12 of a power of two: what is left when 3 / 2 of 2^23 of them are added and taken away
   const float many = __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, size / n) & 0x7f800000u) * 0x1.8p11f;
-  const float m = (s / n + many) - many;
+  float m = (s / n + many) - many;
   float sd = 0.f, sdd = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; i++)
@@ -119,7 +120,29 @@ __global__ void __launch_bounds__(C::NT) alcop_layernorm_rows(const LayerNormArg
       sdd += h[i][e] * h[i][e];
     }
   row_sums<C::TPR, HW>(sd, sdd, lds + 128);
-  const float off = sd / n, var = sdd / n - off * off;
+  float off = sd / n, var = sdd / n - off * off;
+  // a row that lies so far away that m is further from the mean than its spread: the square took the digits, and the row moves once more
+  const bool far = off * off > var;
+  if (HW::ballot(far)) {
+    const float by = far ? off : 0.f;              // the other rows of the wave stay as they are
+    m += by;
+    sd = sdd = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; i++)
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const bool there = C::WHOLE ? chunk_at<C>(me, i) < p.cols : chunk_at<C>(me, i) + e < p.cols;
+        h[i][e] -= by;
+        const float d = there ? h[i][e] : 0.f;
+        sd += d;
+        sdd += d * d;
+      }
+    row_sums<C::TPR, HW>(sd, sdd, lds);            // where the first two were
+    if (far) {
+      off = sd / n;
+      var = sdd / n - off * off;
+    }
+  }
   const float rstd = 1.0f / HW::sqrt((var < 0.f ? 0.f : var) + p.eps);       // NaN stays
   if (me == 0 && cols) {
     if (p.mean != nullptr) HW::global_store_u32(p.mean + row, __builtin_bit_cast(uint32_t, m + off));

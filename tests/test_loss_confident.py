@@ -57,7 +57,7 @@ def check_confident(call, dtype, behind, alpha, dev="cpu"):
 
 
 def emulated(fn, *args, **kw):
-    ts = [t for t in args if isinstance(t, torch.Tensor)]
+    ts = [t for t in list(args) + list(kw.values()) if isinstance(t, torch.Tensor)]
     errs = emu.call(fn, *args, reads=ts, writes=ts, **kw)
     assert not errs, errs[:3]
 
