@@ -497,7 +497,8 @@ int alcop_quantize_rows(const void* x, void* y, void* scale, int rows, int cols,
  * Layer norm of rows, with the residual's addition in front of it:
  *     h = x + residual;   mean[i] = mean_j h[i][j];   rstd[i] = 1 / sqrt(mean_j (h[i][j] - mean[i])^2 + eps);
  *     y[i][j] = (h[i][j] - mean[i]) * rstd[i] * gain[j] + shift[j]
- * in fp32, the mean and the variance of a row that lies far from 0 without cancellation; total receives h, mean and
+ * in fp32, the mean and the variance of a row that lies far from 0 without cancellation (squares of h - mean and their sum have to stay
+ * below 2^128); total receives h, mean and
  * rstd (rows fp32 values each) what the backward pass asks for.
  *   gain (NULL = 1), shift (NULL = 0): cols fp32 values; residual, total, mean, rstd may be NULL.  Types, y in 8 bits with a scale per
  *     row, sizes, alignment and what may be the same matrix: as for alcop_rmsnorm.  A row with an infinity or a NaN
@@ -547,7 +548,8 @@ int alcop_grouped_linear(const void* A, const void* W, const void* offsets, void
 /*
  * Its gradients, as alcop_linear_backward has them.  With dZ = dC * act'(pre), rounded to the type `in`, for every group
  *     dA = alpha * dZ . W_g^T,   dW_g = alpha * A_g^T . dZ_g  (stored as W_g is),   dbias[g][j] = sum of dZ over the group's rows
- * before the rounding; dW_g and dbias[g] of a group without rows are 0, rows of no group are left as they are in dA.
+ * before the rounding; dW_g and dbias[g] of a group without rows are 0, rows of no group are left as they are in dA.  scale_a and scale_w
+ * are no part of it: whoever weighs rows of the products weighs those of dC, and takes the weights' gradient from C.
  *   dA, dW, dbias may be NULL (not all).  Types, alignment and pitches as for alcop_linear_backward; dW_g at dW + g * stridedW,
  *     which do not overlap; dbias: groups x N fp32 values, N below 2^29.  groups <= 64000.
  *   workspace: DEVICE, 16-byte aligned, at least alcop_grouped_linear_backward_workspace_bytes(rows, groups, N, K) bytes,

@@ -16,9 +16,9 @@
 // that takes the largest |dloss| of the rows that count to 2^14 .. 2^15 (G is at most that), and the products by 1 / S.  bf16 has
 // fp32's range, S = 1.
 //
-// What bounds them: the matrix cores.  8192 rows, 65536 x 2048 bf16: 1.83 ms = 1.20 PFLOP/s (the cores 67 % busy at the 1.7 GHz that
-// power leaves), 6 us for the strips.  Gradients of 4096 rows: four pieces of 248 us for the logits and G (1.11 PFLOP/s), 220 for dX and 207
-// for dW, 15 in the end to round dX.  509 x 30011 x 768 fp16, one turn of the card: 31 us, in which 46 MB of new vectors are read, and 5.
+// What bounds them: the matrix cores.  8192 rows, 65536 x 2048 bf16: 1.83 to 1.94 ms by card = 1.20 to 1.13 PFLOP/s (the cores 67 % busy
+// at the 1.7 GHz that power leaves), 6 us for the strips.  Gradients of 4096 rows: four pieces of 248 to 256 us for the logits and G (1.11
+// to 1.08 PFLOP/s), 220 to 226 for dX and 207 to 215 for dW, 15 in the end to round dX.  509 x 30011 x 768 fp16, one turn of the card: 31 us, in which 46 MB of new vectors are read, and 5.
 //
 // Exponents are of 2: u = z log2 e, exp2(u - shift) with u - shift in one fma from the accumulator.
 #pragma once
