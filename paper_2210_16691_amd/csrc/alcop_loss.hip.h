@@ -338,7 +338,7 @@ __global__ void __launch_bounds__(1024) alcop_loss_scale(const LossScaleArgs p)
   }
   top = row_max<1024, HW>(top, lds);
   int e = 14 - ((int)(top >> 23) - 127);
-  e = e > 100 ? 100 : e < -100 ? -100 : e;
+  e = e > 126 ? 126 : e;                   // -113 at least; S and 1 / S are normal numbers
   if (tid == 0) {
     HW::global_store_u32(p.scale, (uint32_t)(127 + e) << 23);
     HW::global_store_u32(p.scale + 1, (uint32_t)(127 - e) << 23);
