@@ -539,7 +539,7 @@ int alcop_layernorm_backward(const void* dy, const void* total, const void* gain
  *     types, alignment and pitches as for alcop_linear, but that bias and scale_w may start at any 4 bytes; strideW a multiple of 8
  *     (ALCOP_E4M3: 16) elements, 0 if all groups have the same.  ALCOP_LINEAR_KERNEL names a kernel here and in the
  *     gradients' dA too, ALCOP_GRADIENT_KERNEL one of dW's (tuning and test knobs).
- * One launch.  1 <= groups < 2^24.  The same call gives the same bits.
+ * One launch, of which every block reads all offsets: meant for thousands of groups.  1 <= groups < 2^24.  The same call gives the same bits.
  */
 int alcop_grouped_linear(const void* A, const void* W, const void* offsets, void* C, int rows, int groups, int N, int K,
                          long lda, long ldw, long strideW, long ldc, int transB, alcop_dtype in, alcop_dtype out,

@@ -531,7 +531,7 @@ def alcop_linear_backward(dC, A, W, dA=None, dW=None, dbias=None, pre=None, act=
                           stream=None):
     """Gradients of alcop_linear: with dZ = dC * act'(pre), dA = alpha * dZ.W^T, dW = alpha * A^T.dZ (stored as W is) and
     dbias = the column sums of dZ; what is None is left out.  dC, A, W, pre have one type, fp16 or bf16; dA and
-    dW that one or both fp32; dbias fp32.  workspace: at least alcop_linear_backward_workspace_bytes(M, N, K) bytes, for
+    dW are both of it or both fp32; dbias fp32.  workspace: at least alcop_linear_backward_workspace_bytes(M, N, K) bytes, for
     an activation or dbias."""
     if _marshal_lib is _lib is not None:
         rc = _marshal.linear_backward(dC, A, W, dA, dW, dbias, pre, act, alpha, transB, workspace, stream)
@@ -736,7 +736,7 @@ def alcop_grouped_linear_backward(dC, A, W, offsets, dA=None, dW=None, dbias=Non
                                   workspace=None, stream=None):
     """Gradients of alcop_grouped_linear: with dZ = dC * act'(pre), dA = alpha * dZ.W[g]^T, dW[g] = alpha * A_g^T.dZ_g (stored as
     W[g] is) and dbias[g] the column sums of dZ over the group's rows (0 for a group without); what is None is left
-    out.  dC, A, W, pre have one type, fp16 or bf16; dA and dW that one or both fp32; dbias fp32 [groups,N].  workspace: at
+    out.  dC, A, W, pre have one type, fp16 or bf16; dA and dW are both of it or both fp32; dbias fp32 [groups,N].  workspace: at
     least alcop_grouped_linear_backward_workspace_bytes(rows, groups, N, K) bytes, for an activation or dbias."""
     if _marshal_lib is _lib is not None:
         rc = _marshal.grouped_linear_backward(dC, A, W, offsets, dA, dW, dbias, pre, act, alpha, transB, workspace, stream)
@@ -808,7 +808,7 @@ def alcop_linear_cross_entropy_backward_workspace_bytes(rows: int, vocab: int, K
 def alcop_linear_cross_entropy_backward(X, W, labels, lse, workspace, dX=None, dW=None, dloss=None, alpha=1.0, stream=None):
     """Gradients of alcop_linear_cross_entropy: with G = dloss * (exp(z - lse) - one(label)), 0 in rows that do not count,
     dX = alpha * G.W and dW = alpha * G^T.X; what is None is left out.  lse as the forward call left it; dloss: an fp32 vector of rows
-    values, None = 1.  dX and dW have X's type, or one or both fp32.  workspace: at least
+    values, None = 1.  dX and dW both have X's type, or both are fp32.  workspace: at least
     alcop_linear_cross_entropy_backward_workspace_bytes(rows, vocab, K) bytes."""
     if _marshal_lib is _lib is not None:
         rc = _marshal.cross_entropy_backward(X, W, labels, lse, workspace, dX, dW, dloss, alpha, stream)
